@@ -369,6 +369,99 @@ uint64_t fastrack_sample_chains(const uint64_t *h_sample_len, uint64_t n_samples
  */
 int fastrack_clock_probe(uint64_t window_us, uint32_t n_probes, uint64_t *d_out, void *stream);
 
+/*
+ * Microscaled (MX) tensors: what crosses the link in few bits and is used on the
+ * GPU as it arrives. A matrix of `cols` columns holds mx_blocks = ceil(cols / 32)
+ * blocks of 32 values a row; a block is its codes and one scale byte e, worth
+ * 2^(e - 127), and the whole block is NaN where e = 255.
+ *   FASTRACK_MX4  16 bytes a block: E2M1 codes (0 0.5 1 1.5 2 3 4 6 and their
+ *                 negatives, sign in bit 3), element 2i in the low half of byte i
+ *   FASTRACK_MX8  32 bytes a block: int8 q, worth q / 64
+ * Codes are [rows][blocks][16 or 32] bytes, 16-byte aligned; scales are
+ * [rows][blocks] bytes of any alignment. The codes of a row past `cols` are zero
+ * (the quantizer writes them so; other sources of codes must too).
+ *
+ * Float matrices are given as an address, an element type and a row stride `ld`
+ * in elements, with neighbouring elements of a row side by side; any alignment of
+ * the element type. An input's stride may be 0 (one row for all); an output's
+ * rows must not overlap. Sizes are at most 2^31 - 1. Where a size is 0 nothing is
+ * read, and a sum over nothing is 0. Outputs must not overlap inputs. Sums are in
+ * 32 bits; an output in 16 bits is rounded once, to nearest even.
+ */
+enum fastrack_type { FASTRACK_BF16 = 0, FASTRACK_FP16 = 1, FASTRACK_FP32 = 2 };
+enum fastrack_mx_format { FASTRACK_MX4 = 4, FASTRACK_MX8 = 8 };
+enum fastrack_mx_activation { FASTRACK_SILU = 0, FASTRACK_GELU = 1 };
+
+/* Bytes of the codes and of the scales of a rows x cols matrix (0 if out of range). */
+uint64_t fastrack_mx_code_bytes(uint32_t format, uint64_t rows, uint64_t cols);
+uint64_t fastrack_mx_scale_bytes(uint64_t rows, uint64_t cols);
+
+/*
+ * Quantize: the block's exponent is floor(log2 of its largest magnitude), less 2
+ * in MX4 (whose largest power is 4), at least -127; each value over the scale goes
+ * to the nearest code, ties to the even one, and past the largest code to that
+ * (6, or 127 / 64). A block that holds a NaN or an infinity gets scale byte 255
+ * and codes 0.
+ * EINVAL: unknown format or type, NULL or misaligned buffers, sizes out of range,
+ * codes or scales overlapping x or each other.
+ */
+int fastrack_mx_quantize(uint32_t format, uint32_t type, const void *d_x, uint64_t ldx, uint64_t rows, uint64_t cols,
+                         uint8_t *d_codes, uint8_t *d_scales, void *stream);
+
+/* The values that the codes stand for (exact in bf16 and fp32; in fp16 rounded,
+ * past its range infinite). EINVAL as for quantize. */
+int fastrack_mx_dequantize(uint32_t format, const uint8_t *d_codes, const uint8_t *d_scales, uint64_t rows,
+                           uint64_t cols, uint32_t type, void *d_out, uint64_t ld_out, void *stream);
+
+/*
+ * An activation that keeps what its gradient needs in 8 bits, in one pass:
+ *   y = f(x), or f(x) * gate where d_gate is not NULL; x (and gate) quantized to MX8
+ * with f(x) = x / (1 + e^-x) (SILU) or x P(x), P the normal distribution (GELU).
+ * The gradients are taken at the kept values x^ and gate^:
+ *   dx = dy * gate^ * f'(x^),  dgate = dy * f(x^)    (no gate: d_gcodes NULL, dx = dy * f'(x^))
+ * EINVAL as for quantize, and an unknown activation.
+ */
+int fastrack_mx_act(uint32_t act, uint32_t type, const void *d_x, uint64_t ldx, const void *d_gate, uint64_t ld_gate,
+                    uint64_t rows, uint64_t cols, void *d_y, uint64_t ldy, uint8_t *d_xcodes, uint8_t *d_xscales,
+                    uint8_t *d_gcodes, uint8_t *d_gscales, void *stream);
+int fastrack_mx_act_grad(uint32_t act, uint32_t type, const void *d_dy, uint64_t ld_dy, const uint8_t *d_xcodes,
+                         const uint8_t *d_xscales, const uint8_t *d_gcodes, const uint8_t *d_gscales, uint64_t rows,
+                         uint64_t cols, void *d_dx, uint64_t ld_dx, void *d_dgate, uint64_t ld_dgate, void *stream);
+
+/*
+ * The products of a linear layer of n outputs and k inputs over m tokens, with its
+ * weights w [n][k] in MX4 and its kept input x^ [m][k] in MX8:
+ *   linear             y[m][n]  = sum over k of x[m][k] w[n][k]
+ *   linear_grad_input  dx[m][k] = sum over n of dy[m][n] w[n][k]
+ *   weight_grad        dw[n][k] = sum over m of dy[m][n] x^[m][k], added to what d_dw
+ *                      holds where accumulate is 1 (32-bit d_dw only)
+ *   linear_mx          linear with x in MX4 as well
+ * Every MX value is exact in bf16, and the products of the float operand's bf16
+ * terms (1 for bf16, 2 for fp16, 3 for fp32) with it are exact: what is rounded is
+ * the 32-bit sum.
+ * d_work: fastrack_mx_work_bytes(...) bytes, 16-byte aligned (NULL if that is 0);
+ * it depends on the float operand's address and stride (an operand that is not
+ * bf16 in whole 16-byte pieces is laid out there first) and on the device.
+ * EINVAL as for quantize; a workspace too small; more than 2^24 output tiles of
+ * 128 x 128.
+ */
+enum fastrack_mx_product { FASTRACK_MX_LINEAR = 0, FASTRACK_MX_GRAD_INPUT = 1, FASTRACK_MX_WEIGHT_GRAD = 2,
+                           FASTRACK_MX_LINEAR_MX = 3 };
+uint64_t fastrack_mx_work_bytes(uint32_t op, uint32_t type, const void *d_a, uint64_t lda, uint64_t m, uint64_t n,
+                                uint64_t k);
+int fastrack_mx_linear(uint32_t type, const void *d_x, uint64_t ldx, const uint8_t *d_codes, const uint8_t *d_scales,
+                       uint64_t m, uint64_t n, uint64_t k, uint32_t out_type, void *d_y, uint64_t ldy, void *d_work,
+                       uint64_t work_bytes, void *stream);
+int fastrack_mx_linear_grad_input(uint32_t type, const void *d_dy, uint64_t ld_dy, const uint8_t *d_codes,
+                                  const uint8_t *d_scales, uint64_t m, uint64_t n, uint64_t k, uint32_t out_type,
+                                  void *d_dx, uint64_t ld_dx, void *d_work, uint64_t work_bytes, void *stream);
+int fastrack_mx_weight_grad(uint32_t type, const void *d_dy, uint64_t ld_dy, const uint8_t *d_codes,
+                            const uint8_t *d_scales, uint64_t m, uint64_t n, uint64_t k, uint32_t out_type, void *d_dw,
+                            uint64_t ld_dw, uint32_t accumulate, void *d_work, uint64_t work_bytes, void *stream);
+int fastrack_mx_linear_mx(const uint8_t *d_xcodes, const uint8_t *d_xscales, const uint8_t *d_codes,
+                          const uint8_t *d_scales, uint64_t m, uint64_t n, uint64_t k, uint32_t out_type, void *d_y,
+                          uint64_t ldy, void *d_work, uint64_t work_bytes, void *stream);
+
 /* Message of the last failure on this thread ("" if none). */
 const char *fastrack_last_error(void);
 

@@ -16,7 +16,8 @@ from . import build as _build
 
 __all__ = ["FastrackError", "decrypt_verify", "decrypt_verify_noalloc", "encrypt_tag", "decrypt_eager", "Eager", "keystream", "apply_verify",
            "pipeline_h2d", "pipeline_d2h", "decrypt_verify_ragged", "encrypt_tag_ragged", "sample_chains", "num_chains", "stage_bytes", "shutdown", "clock_probe", "clock_ghz", "library_path", "F_SEQ_GHASH", "PIPE_FUSED",
-           "PIPE_EAGER", "PIPE_OTP", "PIPE_DIRECT"]
+           "PIPE_EAGER", "PIPE_OTP", "PIPE_DIRECT", "MX4", "MX8", "mx4_quantize", "mx4_dequantize", "mx4_linear",
+           "mx4_linear_grad_input", "mx8_quantize", "mx8_dequantize", "mx8_act", "mx8_act_grad", "mx8_weight_grad"]
 
 F_SEQ_GHASH = 1
 PIPE_FUSED, PIPE_EAGER, PIPE_OTP, PIPE_DIRECT = 0, 1, 2, 3
@@ -85,6 +86,7 @@ def lib():
         L.fastrack_sample_chains.restype = u64
         L.fastrack_clock_probe.argtypes = [u64, u32, vp, vp]
         L.fastrack_clock_probe.restype = _ct.c_int
+        _mx._bind(L)
         L.fastrack_last_error.restype = _ct.c_char_p
         L.fastrack_shutdown.restype = None
         _lib = L
@@ -585,3 +587,8 @@ def clock_ghz(probe):
 def shutdown():
     if _lib is not None:
         _lib.fastrack_shutdown()
+
+
+from . import mx as _mx  # noqa: E402  (uses the helpers above)
+from .mx import (MX4, MX8, mx4_dequantize, mx4_linear, mx4_linear_grad_input, mx4_quantize, mx8_act,  # noqa: E402
+                 mx8_act_grad, mx8_dequantize, mx8_quantize, mx8_weight_grad)

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUT_DIR, "libfastrack.so")
 # Each source with the LLVM scheduling flags it is built with (see below).
-SOURCES = [("kernels.hip", True), ("api.hip", True), ("bitslice.hip", False)]
+SOURCES = [("kernels.hip", True), ("api.hip", True), ("bitslice.hip", False), ("mx.hip", False), ("mx_gemm.hip", False),
+           ("mx_api.hip", False)]
 ARCH = "gfx950"
 
 
@@ -27,7 +28,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(OUT_DIR, exist_ok=True)
     tmp = LIB + ".tmp%d" % os.getpid()
     base = [hipcc(), "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
-            # keep hipcc from forming packed-FP32 instructions (this code has no FP, the flag is policy)
+            # keep hipcc from forming packed-FP32 instructions (the ciphers have no FP, the MX operators do)
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
             "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     # LLVM's iterative max-occupancy scheduler keeps 4-8 table lookups in flight

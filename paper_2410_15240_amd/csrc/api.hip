@@ -610,6 +610,16 @@ FT_EXPORT uint64_t fastrack_num_chains(uint64_t len, uint64_t chain_bytes)
 
 FT_EXPORT const char *fastrack_last_error(void) { return g_err.c_str(); }
 
+// The message that the other sources' entries leave (mx_api.hip).
+namespace fastrack {
+int set_error(int code, const char *msg)
+{
+    g_err = msg;
+    return code;
+}
+void clear_error() { g_err.clear(); }
+}  // namespace fastrack
+
 FT_EXPORT int fastrack_plan(uint64_t len, uint64_t chain_bytes, uint32_t num_cu, uint64_t *out)
 {
     g_err.clear();
