@@ -63,7 +63,7 @@ __device__ __forceinline__ void get(const MxMatrix &q, const Unit &u, float (&v)
 {
     const uint32_t e = q.scales[u.block];
     if (FMT == kMx4)
-        decode4_f32(reinterpret_cast<const uint32_t *>(q.codes)[u.block * 4 + u.lane], scale_f32(e), v);
+        decode4_f32(reinterpret_cast<const uint32_t *>(q.codes)[u.block * 4 + u.lane], scale4_f32(e), v);
     else
         decode8_f32(reinterpret_cast<const u32x2 *>(q.codes)[u.block * 4 + u.lane], scale8_f32(e), v);
 }
@@ -153,12 +153,6 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(Shape sh, MxRows dy,
     store8<T, VEC>(dx.p, u.row * dx.ld, u.c, sh.cols, v);
     if (GATE)
         store8<T, VEC>(dgate.p, u.row * dgate.ld, u.c, sh.cols, g);
-}
-
-// Rows that start on 16-byte boundaries.
-bool vec_rows(const MxRows &r, uint32_t type)
-{
-    return reinterpret_cast<uintptr_t>(r.p) % 16 == 0 && r.ld * mx_type_size(type) % 16 == 0;
 }
 
 // Calls launch(shape, grid) for row ranges of fewer than 2^32 units each.

@@ -93,6 +93,10 @@ __device__ __forceinline__ float scale8_f32(uint32_t e)
     return e == 255u ? bits_f32(0x7FC00000u) : s;
 }
 
+// The same for the conversions from and to E2M1, which read the exponent bits alone: 0 is 2^-127
+// to them, 255 a NaN.
+__device__ __forceinline__ float scale4_f32(uint32_t e) { return bits_f32(e << 23); }
+
 // Eight E2M1 codes as bf16 pairs. Exact: 2 significant bits and any power of two down to
 // 2^-128, which bf16 holds as a subnormal.
 __device__ __forceinline__ u32x4 decode4_bf16(uint32_t codes, float scale)
@@ -112,24 +116,25 @@ __device__ __forceinline__ void decode4_f32(uint32_t codes, float scale, float (
     v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
 }
 
+// Eight int8 codes as floats. (The two words are kept apart from each other: taken as one of 64
+// bits, each byte is cut out by an instruction of its own before the conversion.)
 __device__ __forceinline__ void decode8_f32(u32x2 codes, float scale, float (&v)[8])
 {
+    uint32_t w[2] = {codes[0], codes[1]};
+    asm("" : "+v"(w[0]));
+    asm("" : "+v"(w[1]));
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        v[i] = (float)(int8_t)(codes[i / 4] >> (8 * (i % 4))) * scale;
+        v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * scale;
 }
 
-// Eight int8 codes as bf16 pairs. Exact: 7 significant bits and a power of two down to
-// 2^-133, bf16's smallest subnormal.
-__device__ __forceinline__ u32x4 decode8_bf16(u32x2 codes, float scale)
+// Two of a word's four int8 codes (the lower or the upper ones) as a bf16 pair. Exact: 7
+// significant bits and a power of two down to 2^-133, bf16's smallest subnormal.
+__device__ __forceinline__ uint32_t decode8_pair(uint32_t word, int upper, float scale)
 {
-    float v[8];
-    decode8_f32(codes, scale, v);
-    u32x4 o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        o[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
-    return o;
+    asm("" : "+v"(word));
+    const float a = (float)(int8_t)(word >> (16 * upper)) * scale, b = (float)(int8_t)(word >> (16 * upper + 8)) * scale;
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
 // The largest magnitude of a block, as the bits of |v| (ordered like the values, infinity and
@@ -162,7 +167,7 @@ __device__ __forceinline__ uint32_t encode4(const float (&v)[8], uint32_t e)
 {
     if (e == 255u)
         return 0;
-    const float s = scale_f32(e);
+    const float s = scale4_f32(e);
     uint32_t o = 0;
     o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[0], v[1], s, 0);
     o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[2], v[3], s, 1);

@@ -23,14 +23,16 @@ struct Gemm {
     MxMatrix q;
     uint32_t nb;             // blocks in a row of q
     uint32_t m, n, k;        // output m x n, summed axis k
+    uint32_t planes;
+    uint32_t whole;          // whole stages of a term that are read unchecked
     uint32_t stages;         // planes * ceil(k / kBK)
-    uint32_t kstages;        // ceil(k / kBK)
     uint32_t splits, per;    // parts of the sum, stages in each
     uint32_t tm, tn;         // output tiles
     void *c;
     uint64_t ldc;
     uint32_t ctype;
     uint32_t accumulate;
+    uint32_t c_vec;          // rows of c start on 16-byte boundaries
     float *parts;            // [splits][m][n] where splits > 1
 };
 
@@ -49,67 +51,279 @@ __device__ __forceinline__ uint32_t at_t(uint32_t r, uint32_t col)
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// A 32 x 16 operand of the matrix instruction: lane l holds 8 consecutive values of the
-// summed axis, from 8 (l / 32), of row l % 32.
-__device__ __forceinline__ bf16x8 frag_k(const uint8_t *t, uint32_t row0, uint32_t ks, uint32_t lane)
+// Tile of workgroup `id`. Workgroups go to the 8 XCDs in turn, each with its own L2: an XCD
+// takes a run of neighbouring tiles, in bands of 8 tile rows, so that the tiles it works on at
+// one time share rows of both operands.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t &m, uint32_t &n)
 {
-    return *reinterpret_cast<const bf16x8 *>(t + at_k(row0 + (lane & 31), ks * 2 + (lane >> 5)));
+    constexpr uint32_t kXcds = 8, kBand = 8;
+    const uint32_t tiles = tm * tn, q = tiles / kXcds, r = tiles % kXcds, x = id % kXcds;
+    const uint32_t i = x * q + min(x, r) + id / kXcds;
+    const uint32_t band = i / (kBand * tn), first = band * kBand, rows = min(kBand, tm - first), j = i - first * tn;
+    m = first + j % rows;
+    n = j / rows;
 }
 
-// The same from a tile stored along the output axis: in each group of 16 lanes, lane j gives
-// the address of 4 columns of row j / 4 and receives column j of the 4 rows.
-template <int W>
-__device__ __forceinline__ bf16x8 frag_t(uint8_t *t, uint32_t col0, uint32_t ks, uint32_t lane)
+// Offsets of a lane's reads of the matrix instruction's 32 x 16 operands, where lane l holds 8
+// consecutive values of the summed axis, from 8 (l / 32), of row l % 32. In a tile stored along
+// the summed axis they differ by the step (16 values) in the turned bits, and squares of 32
+// rows follow each other.
+__device__ __forceinline__ uint32_t frag_k_at(uint32_t row0, uint32_t ks, uint32_t lane)
 {
-    const uint32_t j = lane & 15, r = ks * 16 + (lane >> 5) * 8 + (j >> 2), c = col0 + ((lane >> 4) & 1) * 16 + (j & 3) * 4;
+    return at_k(row0 + (lane & 31), ks * 2 + (lane >> 5));
+}
+
+// In a tile stored along the output axis: in each group of 16 lanes, lane j gives the address
+// of 4 columns of row j / 4 and receives column j of the 4 rows. Squares of 32 columns differ
+// in the turned bits, and steps of 16 rows follow each other.
+template <int W>
+__device__ __forceinline__ uint32_t frag_t_at(uint32_t col0, uint32_t lane)
+{
+    const uint32_t j = lane & 15;
+    return at_t<W>((lane >> 5) * 8 + (j >> 2), col0 + ((lane >> 4) & 1) * 16 + (j & 3) * 4);
+}
+
+__device__ __forceinline__ bf16x8 read_k(const uint8_t *p) { return *reinterpret_cast<const bf16x8 *>(p); }
+
+template <int W>
+__device__ __forceinline__ bf16x8 read_t(uint8_t *p)
+{
     typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(t + at_t<W>(r, c)));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(t + at_t<W>(r + 4, c)));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * W * 2));
     return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// One 128 x 128 tile of c, or of one part of it. TA: a is summed over its rows (a[k][m])
-// instead of along them (a[m][k]); TB: the same of the MX matrix.
-template <uint32_t FMT, bool TA, bool TB>
-__global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm g)
+// Memory from one address for the whole wave, read at 32-bit offsets of its lanes. (Through
+// plain pointers the compiler keeps every lane's offset in 64 bits and adds it to the address
+// at each load.)
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_at(const void *p)
 {
-    constexpr int BM = 128, BN = 128;
-    __shared__ __align__(16) uint8_t sa[BM * kBK * 2], sb[BN * kBK * 2];
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0xFFFFFFFFu, 0x00027000);
+}
+
+// All waves' LDS accesses before it are done. (Loads from memory may still be on their way.)
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Where a product's results go: parts of a sum as 32-bit floats, or c itself.
+struct Out {
+    void *p;
+    uint64_t ld;
+    uint32_t type, accumulate;
+    bool vec;   // rows start on 16-byte boundaries
+};
+
+// Columns [c, c + 8) of a row.
+__device__ __forceinline__ void put8(const Out &o, uint32_t row, uint32_t c, uint32_t cols, float (&v)[8])
+{
+    const uint64_t at = row * o.ld;
+    if (o.type == kFp32) {
+        if (o.accumulate) {
+            float w[8];
+            load8<kFp32, false>(o.p, at, c, cols, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] += w[i];
+        }
+        o.vec ? store8<kFp32, true>(o.p, at, c, cols, v) : store8<kFp32, false>(o.p, at, c, cols, v);
+    } else if (o.type == kBf16) {
+        o.vec ? store8<kBf16, true>(o.p, at, c, cols, v) : store8<kBf16, false>(o.p, at, c, cols, v);
+    } else {
+        o.vec ? store8<kFp16, true>(o.p, at, c, cols, v) : store8<kFp16, false>(o.p, at, c, cols, v);
+    }
+}
+
+// A workgroup's results, 2 x 2 waves of MI x NJ squares of 32: lane l of a wave holds column
+// l % 32 of rows 8 (r / 4) + 4 (l / 32) + r % 4 of each. They pass through LDS, 64 rows at a
+// time, so that c is written in whole rows of the tile. Rows whose bit 2 is set are turned by
+// 32 columns: the two halves of a wave then write to different banks.
+template <int MI, int NJ>
+__device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds, uint32_t m0, uint32_t n0, uint32_t m,
+                                         uint32_t n, const Out &o)
+{
+    constexpr uint32_t BN = 64 * NJ;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    uint32_t id = blockIdx.x;
-    const uint32_t tiles = g.tm * g.tn, part = id / tiles;
-    id -= part * tiles;
-    const uint32_t m0 = id / g.tn * BM, n0 = id % g.tn * BN;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        if (i)
+            __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const uint32_t y = (wave >> 1) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
+                const uint32_t x = (wave & 1) * 32 * NJ + j * 32 + (lane & 31);
+                lds[y * BN + (x ^ ((y & 4) << 3))] = acc[i][j][r];
+            }
+        __syncthreads();
+#pragma unroll 2
+        for (uint32_t u = t; u < 64 * BN / 8; u += kThreads) {
+            const uint32_t y = u / (BN / 8), x = u % (BN / 8) * 8;
+            const uint32_t row = m0 + (y >> 5) * 32 * MI + i * 32 + (y & 31), col = n0 + x;
+            const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * BN + (x ^ ((y & 4) << 3)));
+            const f32x4 lo = p[0], hi = p[1];
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (row < m && col < n)
+                put8(o, row, col, n, v);
+        }
+    }
+}
+
+// One tile of c, or of one part of it, by 2 x 2 waves of 32 MI x 32 NJ outputs each. TA: a is
+// summed over its rows (a[k][m]) instead of along them (a[m][k]); TB: the same of the MX
+// matrix. While a stage of 64 summed values is multiplied out of one half of the LDS, the next
+// one is decoded from registers to bf16 in the other half, and the one after is on its way
+// from memory.
+//
+// Stages of 64 whole values come first, of every term of a, then the terms' last, short ones.
+// A whole stage is read without a check: rows and columns past the matrices' ends read the
+// last ones again, for results that are not stored. (Rows so long that a tile spans 2^32
+// bytes have no such stages; all of theirs are checked.)
+template <uint32_t FMT, bool TA, bool TB, int MI, int NJ>
+__global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gemm g)
+{
+    constexpr int BM = 64 * MI, BN = 64 * NJ, UA = BM * 8 / kThreads, UB = BN * 8 / kThreads;
+    constexpr uint32_t CB = FMT == kMx4 ? 4 : 8;   // bytes of 8 codes
+    constexpr uint32_t kA = BM * kBK * 2, kHalf = kA + BN * kBK * 2;
+    __shared__ __align__(16) uint8_t lds[2 * kHalf];   // two stages, each a tile of a and one of the MX matrix
+    const uint32_t t = threadIdx.x;
+    const uint32_t lane = t & 63, wave = t >> 6;
+    const uint32_t tiles = g.tm * g.tn, part = blockIdx.x / tiles;
+    uint32_t tile_m, tile_n;
+    tile_of(blockIdx.x - part * tiles, g.tm, g.tn, tile_m, tile_n);
+    const uint32_t m0 = tile_m * BM, n0 = tile_n * BN;
+    const uint32_t wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NJ;
     const uint32_t s_begin = part * g.per, s_end = min(g.stages, s_begin + g.per);
+    const uint32_t full = g.whole, nfull = full * g.planes;   // whole stages of a term, of all
 
-    f32x16 acc[2][2] = {};
-    u32x4 ra[4];
-    u32x2 rb[4];
-    uint32_t re[4];
+    f32x16 acc[MI][NJ] = {};
+    u32x4 ra[UA];
+    u32x2 rb[UB];
+    uint8_t re[UB];
 
-    auto load = [&](uint32_t s) {
-        const uint32_t plane = s / g.kstages, k0 = (s - plane * g.kstages) * kBK;
+    // Offsets in the LDS: of the reads (see frag_k_at, frag_t_at), and of this thread's writes.
+    uint32_t fa_at[4], fb_at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        fa_at[i] = TA ? frag_t_at<BM>(wm + i % MI * 32, lane) : frag_k_at(wm, i, lane);
+        fb_at[i] = kA + (TB ? frag_t_at<BN>(wn + i % NJ * 32, lane) : frag_k_at(wn, i, lane));
+    }
+    const uint32_t wa_at = TA ? at_t<BM>(t / (BM / 8), t % (BM / 8) * 8) : at_k(t / 8, t % 8);
+    const uint32_t wb_at = kA + (TB ? at_t<BN>(t / (BN / 8), t % (BN / 8) * 8) : at_k(t / 8, t % 8));
+
+    // A whole stage: one address for the workgroup and 32-bit offsets of the lanes, in bytes.
+    uint32_t oa[UA], ob[UB], oe[UB];
+#pragma unroll
+    for (int i = 0; i < UA; ++i) {
+        const uint32_t u = i * kThreads + t;
+        if (TA)
+            oa[i] = u / (BM / 8) * (uint32_t)g.lda * 2 + min(u % (BM / 8) * 8, (g.m - 1 - m0) & ~7u) * 2;
+        else
+            oa[i] = min(u / 8, g.m - 1 - m0) * (uint32_t)g.lda * 2 + u % 8 * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < UB; ++i) {
+        const uint32_t u = i * kThreads + t;
+        const uint32_t row = TB ? u / (BN / 8) : min(u / 8, g.n - 1 - n0);
+        const uint32_t unit = TB ? min(u % (BN / 8), (g.nb - n0 / 32) * 4 - 1) : u % 8;
+        ob[i] = row * g.nb * (4 * CB) + unit * CB;
+        oe[i] = row * g.nb + unit / 4;
+    }
+    // Where whole stage `at` of the terms' whole stages lies. Stages are visited in order: going on
+    // to the next is an addition, and at the end of a term one back to the MX matrix's start.
+    const uint64_t block0 = TB ? n0 / 32 : (uint64_t)n0 * g.nb, block_step = TB ? (uint64_t)kBK * g.nb : kBK / 32;
+    const int64_t a_step = TA ? kBK * g.lda * 2 : kBK * 2;
+    uint32_t at = 0;   // within its term
+    const uint8_t *pa = nullptr, *pc = nullptr, *ps = nullptr;
+    auto go_to = [&](uint32_t s) {
+        const uint32_t plane = s / full;
+        at = s - plane * full;
+        pa = reinterpret_cast<const uint8_t *>(g.a + plane * g.a_plane + (TA ? (uint64_t)m0 : m0 * g.lda)) + at * a_step;
+        pc = g.q.codes + (block0 + at * block_step) * (4 * CB);
+        ps = g.q.scales + block0 + at * block_step;
+    };
+    const int64_t a_back = (int64_t)g.a_plane * 2 - (int64_t)(full - 1) * a_step, block_back = -(int64_t)(full - 1) * block_step;
+    auto next = [&](int third) {
+        if (third == 0) {
+            at = at + 1 == full ? 0 : at + 1;
+            pa += at ? a_step : a_back;
+        } else if (third == 1) {
+            pc += (at ? (int64_t)block_step : block_back) * (4 * CB);
+        } else {
+            ps += at ? (int64_t)block_step : block_back;
+        }
+    };
+    auto load_a = [&](int i) { ra[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer_at(pa), oa[i], 0, 0); };
+    auto load_b = [&](int i) {
+        if (FMT == kMx4)
+            rb[i][0] = __builtin_amdgcn_raw_buffer_load_b32(buffer_at(pc), ob[i], 0, 0);
+        else
+            rb[i] = __builtin_amdgcn_raw_buffer_load_b64(buffer_at(pc), ob[i], 0, 0);
+        re[i] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(ps), oe[i], 0, 0);
+    };
+    // The next stage's way from registers to the LDS, in small items, and its registers' next
+    // load: per group one or two units of the MX matrix (the scale, then the codes in pairs or
+    // all of E2M1's, then the write) and as many of a.
+    constexpr int kPieces = FMT == kMx4 ? 2 : 6, kGroup = UB / (UB < UA ? UB : UA) * kPieces + 1, kItems = kGroup * UA;
+    static_assert(UA == UB, "groups of one unit each");
+    float scale;
+    u32x4 dec;
+    auto item = [&](uint8_t *half, int y, bool again) {
+        const int i = y / kGroup, p = y % kGroup;
+        if (p == kGroup - 1) {
+            *reinterpret_cast<u32x4 *>(half + wa_at + i * 4096) = ra[i];
+            if (again)
+                load_a(i);
+            return;
+        }
+        if (p == 0)
+            scale = FMT == kMx4 ? scale4_f32(re[i]) : scale8_f32(re[i]);
+        if (FMT == kMx8 && p >= 1 && p <= 4)
+            dec[p - 1] = decode8_pair(rb[i][(p - 1) / 2], (p - 1) % 2, scale);
+        if (p == kPieces - 1) {
+            if (FMT == kMx4)
+                dec = decode4_bf16(rb[i][0], scale);
+            *reinterpret_cast<u32x4 *>(half + wb_at + i * 4096) = dec;
+            if (again)
+                load_b(i);
+        }
+    };
+    auto load_whole = [&](uint32_t s) {   // in the order of the main loop
+        go_to(s);
+#pragma unroll
+        for (int i = 0; i < UA; ++i) {
+            load_b(i);
+            __builtin_amdgcn_sched_barrier(0);
+            load_a(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Any stage, with every address checked; what lies outside is 0.
+    auto load_short = [&](uint32_t i) {
+        const uint32_t per = (g.k + kBK - 1) / kBK - full, plane = i / per, k0 = (full + i - plane * per) * kBK;
         const uint16_t *a = g.a + plane * g.a_plane;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < UA; ++i) {
             const uint32_t u = i * kThreads + t;
-            uint32_t row, col;   // of a
-            bool in;
-            if (TA) {
-                row = k0 + u / (BM / 8), col = m0 + u % (BM / 8) * 8;
-                in = row < g.k && col < g.m;
-            } else {
-                row = m0 + u / 8, col = k0 + u % 8 * 8;
-                in = row < g.m && col < g.k;
-            }
+            const uint32_t row = TA ? k0 + u / (BM / 8) : m0 + u / 8, col = TA ? m0 + u % (BM / 8) * 8 : k0 + u % 8 * 8;
+            const bool in = row < (TA ? g.k : g.m) && col < (TA ? g.m : g.k);
             ra[i] = in ? *reinterpret_cast<const u32x4 *>(a + row * g.lda + col) : u32x4{0, 0, 0, 0};
-            const uint32_t qrow = TB ? k0 + u / (BN / 8) : n0 + u / 8;
+        }
+#pragma unroll
+        for (int i = 0; i < UB; ++i) {
+            const uint32_t u = i * kThreads + t;
+            const uint32_t row = TB ? k0 + u / (BN / 8) : n0 + u / 8;
             const uint32_t unit = TB ? n0 / 8 + u % (BN / 8) : k0 / 8 + u % 8;   // 8 codes, 4 to a block
-            in = qrow < (TB ? g.k : g.n) && unit / 4 < g.nb;
             rb[i] = u32x2{0, 0};
             re[i] = 0;
-            if (in) {
-                const uint64_t at = (uint64_t)qrow * g.nb;
+            if (row < (TB ? g.k : g.n) && unit / 4 < g.nb) {
+                const uint64_t at = (uint64_t)row * g.nb;
                 re[i] = g.q.scales[at + unit / 4];
                 if (FMT == kMx4)
                     rb[i][0] = reinterpret_cast<const uint32_t *>(g.q.codes)[at * 4 + unit];
@@ -118,66 +332,123 @@ __global__ __launch_bounds__(kThreads) void gemm_kernel(Gemm g)
             }
         }
     };
-    auto store = [&]() {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t u = i * kThreads + t;
-            const uint32_t pa = TA ? at_t<BM>(u / (BM / 8), u % (BM / 8) * 8) : at_k(u / 8, u % 8);
-            *reinterpret_cast<u32x4 *>(sa + pa) = ra[i];
-            const uint32_t pb = TB ? at_t<BN>(u / (BN / 8), u % (BN / 8) * 8) : at_k(u / 8, u % 8);
-            *reinterpret_cast<u32x4 *>(sb + pb) =
-                FMT == kMx4 ? decode4_bf16(rb[i][0], scale_f32(re[i])) : decode8_bf16(rb[i], scale8_f32(re[i]));
+    auto load = [&](uint32_t s) {
+        if (s < nfull) {
+            load_whole(s);
+        } else {
+            load_short(s - nfull);
         }
     };
-
-    if (s_begin < s_end)
-        load(s_begin);
-    for (uint32_t s = s_begin; s < s_end; ++s) {
-        store();
-        __syncthreads();
-        if (s + 1 < s_end)
-            load(s + 1);
-        const uint32_t wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+    bf16x8 fa[2][MI], fb[2][NJ];
+    auto read = [&](uint8_t *half, int ks, int to, int r) {   // operand r of a step
+        if (r < MI)
+            fa[to][r] = TA ? read_t<BM>(half + fa_at[r] + ks * 16 * BM * 2) : read_k(half + fa_at[ks] + r * 4096);
+        else
+            fb[to][r - MI] = TB ? read_t<BN>(half + fb_at[r - MI] + ks * 16 * BN * 2)
+                                : read_k(half + fb_at[ks] + (r - MI) * 4096);
+    };
+    // A step multiplies 16 values of the sum out of registers. `beside(x)` is what is issued
+    // after product x: the matrix unit is busy 32 cycles with each, so the rest of the wave's work
+    // is dealt out between them, in this order.
+    constexpr int P = MI * NJ, R = MI + NJ;
+    auto step = [&](int regs, auto beside) {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            bf16x8 fa[2], fb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fa[i] = TA ? frag_t<BM>(sa, wm + i * 32, ks, lane) : frag_k(sa, wm + i * 32, ks, lane);
-                fb[i] = TB ? frag_t<BN>(sb, wn + i * 32, ks, lane) : frag_k(sb, wn + i * 32, ks, lane);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        for (int x = 0; x < P; ++x) {
+            acc[x / NJ][x % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[regs][x / NJ], fb[regs][x % NJ],
+                                                                          acc[x / NJ][x % NJ], 0, 0, 0);
+            beside(x);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __syncthreads();
+    };
+    // Item y of n dealt over the products [from, to): whether it comes after product x.
+    auto turn = [](int x, int y, int n, int from, int to) { return from + y * (to - from) / n == x; };
+    // One stage, out of `here`, whose first operands are in registers: each step multiplies what
+    // the one before has read. The next stage goes to `there` beside the first three steps
+    // (`beside(x)` after product x of their 3 P), and its first operands are read under the last.
+    auto stage = [&](uint8_t *here, uint8_t *there, auto beside, auto last) {
+#pragma unroll
+        for (int ks = 0; ks < 3; ++ks)
+            step(ks & 1, [&](int x) {
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (turn(x, r, R, 0, P / 2))
+                        read(here, ks + 1, (ks + 1) & 1, r);
+                beside(ks * P + x);
+            });
+        step(1, [&](int x) {
+            if (x == P / 4)
+                lds_barrier();
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (turn(x, r, R, P / 4, P * 3 / 4))
+                    read(there, 0, 0, r);
+            last(x);
+        });
+    };
+
+    if (s_begin < s_end) {
+        uint8_t *const h0 = lds, *const h1 = lds + kHalf;
+        auto put = [&](uint8_t *half) {
+#pragma unroll
+            for (int y = 0; y < kItems; ++y)
+                item(half, y, false);
+        };
+        auto begin = [&](auto ld) {
+            ld(s_begin);
+            put(h0);
+            if (s_begin + 1 < s_end)
+                ld(s_begin + 1);
+            lds_barrier();
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                read(h0, 0, 0, r);
+        };
+        uint32_t s = s_begin;
+        auto whole = [&](uint8_t *here, uint8_t *there) {
+            stage(here, there, [&](int x) {
+#pragma unroll
+                for (int y = 0; y < kItems; ++y)
+                    if (turn(x, y, kItems, 0, 3 * P))
+                        item(there, y, true);
+            }, [&](int x) {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (turn(x, i, 3, P / 2, P))
+                        next(i);
+            });
+            ++s;
+        };
+        // (The main loop has a way in of its own: the waits it puts before its registers' use
+        // count the loads issued since, on every way in.)
+        if (s + 3 < min(s_end, nfull)) {
+            begin(load_whole);
+            go_to(s + 2);
+            do {
+                whole(h0, h1);
+                whole(h1, h0);
+            } while (s + 3 < min(s_end, nfull));
+        } else {
+            begin(load);
+        }
+        uint32_t h = 0;
+        for (; s < s_end; ++s, h ^= 1) {
+            uint8_t *here = lds + h * kHalf, *there = lds + (h ^ 1) * kHalf;
+            stage(here, there, [&](int x) {
+                if (x == 3 * P - 1) {
+                    if (s + 1 < s_end)
+                        put(there);
+                    if (s + 2 < s_end)
+                        load(s + 2);
+                }
+            }, [](int) {});
+        }
+        lds_barrier();
     }
 
-    // Lane l holds column l % 32 of rows 8 (r / 4) + 4 (l / 32) + r % 4.
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t row = m0 + (wave >> 1) * 64 + i * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-                const uint32_t col = n0 + (wave & 1) * 64 + j * 32 + (lane & 31);
-                if (row >= g.m || col >= g.n)
-                    continue;
-                const float v = acc[i][j][r];
-                if (g.splits > 1) {
-                    g.parts[((uint64_t)part * g.m + row) * g.n + col] = v;
-                } else if (g.ctype == kFp32) {
-                    float *p = reinterpret_cast<float *>(g.c) + row * g.ldc + col;
-                    *p = g.accumulate ? *p + v : v;
-                } else if (g.ctype == kBf16) {
-                    reinterpret_cast<__bf16 *>(g.c)[row * g.ldc + col] = (__bf16)v;
-                } else {
-                    reinterpret_cast<_Float16 *>(g.c)[row * g.ldc + col] = (_Float16)v;
-                }
-            }
+    Out o = {g.c, g.ldc, g.ctype, g.accumulate, g.c_vec != 0};
+    if (g.splits > 1)
+        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
+    put_tile<MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
 // c = the sum of the parts, always in the same order.
@@ -241,7 +512,8 @@ uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 struct Plan {
     bool in_place;
     uint64_t a_rows, a_cols, a_ld, a_bytes;   // a's terms in the workspace, where not in place
-    uint32_t kstages, stages, splits, per, tm, tn;
+    uint32_t planes, stages, splits, per, tm, tn;
+    int tile;                                 // side of an output tile
     uint64_t m, n, k;                         // output m x n, summed axis k
     uint64_t bytes() const { return a_bytes + (splits > 1 ? (uint64_t)splits * m * n * 4 : 0); }
 };
@@ -259,10 +531,11 @@ Plan plan_of(const MxProduct &p, int num_cu)
     r.in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 16 == 0 && p.a.ld % 8 == 0 && r.a_cols % 8 == 0;
     r.a_ld = round_up(r.a_cols, 8);
     r.a_bytes = r.in_place ? 0 : round_up(planes_of(p.type) * r.a_rows * r.a_ld * 2, 256);
-    r.kstages = (uint32_t)((r.k + kBK - 1) / kBK);
-    r.stages = r.kstages * (r.in_place ? 1 : planes_of(p.type));
-    r.tm = (uint32_t)((r.m + 127) / 128);
-    r.tn = (uint32_t)((r.n + 127) / 128);
+    r.planes = r.in_place ? 1 : planes_of(p.type);
+    r.stages = (uint32_t)((r.k + kBK - 1) / kBK) * r.planes;
+    r.tile = (r.m + 255) / 256 * ((r.n + 255) / 256) >= (uint64_t)num_cu / 2 ? 256 : 128;
+    r.tm = (uint32_t)((r.m + r.tile - 1) / r.tile);
+    r.tn = (uint32_t)((r.n + r.tile - 1) / r.tile);
     // Fewer tiles than CUs: cut the sum, down to 4 stages a part.
     const uint64_t tiles = (uint64_t)r.tm * r.tn;
     uint64_t splits = tiles >= (uint64_t)num_cu ? 1 : (uint64_t)num_cu * 2 / (tiles ? tiles : 1);
@@ -288,6 +561,7 @@ struct Gemm4 {
     void *c;
     uint64_t ldc;
     uint32_t ctype;
+    uint32_t c_vec;
     float *parts;
 };
 
@@ -300,7 +574,8 @@ __global__ __launch_bounds__(kThreads) void gemm4_kernel(Gemm4 g)
 {
     constexpr int BM = 128, BN = 128;
     typedef int i32x8 __attribute__((ext_vector_type(8)));
-    __shared__ __align__(16) uint8_t sa[BM * kBK4 / 2], sb[BN * kBK4 / 2];
+    __shared__ __align__(16) uint8_t sl[64 * BN * 4];   // both tiles of a stage; results on their way out
+    uint8_t *sa = sl, *sb = sl + BM * kBK4 / 2;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     uint32_t id = blockIdx.x;
     const uint32_t tiles = g.tm * g.tn, part = id / tiles;
@@ -372,26 +647,10 @@ __global__ __launch_bounds__(kThreads) void gemm4_kernel(Gemm4 g)
         }
         __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t row = m0 + wm + i * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-                const uint32_t col = n0 + wn + j * 32 + (lane & 31);
-                if (row >= g.m || col >= g.n)
-                    continue;
-                const float v = acc[i][j][r];
-                if (g.splits > 1)
-                    g.parts[((uint64_t)part * g.m + row) * g.n + col] = v;
-                else if (g.ctype == kFp32)
-                    reinterpret_cast<float *>(g.c)[row * g.ldc + col] = v;
-                else if (g.ctype == kBf16)
-                    reinterpret_cast<__bf16 *>(g.c)[row * g.ldc + col] = (__bf16)v;
-                else
-                    reinterpret_cast<_Float16 *>(g.c)[row * g.ldc + col] = (_Float16)v;
-            }
+    Out o = {g.c, g.ldc, g.ctype, 0, g.c_vec != 0};
+    if (g.splits > 1)
+        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
+    put_tile<2, 2>(acc, reinterpret_cast<float *>(sl), m0, n0, g.m, g.n, o);
 }
 
 Gemm4 plan4_of(const Mx4Product &p, int num_cu)
@@ -438,7 +697,7 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
         g.lda = r.a_ld;
         g.a_plane = r.a_rows * r.a_ld;
         const uint64_t units = r.a_rows * (r.a_ld / 8);
-        const bool vec = reinterpret_cast<uintptr_t>(p.a.p) % 16 == 0 && p.a.ld * mx_type_size(p.type) % 16 == 0;
+        const bool vec = vec_rows(p.a, p.type);
         const dim3 grid((uint32_t)((units + kThreads - 1) / kThreads));
 #define MX_TERMS(T)                                                                                                   \
     do {                                                                                                              \
@@ -466,7 +725,10 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     g.n = (uint32_t)r.n;
     g.k = (uint32_t)r.k;
     g.stages = r.stages;
-    g.kstages = r.kstages ? r.kstages : 1;
+    g.planes = r.planes;
+    const bool ta = p.op == kWeightGrad, tb = p.op != kLinear;
+    const uint64_t span_a = (ta ? kBK : 256) * g.lda * 2 + 512, span_b = (tb ? kBK : 256) * (uint64_t)g.nb * 32 + 8192;
+    g.whole = span_a < 1ull << 32 && span_b < 1ull << 32 ? g.k / kBK : 0;
     g.splits = r.splits;
     g.per = r.per;
     g.tm = r.tm;
@@ -475,14 +737,23 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     g.ldc = p.c.ld;
     g.ctype = p.ctype;
     g.accumulate = p.accumulate;
+    g.c_vec = vec_rows(p.c, p.ctype);
     g.parts = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.work) + r.a_bytes);
     const dim3 grid(r.tm * r.tn * r.splits);
+#define MX_GEMM(...)                                                                               \
+    do {                                                                                           \
+        if (r.tile == 256)                                                                         \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 4, 4>), grid, dim3(kThreads), 0, s, g);   \
+        else                                                                                       \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 2>), grid, dim3(kThreads), 0, s, g);   \
+    } while (0)
     if (p.op == kLinear)
-        hipLaunchKernelGGL((gemm_kernel<kMx4, false, false>), grid, dim3(kThreads), 0, s, g);
+        MX_GEMM(kMx4, false, false);
     else if (p.op == kGradInput)
-        hipLaunchKernelGGL((gemm_kernel<kMx4, false, true>), grid, dim3(kThreads), 0, s, g);
+        MX_GEMM(kMx4, false, true);
     else
-        hipLaunchKernelGGL((gemm_kernel<kMx8, true, true>), grid, dim3(kThreads), 0, s, g);
+        MX_GEMM(kMx8, true, true);
+#undef MX_GEMM
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || r.splits == 1)
         return e;
@@ -506,6 +777,7 @@ hipError_t launch_mx4_product(const Mx4Product &p, int num_cu, hipStream_t s)
     g.c = p.c.p;
     g.ldc = p.c.ld;
     g.ctype = p.ctype;
+    g.c_vec = vec_rows(p.c, p.ctype);
     g.parts = reinterpret_cast<float *>(p.work);
     hipLaunchKernelGGL(gemm4_kernel, dim3(g.tm * g.tn * g.splits), dim3(kThreads), 0, s, g);
     const hipError_t e = hipGetLastError();

@@ -216,6 +216,21 @@ def test_products_are_exact_on_whole_numbers(op, name, m, n, k):
 
 @pytest.mark.parametrize("op", ["linear", "grad", "weight"])
 @pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("rows,cols,sums", [(3001, 2888, 136), (2900, 3009, 700), (4096, 2304, 64), (2823, 2817, 5),
+                                            (260, 32008, 320)])
+def test_products_with_many_outputs_are_exact_on_whole_numbers(op, name, rows, cols, sums):
+    """Enough output tiles for every CU: the largest tiles, with edges, whole stages of the sum and short ones."""
+    m, n, k = dict(linear=(rows, cols, sums), grad=(rows, sums, cols), weight=(sums, rows, cols))[op]
+    rng = np.random.default_rng(rows + cols + sums)
+    x, q, _, f = layer(rng, op, m, n, k, "whole")
+    want = torch.from_numpy(f(x)).float()
+    for pad in (0, 3):
+        got = product(op, gpu(x, TYPES[name], pad), q, dtype=torch.float32).cpu()
+        assert torch.equal(got, want), (pad, torch.nonzero(got != want)[:4].tolist())
+
+
+@pytest.mark.parametrize("op", ["linear", "grad", "weight"])
+@pytest.mark.parametrize("name", list(TYPES))
 @pytest.mark.parametrize("out", list(TYPES))
 @pytest.mark.parametrize("m,n,k", [(1, 96, 700), (29, 200, 333), (150, 140, 260), (300, 30, 70)])
 def test_products_of_normal_inputs(op, name, out, m, n, k):
