@@ -36,9 +36,9 @@ struct Gemm {
     float *parts;            // [splits][m][n] where splits > 1
 };
 
-// 16-byte chunk c of row r of a tile whose rows are 128 bytes: the low three bits of the row
-// turn the chunk's place, so that a wave's reads of one chunk from 32 rows use every bank.
-__device__ __forceinline__ uint32_t at_k(uint32_t r, uint32_t c) { return r * 128 + ((c ^ (r & 7)) << 4); }
+// 16-byte chunk c of row r of a tile whose rows are 128 bytes: bits 1 to 3 of the row turn the
+// chunk's place, so that one chunk of 16 rows in turn lies in all 64 banks, once in each.
+__device__ __forceinline__ uint32_t at_k(uint32_t r, uint32_t c) { return r * 128 + ((c ^ ((r >> 1) & 7)) << 4); }
 
 // A tile stored along the output axis, rows of W columns: 64-byte groups of a row are turned
 // by its low two bits, since a transposing read takes 4 rows of one 64-byte group at once.
