@@ -13,6 +13,11 @@
 namespace fastrack {
 namespace mx {
 
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
+
 constexpr int kThreads = 256;   // 4 waves, 2 x 2 over the output tile
 constexpr uint32_t kBK = 64;    // of the summed axis, at a time
 
@@ -552,12 +557,14 @@ Plan plan_of(const MxProduct &p, int num_cu)
 
 // ---- MX4 x MX4 -------------------------------------------------------------------------
 
-constexpr uint32_t kBK4 = 128;
+constexpr uint32_t kBK4 = 256;   // 8 blocks: rows of 128 bytes, as above
 
 struct Gemm4 {
     MxMatrix x, w;
     uint32_t nb, m, n;
+    uint32_t whole;          // stages of 8 blocks that are read unchecked
     uint32_t stages, splits, per, tm, tn;
+    int tile;
     void *c;
     uint64_t ldc;
     uint32_t ctype;
@@ -565,92 +572,247 @@ struct Gemm4 {
     float *parts;
 };
 
-// Rows of 64 bytes (4 blocks): the chunk's place turned by bits 1 and 2 of the row.
-__device__ __forceinline__ uint32_t at4(uint32_t r, uint32_t c) { return r * 64 + ((c ^ ((r >> 1) & 3)) << 4); }
+typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// Both operands stay in 4 bits: the scaled matrix instruction takes 32 codes and their
-// block's scale byte per lane, rows l % 32, block l / 32.
-__global__ __launch_bounds__(kThreads) void gemm4_kernel(Gemm4 g)
+// Both operands stay in 4 bits: the scaled matrix instruction takes 32 codes and their block's
+// scale byte per lane, row l % 32, block l / 32. A stage of 8 blocks is laid out, copied and
+// read like one of 64 bf16 values above (16 bytes are a block here), and its 8 scales of each
+// row beside it. A lane reads its row's 8 scales at once, and the instruction picks the byte:
+// blocks 2 ks of the lower lanes, 2 ks + 1 of the upper ones, whose words are shifted down by
+// one byte.
+template <int MI, int NJ>
+__global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Gemm4 g)
 {
-    constexpr int BM = 128, BN = 128;
-    typedef int i32x8 __attribute__((ext_vector_type(8)));
-    __shared__ __align__(16) uint8_t sl[64 * BN * 4];   // both tiles of a stage; results on their way out
-    uint8_t *sa = sl, *sb = sl + BM * kBK4 / 2;
+    constexpr int BM = 64 * MI, BN = 64 * NJ, U = BM * 8 / kThreads, R = MI + NJ, P = MI * NJ;
+    static_assert(BM == BN, "one count of copies");
+    constexpr uint32_t kA = BM * 128, kB = BN * 128, kHalf = kA + kB + (BM + BN) * 8;
+    __shared__ __align__(16) uint8_t lds[2 * kHalf];   // two stages: codes of x, of w, scales of x, of w
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    uint32_t id = blockIdx.x;
-    const uint32_t tiles = g.tm * g.tn, part = id / tiles;
-    id -= part * tiles;
-    const uint32_t m0 = id / g.tn * BM, n0 = id % g.tn * BN;
-    const uint32_t wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
+    const uint32_t tiles = g.tm * g.tn, part = blockIdx.x / tiles;
+    uint32_t tile_m, tile_n;
+    tile_of(blockIdx.x - part * tiles, g.tm, g.tn, tile_m, tile_n);
+    const uint32_t m0 = tile_m * BM, n0 = tile_n * BN;
+    const uint32_t wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NJ;
     const uint32_t s_begin = part * g.per, s_end = min(g.stages, s_begin + g.per);
 
-    f32x16 acc[2][2] = {};
-    u32x4 ra[2], rb[2];
-    uint32_t ea[2][2], eb[2][2], na[2][2], nb[2][2];
-    auto scale = [&](const MxMatrix &q, uint32_t row, uint32_t rows, uint32_t block) -> uint32_t {
-        return row < rows && block < g.nb ? q.scales[(uint64_t)row * g.nb + block] : 127u;
+    f32x16 acc[MI][NJ] = {};
+    u32x4 rc[2][U];            // codes on their way: of x, of w
+    constexpr int S = (BM + BN) / kThreads;   // rows of scales that a thread copies
+    u32x2 rsc[S];
+
+    uint32_t frag_at[2][4], code_at[2][U], scale_at[S];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        frag_at[0][i] = frag_k_at(wm, i, lane);
+        frag_at[1][i] = kA + frag_k_at(wn, i, lane);
+    }
+    const uint32_t write_at = at_k(t / 8, t % 8);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        code_at[0][i] = min(i * 32 + t / 8, g.m - 1 - m0) * g.nb * 16 + t % 8 * 16;
+        code_at[1][i] = min(i * 32 + t / 8, g.n - 1 - n0) * g.nb * 16 + t % 8 * 16;
+    }
+    // Row r of the stage's scales: x's rows, then w's.
+    auto row_of = [&](int i) { return (uint32_t)i * kThreads + t; };
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const uint32_t r = row_of(i);
+        scale_at[i] = r < BM ? min(r, g.m - 1 - m0) * g.nb : min(r - BM, g.n - 1 - n0) * g.nb;
+    }
+    const uint8_t *px = nullptr, *pw = nullptr, *sx = nullptr, *sw = nullptr;   // the next whole stage
+    auto go_to = [&](uint32_t s) {
+        const uint64_t x = (uint64_t)m0 * g.nb + s * 8, w = (uint64_t)n0 * g.nb + s * 8;
+        px = g.x.codes + x * 16, sx = g.x.scales + x;
+        pw = g.w.codes + w * 16, sw = g.w.scales + w;
+    };
+    auto load_code = [&](int o, int i) {
+        rc[o][i] = __builtin_amdgcn_raw_buffer_load_b128(buffer_at(o ? pw : px), code_at[o][i], 0, 0);
+    };
+    auto load_scale = [&](int i) {   // 8 bytes of any alignment
+        const uint8_t *base = (BM % kThreads == 0 ? i * kThreads < BM : t < BM) ? sx : sw;
+        __builtin_memcpy(&rsc[i], base + scale_at[i], 8);
+    };
+    constexpr int kItems = 2 * U + S;
+    auto write = [&](uint8_t *half, int y) {
+        if (y < 2 * U)
+            *reinterpret_cast<u32x4 *>(half + (y & 1) * kA + write_at + (y >> 1) * 4096) = rc[y & 1][y >> 1];
+        else
+            *reinterpret_cast<u32x2 *>(half + kA + kB + row_of(y - 2 * U) * 8) = rsc[y - 2 * U];
+    };
+    auto load_item = [&](int y) {
+        if (y < 2 * U)
+            load_code(y & 1, y >> 1);
+        else
+            load_scale(y - 2 * U);
+    };
+    auto load_whole = [&](uint32_t s) {
+        go_to(s);
+#pragma unroll
+        for (int y = 0; y < kItems; ++y) {
+            load_item(y);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Any stage, every address checked: blocks past the end are 0.
+    auto load_short = [&](uint32_t s) {
+        const uint32_t b0 = s * 8, block = b0 + t % 8;
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const uint32_t row = (o ? n0 : m0) + i * 32 + t / 8;
+                rc[o][i] = u32x4{0, 0, 0, 0};
+                if (row < (o ? g.n : g.m) && block < g.nb)
+                    rc[o][i] = reinterpret_cast<const u32x4 *>(o ? g.w.codes : g.x.codes)[(uint64_t)row * g.nb + block];
+            }
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const bool w = row_of(i) >= BM;
+            const uint32_t row = w ? n0 + row_of(i) - BM : m0 + row_of(i);
+            const uint8_t *p = (w ? g.w.scales : g.x.scales) + (uint64_t)row * g.nb + b0;
+            uint64_t v = 0;   // a block of codes 0 is 0 at any scale but a NaN
+            if (row < (w ? g.n : g.m))
+#pragma unroll 1
+                for (uint32_t j = 0; j < min(8u, g.nb - b0); ++j)
+                    v |= (uint64_t)p[j] << (8 * j);
+            rsc[i] = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
+        }
     };
     auto load = [&](uint32_t s) {
-        const uint32_t b0 = s * (kBK4 / 32);
+        if (s < g.whole)
+            load_whole(s);
+        else
+            load_short(s);
+    };
+
+    u32x4 fc[2][R];            // operands of two steps
+    u32x2 next_scale[R];
+    uint32_t scale[R][2];
+    auto read = [&](uint8_t *half, int ks, int to, int r) {
+        fc[to][r] = *reinterpret_cast<const u32x4 *>(half + (r < MI ? frag_at[0][ks] + r * 4096 : frag_at[1][ks] + (r - MI) * 4096));
+    };
+    auto read_scale = [&](uint8_t *half, int r) {
+        const uint32_t row = r < MI ? wm + r * 32 : BM + wn + (r - MI) * 32;
+        next_scale[r] = *reinterpret_cast<const u32x2 *>(half + kA + kB + (row + (lane & 31)) * 8);
+    };
+    const uint32_t shift = (lane >> 5) * 8;
+    auto take_scale = [&](int r) {
+        scale[r][0] = next_scale[r][0] >> shift;
+        scale[r][1] = next_scale[r][1] >> shift;
+    };
+    auto wide = [](u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; };
+    // As in gemm_kernel: other work is dealt out after each product.
+    auto turn = [](int x, int y, int n, int from, int to) { return from + y * (to - from) / n == x; };
+    auto step = [&](auto ks_, auto beside) {
+        constexpr int ks = decltype(ks_)::value;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t u = i * kThreads + t, row = u / 4, block = b0 + u % 4;
-            ra[i] = rb[i] = u32x4{0, 0, 0, 0};
-            if (m0 + row < g.m && block < g.nb)
-                ra[i] = reinterpret_cast<const u32x4 *>(g.x.codes)[(uint64_t)(m0 + row) * g.nb + block];
-            if (n0 + row < g.n && block < g.nb)
-                rb[i] = reinterpret_cast<const u32x4 *>(g.w.codes)[(uint64_t)(n0 + row) * g.nb + block];
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                const uint32_t bl = b0 + ks * 2 + (lane >> 5);
-                na[ks][i] = scale(g.x, m0 + wm + i * 32 + (lane & 31), g.m, bl);
-                nb[ks][i] = scale(g.w, n0 + wn + i * 32 + (lane & 31), g.n, bl);
-            }
+        for (int x = 0; x < P; ++x) {
+            const int i = x / NJ, j = x % NJ;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                wide(fc[ks & 1][i]), wide(fc[ks & 1][MI + j]), acc[i][j], 4, 4, ks % 2 * 2, (int)scale[i][ks / 2],
+                ks % 2 * 2, (int)scale[MI + j][ks / 2]);
+            beside(x);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    if (s_begin < s_end)
-        load(s_begin);
-    for (uint32_t s = s_begin; s < s_end; ++s) {
+    auto stage = [&](uint8_t *here, uint8_t *there, auto beside, auto last) {
+        auto early = [&](auto ks_) {
+            constexpr int ks = decltype(ks_)::value;
+            step(ks_, [&](int x) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t u = i * kThreads + t;
-            *reinterpret_cast<u32x4 *>(sa + at4(u / 4, u % 4)) = ra[i];
-            *reinterpret_cast<u32x4 *>(sb + at4(u / 4, u % 4)) = rb[i];
+                for (int r = 0; r < R; ++r)
+                    if (turn(x, r, R, 0, P / 2))
+                        read(here, ks + 1, (ks + 1) & 1, r);
+                beside(ks * P + x);
+            });
+        };
+        early(Const<0>());
+        early(Const<1>());
+        early(Const<2>());
+        step(Const<3>(), [&](int x) {
+            if (x == P / 4)
+                lds_barrier();
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                ea[ks][i] = na[ks][i];
-                eb[ks][i] = nb[ks][i];
-            }
-        }
-        __syncthreads();
-        if (s + 1 < s_end)
-            load(s + 1);
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            i32x8 fa[2] = {}, fb[2] = {};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32x4 va = *reinterpret_cast<const u32x4 *>(sa + at4(wm + i * 32 + (lane & 31), ks * 2 + (lane >> 5)));
-                const u32x4 vb = *reinterpret_cast<const u32x4 *>(sb + at4(wn + i * 32 + (lane & 31), ks * 2 + (lane >> 5)));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    fa[i][j] = (int)va[j];
-                    fb[i][j] = (int)vb[j];
+            for (int r = 0; r < R; ++r)
+                if (turn(x, r, R, P / 4, P * 3 / 4)) {
+                    read_scale(there, r);
+                    read(there, 0, 0, r);
                 }
+            last(x);
+        });
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            take_scale(r);
+    };
+
+    if (s_begin < s_end) {
+        uint8_t *const h0 = lds, *const h1 = lds + kHalf;
+        auto put = [&](uint8_t *half) {
+#pragma unroll
+            for (int y = 0; y < kItems; ++y)
+                write(half, y);
+        };
+        auto begin = [&](auto ld) {
+            ld(s_begin);
+            put(h0);
+            if (s_begin + 1 < s_end)
+                ld(s_begin + 1);
+            lds_barrier();
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                read_scale(h0, r);
+                read(h0, 0, 0, r);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int r = 0; r < R; ++r)
+                take_scale(r);
+        };
+        uint32_t s = s_begin;
+        auto whole = [&](uint8_t *here, uint8_t *there) {
+            stage(here, there, [&](int x) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0,
-                                                                                (int)ea[ks][i], 0, (int)eb[ks][j]);
+                for (int y = 0; y < kItems; ++y)
+                    if (turn(x, y, kItems, 0, 3 * P)) {
+                        write(there, y);
+                        load_item(y);
+                    }
+            }, [&](int x) {
+                if (x == P - 2) {
+                    px += 128, pw += 128;
+                    sx += 8, sw += 8;
+                }
+            });
+            ++s;
+        };
+        if (s + 3 < min(s_end, g.whole)) {
+            begin(load_whole);
+            go_to(s + 2);
+            do {
+                whole(h0, h1);
+                whole(h1, h0);
+            } while (s + 3 < min(s_end, g.whole));
+        } else {
+            begin(load);
         }
-        __syncthreads();
+        uint32_t h = 0;
+        for (; s < s_end; ++s, h ^= 1) {
+            uint8_t *here = lds + h * kHalf, *there = lds + (h ^ 1) * kHalf;
+            stage(here, there, [&](int x) {
+                if (x == 3 * P - 1) {
+                    if (s + 1 < s_end)
+                        put(there);
+                    if (s + 2 < s_end)
+                        load(s + 2);
+                }
+            }, [](int) {});
+        }
+        lds_barrier();
     }
+
     Out o = {g.c, g.ldc, g.ctype, 0, g.c_vec != 0};
     if (g.splits > 1)
         o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
-    put_tile<2, 2>(acc, reinterpret_cast<float *>(sl), m0, n0, g.m, g.n, o);
+    put_tile<MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
 Gemm4 plan4_of(const Mx4Product &p, int num_cu)
@@ -661,9 +823,11 @@ Gemm4 plan4_of(const Mx4Product &p, int num_cu)
     g.nb = (uint32_t)mx_blocks(p.k);
     g.m = (uint32_t)p.m;
     g.n = (uint32_t)p.n;
-    g.stages = (uint32_t)((p.k + kBK4 - 1) / kBK4);
-    g.tm = (uint32_t)((p.m + 127) / 128);
-    g.tn = (uint32_t)((p.n + 127) / 128);
+    g.whole = 256ull * g.nb * 16 + 128 < 1ull << 32 ? g.nb / 8 : 0;   // a tile's offsets in 32 bits
+    g.stages = (g.nb + 7) / 8;
+    g.tile = (p.m + 255) / 256 * ((p.n + 255) / 256) >= (uint64_t)num_cu / 2 ? 256 : 128;
+    g.tm = (uint32_t)((p.m + g.tile - 1) / g.tile);
+    g.tn = (uint32_t)((p.n + g.tile - 1) / g.tile);
     const uint64_t tiles = (uint64_t)g.tm * g.tn;
     uint64_t splits = tiles >= (uint64_t)num_cu ? 1 : (uint64_t)num_cu * 2 / (tiles ? tiles : 1);
     if (splits > g.stages / 4)
@@ -779,7 +943,11 @@ hipError_t launch_mx4_product(const Mx4Product &p, int num_cu, hipStream_t s)
     g.ctype = p.ctype;
     g.c_vec = vec_rows(p.c, p.ctype);
     g.parts = reinterpret_cast<float *>(p.work);
-    hipLaunchKernelGGL(gemm4_kernel, dim3(g.tm * g.tn * g.splits), dim3(kThreads), 0, s, g);
+    const dim3 grid(g.tm * g.tn * g.splits);
+    if (g.tile == 256)
+        hipLaunchKernelGGL((gemm4_kernel<4, 4>), grid, dim3(kThreads), 0, s, g);
+    else
+        hipLaunchKernelGGL((gemm4_kernel<2, 2>), grid, dim3(kThreads), 0, s, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1)
         return e;

@@ -92,6 +92,16 @@ class _MX:
         device = _torch.device("cuda", _torch.cuda.current_device()) if device is None else device
         return cls.view(_torch.empty(cls.nbytes(rows, cols), dtype=_uint8, device=device), rows, cols)
 
+    @classmethod
+    def _new(cls, rows, cols, device):
+        """What a call returns: codes and scales of their own (a call's shapes need no check, and two allocations cost
+        a third of cutting one buffer into views: 2.3 and 6.4 us)."""
+        q, blocks = object.__new__(cls), -(-cols // 32)
+        q.codes = _torch.empty((rows, blocks * cls.block_bytes), dtype=cls.code_type, device=device)
+        q.scales = _torch.empty((rows, blocks), dtype=_uint8, device=device)
+        q.rows, q.cols = rows, cols
+        return q
+
     def __repr__(self):
         return "%s(%d x %d, %s)" % (type(self).__name__, self.rows, self.cols, self.codes.device)
 
@@ -190,7 +200,7 @@ def _keep(new, stream, device):
 
 def _new_mx(q, what, cls, rows, cols, device, idx, new):
     if q is None:
-        q = cls.empty(rows, cols, device)
+        q = cls._new(rows, cols, device)
         new.append(q)
         return q
     return _mx(q, what, cls, idx, rows, cols)
@@ -218,7 +228,8 @@ def _dequantize(cls, q, dtype, out, stream):
 
 
 def mx4_quantize(x, out=None, stream=None):
-    """x (..., cols) as an MX4 of its rows: nearest code, ties to the even one, saturated at 6 times the scale."""
+    """x (..., cols) as an MX4 of its rows: nearest code, ties to the even one, saturated at 6 times the scale.
+    To send the result as one message give out=MX4.view(buf, rows, cols) of the message's buffer."""
     return _quantize(MX4, x, out, stream)
 
 

@@ -260,7 +260,18 @@ def test_product_of_two_mx4_is_exact_on_whole_numbers(m, n, k):
         assert torch.equal(F.mx4_linear(qx, qw, dtype=dt).cpu(), torch.from_numpy(want).to(dt))
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 64, 500), (40, 200, 321), (200, 130, 1000)])
+@pytest.mark.parametrize("m,n,k", [(3001, 2888, 136), (2900, 3009, 2000), (4096, 2304, 256), (2823, 2817, 5), (260, 32008, 1300),
+                                   (16, 16, 5000), (300, 200, 4992)])
+def test_product_of_two_mx4_with_many_outputs_or_a_long_sum(m, n, k):
+    rng = np.random.default_rng(m + n + k)
+    qx, vx = random_mx(rng, m, k, 4, True)
+    qw, vw = random_mx(rng, n, k, 4, True)
+    want = torch.from_numpy(vx @ vw.T).float()
+    got = F.mx4_linear(qx, qw, dtype=torch.float32).cpu()
+    assert torch.equal(got, want), torch.nonzero(got != want)[:4].tolist()
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 64, 500), (40, 200, 321), (200, 130, 1000), (2600, 2700, 900)])
 def test_product_of_two_mx4_with_any_scales(m, n, k):
     rng = np.random.default_rng(m + n + k)
     qx, vx = random_mx(rng, m, k, 4)
