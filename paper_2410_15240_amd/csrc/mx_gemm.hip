@@ -148,11 +148,11 @@ __device__ __forceinline__ void put8(const Out &o, uint32_t row, uint32_t c, uin
 // l % 32 of rows 8 (r / 4) + 4 (l / 32) + r % 4 of each. They pass through LDS, 64 rows at a
 // time, so that c is written in whole rows of the tile. Rows whose bit 2 is set are turned by
 // 32 columns: the two halves of a wave then write to different banks.
-template <int MI, int NJ>
+template <int WN, int MI, int NJ>
 __device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds, uint32_t m0, uint32_t n0, uint32_t m,
                                          uint32_t n, const Out &o)
 {
-    constexpr uint32_t BN = 64 * NJ;
+    constexpr uint32_t BN = 32 * WN * NJ, TH = 128 * WN;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
@@ -162,13 +162,13 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const uint32_t y = (wave >> 1) * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-                const uint32_t x = (wave & 1) * 32 * NJ + j * 32 + (lane & 31);
+                const uint32_t y = wave / WN * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
+                const uint32_t x = wave % WN * 32 * NJ + j * 32 + (lane & 31);
                 lds[y * BN + (x ^ ((y & 4) << 3))] = acc[i][j][r];
             }
         __syncthreads();
 #pragma unroll 2
-        for (uint32_t u = t; u < 64 * BN / 8; u += kThreads) {
+        for (uint32_t u = t; u < 64 * BN / 8; u += TH) {
             const uint32_t y = u / (BN / 8), x = u % (BN / 8) * 8;
             const uint32_t row = m0 + (y >> 5) * 32 * MI + i * 32 + (y & 31), col = n0 + x;
             const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * BN + (x ^ ((y & 4) << 3)));
@@ -190,20 +190,22 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds
 // A whole stage is read without a check: rows and columns past the matrices' ends read the
 // last ones again, for results that are not stored. (Rows so long that a tile spans 2^32
 // bytes have no such stages; all of theirs are checked.)
-template <uint32_t FMT, bool TA, bool TB, int MI, int NJ>
-__global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gemm g)
+template <uint32_t FMT, bool TA, bool TB, int WN, int MI, int NJ>
+__global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gemm g)
 {
-    constexpr int BM = 64 * MI, BN = 64 * NJ, UA = BM * 8 / kThreads, UB = BN * 8 / kThreads;
+    constexpr int BM = 64 * MI, BN = 32 * WN * NJ, TH = 128 * WN, UA = BM * 8 / TH, UB = BN * 8 / TH;
     constexpr uint32_t CB = FMT == kMx4 ? 4 : 8;   // bytes of 8 codes
-    constexpr uint32_t kA = BM * kBK * 2, kHalf = kA + BN * kBK * 2;
-    __shared__ __align__(16) uint8_t lds[2 * kHalf];   // two stages, each a tile of a and one of the MX matrix
+    // Two stages: both tiles of a, then both of the MX matrix, so that a lane's offsets within
+    // either are a register and a constant of 16 bits.
+    constexpr uint32_t kA = BM * kBK * 2, kB = BN * kBK * 2;
+    __shared__ __align__(16) uint8_t lds[2 * (kA + kB)];
     const uint32_t t = threadIdx.x;
     const uint32_t lane = t & 63, wave = t >> 6;
     const uint32_t tiles = g.tm * g.tn, part = blockIdx.x / tiles;
     uint32_t tile_m, tile_n;
     tile_of(blockIdx.x - part * tiles, g.tm, g.tn, tile_m, tile_n);
     const uint32_t m0 = tile_m * BM, n0 = tile_n * BN;
-    const uint32_t wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NJ;
+    const uint32_t wm = wave / WN * 32 * MI, wn = wave % WN * 32 * NJ;
     const uint32_t s_begin = part * g.per, s_end = min(g.stages, s_begin + g.per);
     const uint32_t full = g.whole, nfull = full * g.planes;   // whole stages of a term, of all
 
@@ -217,16 +219,16 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         fa_at[i] = TA ? frag_t_at<BM>(wm + i % MI * 32, lane) : frag_k_at(wm, i, lane);
-        fb_at[i] = kA + (TB ? frag_t_at<BN>(wn + i % NJ * 32, lane) : frag_k_at(wn, i, lane));
+        fb_at[i] = 2 * kA + (TB ? frag_t_at<BN>(wn + i % NJ * 32, lane) : frag_k_at(wn, i, lane));
     }
     const uint32_t wa_at = TA ? at_t<BM>(t / (BM / 8), t % (BM / 8) * 8) : at_k(t / 8, t % 8);
-    const uint32_t wb_at = kA + (TB ? at_t<BN>(t / (BN / 8), t % (BN / 8) * 8) : at_k(t / 8, t % 8));
+    const uint32_t wb_at = 2 * kA + (TB ? at_t<BN>(t / (BN / 8), t % (BN / 8) * 8) : at_k(t / 8, t % 8));
 
     // A whole stage: one address for the workgroup and 32-bit offsets of the lanes, in bytes.
     uint32_t oa[UA], ob[UB], oe[UB];
 #pragma unroll
     for (int i = 0; i < UA; ++i) {
-        const uint32_t u = i * kThreads + t;
+        const uint32_t u = i * TH + t;
         if (TA)
             oa[i] = u / (BM / 8) * (uint32_t)g.lda * 2 + min(u % (BM / 8) * 8, (g.m - 1 - m0) & ~7u) * 2;
         else
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
     }
 #pragma unroll
     for (int i = 0; i < UB; ++i) {
-        const uint32_t u = i * kThreads + t;
+        const uint32_t u = i * TH + t;
         const uint32_t row = TB ? u / (BN / 8) : min(u / 8, g.n - 1 - n0);
         const uint32_t unit = TB ? min(u % (BN / 8), (g.nb - n0 / 32) * 4 - 1) : u % 8;
         ob[i] = row * g.nb * (4 * CB) + unit * CB;
@@ -279,10 +281,10 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
     static_assert(UA == UB, "groups of one unit each");
     float scale;
     u32x4 dec;
-    auto item = [&](uint8_t *half, int y, bool again) {
+    auto item = [&](uint32_t half, int y, bool again) {
         const int i = y / kGroup, p = y % kGroup;
         if (p == kGroup - 1) {
-            *reinterpret_cast<u32x4 *>(half + wa_at + i * 4096) = ra[i];
+            *reinterpret_cast<u32x4 *>(lds + wa_at + half * kA + i * TH * 16) = ra[i];
             if (again)
                 load_a(i);
             return;
@@ -294,7 +296,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
         if (p == kPieces - 1) {
             if (FMT == kMx4)
                 dec = decode4_bf16(rb[i][0], scale);
-            *reinterpret_cast<u32x4 *>(half + wb_at + i * 4096) = dec;
+            *reinterpret_cast<u32x4 *>(lds + wb_at + half * kB + i * TH * 16) = dec;
             if (again)
                 load_b(i);
         }
@@ -315,14 +317,14 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
         const uint16_t *a = g.a + plane * g.a_plane;
 #pragma unroll
         for (int i = 0; i < UA; ++i) {
-            const uint32_t u = i * kThreads + t;
+            const uint32_t u = i * TH + t;
             const uint32_t row = TA ? k0 + u / (BM / 8) : m0 + u / 8, col = TA ? m0 + u % (BM / 8) * 8 : k0 + u % 8 * 8;
             const bool in = row < (TA ? g.k : g.m) && col < (TA ? g.m : g.k);
             ra[i] = in ? *reinterpret_cast<const u32x4 *>(a + row * g.lda + col) : u32x4{0, 0, 0, 0};
         }
 #pragma unroll
         for (int i = 0; i < UB; ++i) {
-            const uint32_t u = i * kThreads + t;
+            const uint32_t u = i * TH + t;
             const uint32_t row = TB ? k0 + u / (BN / 8) : n0 + u / 8;
             const uint32_t unit = TB ? n0 / 8 + u % (BN / 8) : k0 / 8 + u % 8;   // 8 codes, 4 to a block
             rb[i] = u32x2{0, 0};
@@ -345,12 +347,12 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
         }
     };
     bf16x8 fa[2][MI], fb[2][NJ];
-    auto read = [&](uint8_t *half, int ks, int to, int r) {   // operand r of a step
+    auto read = [&](uint32_t half, int ks, int to, int r) {   // operand r of a step
         if (r < MI)
-            fa[to][r] = TA ? read_t<BM>(half + fa_at[r] + ks * 16 * BM * 2) : read_k(half + fa_at[ks] + r * 4096);
+            fa[to][r] = TA ? read_t<BM>(lds + fa_at[r] + half * kA + ks * 16 * BM * 2) : read_k(lds + fa_at[ks] + half * kA + r * 4096);
         else
-            fb[to][r - MI] = TB ? read_t<BN>(half + fb_at[r - MI] + ks * 16 * BN * 2)
-                                : read_k(half + fb_at[ks] + (r - MI) * 4096);
+            fb[to][r - MI] = TB ? read_t<BN>(lds + fb_at[r - MI] + half * kB + ks * 16 * BN * 2)
+                                : read_k(lds + fb_at[ks] + half * kB + (r - MI) * 4096);
     };
     // A step multiplies 16 values of the sum out of registers. `beside(x)` is what is issued
     // after product x: the matrix unit is busy 32 cycles with each, so the rest of the wave's work
@@ -370,7 +372,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
     // One stage, out of `here`, whose first operands are in registers: each step multiplies what
     // the one before has read. The next stage goes to `there` beside the first three steps
     // (`beside(x)` after product x of their 3 P), and its first operands are read under the last.
-    auto stage = [&](uint8_t *here, uint8_t *there, auto beside, auto last) {
+    auto stage = [&](uint32_t here, uint32_t there, auto beside, auto last) {
 #pragma unroll
         for (int ks = 0; ks < 3; ++ks)
             step(ks & 1, [&](int x) {
@@ -392,24 +394,23 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
     };
 
     if (s_begin < s_end) {
-        uint8_t *const h0 = lds, *const h1 = lds + kHalf;
-        auto put = [&](uint8_t *half) {
+        auto put = [&](uint32_t half) {
 #pragma unroll
             for (int y = 0; y < kItems; ++y)
                 item(half, y, false);
         };
         auto begin = [&](auto ld) {
             ld(s_begin);
-            put(h0);
+            put(0);
             if (s_begin + 1 < s_end)
                 ld(s_begin + 1);
             lds_barrier();
 #pragma unroll
             for (int r = 0; r < R; ++r)
-                read(h0, 0, 0, r);
+                read(0, 0, 0, r);
         };
         uint32_t s = s_begin;
-        auto whole = [&](uint8_t *here, uint8_t *there) {
+        auto whole = [&](uint32_t here, uint32_t there) {
             stage(here, there, [&](int x) {
 #pragma unroll
                 for (int y = 0; y < kItems; ++y)
@@ -429,19 +430,18 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
             begin(load_whole);
             go_to(s + 2);
             do {
-                whole(h0, h1);
-                whole(h1, h0);
+                whole(0, 1);
+                whole(1, 0);
             } while (s + 3 < min(s_end, nfull));
         } else {
             begin(load);
         }
         uint32_t h = 0;
         for (; s < s_end; ++s, h ^= 1) {
-            uint8_t *here = lds + h * kHalf, *there = lds + (h ^ 1) * kHalf;
-            stage(here, there, [&](int x) {
+            stage(h, h ^ 1, [&](int x) {
                 if (x == 3 * P - 1) {
                     if (s + 1 < s_end)
-                        put(there);
+                        put(h ^ 1);
                     if (s + 2 < s_end)
                         load(s + 2);
                 }
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm_kernel(Gem
     Out o = {g.c, g.ldc, g.ctype, g.accumulate, g.c_vec != 0};
     if (g.splits > 1)
         o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
-    put_tile<MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
+    put_tile<WN, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
 // c = the sum of the parts, always in the same order.
@@ -585,8 +585,8 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
 {
     constexpr int BM = 64 * MI, BN = 64 * NJ, U = BM * 8 / kThreads, R = MI + NJ, P = MI * NJ;
     static_assert(BM == BN, "one count of copies");
-    constexpr uint32_t kA = BM * 128, kB = BN * 128, kHalf = kA + kB + (BM + BN) * 8;
-    __shared__ __align__(16) uint8_t lds[2 * kHalf];   // two stages: codes of x, of w, scales of x, of w
+    constexpr uint32_t kA = BM * 128, kB = BN * 128, kS = (BM + BN) * 8;
+    __shared__ __align__(16) uint8_t lds[2 * (kA + kB + kS)];   // two stages: codes of x, of w, scales
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const uint32_t tiles = g.tm * g.tn, part = blockIdx.x / tiles;
     uint32_t tile_m, tile_n;
@@ -604,9 +604,9 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         frag_at[0][i] = frag_k_at(wm, i, lane);
-        frag_at[1][i] = kA + frag_k_at(wn, i, lane);
+        frag_at[1][i] = 2 * kA + frag_k_at(wn, i, lane);
     }
-    const uint32_t write_at = at_k(t / 8, t % 8);
+    const uint32_t write_at = at_k(t / 8, t % 8), write_w = 2 * kA + write_at;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         code_at[0][i] = min(i * 32 + t / 8, g.m - 1 - m0) * g.nb * 16 + t % 8 * 16;
@@ -633,11 +633,11 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
         __builtin_memcpy(&rsc[i], base + scale_at[i], 8);
     };
     constexpr int kItems = 2 * U + S;
-    auto write = [&](uint8_t *half, int y) {
+    auto write = [&](uint32_t half, int y) {
         if (y < 2 * U)
-            *reinterpret_cast<u32x4 *>(half + (y & 1) * kA + write_at + (y >> 1) * 4096) = rc[y & 1][y >> 1];
+            *reinterpret_cast<u32x4 *>(lds + (y & 1 ? write_w + half * kB : write_at + half * kA) + (y >> 1) * 4096) = rc[y & 1][y >> 1];
         else
-            *reinterpret_cast<u32x2 *>(half + kA + kB + row_of(y - 2 * U) * 8) = rsc[y - 2 * U];
+            *reinterpret_cast<u32x2 *>(lds + 2 * (kA + kB) + half * kS + row_of(y - 2 * U) * 8) = rsc[y - 2 * U];
     };
     auto load_item = [&](int y) {
         if (y < 2 * U)
@@ -688,12 +688,12 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
     u32x4 fc[2][R];            // operands of two steps
     u32x2 next_scale[R];
     uint32_t scale[R][2];
-    auto read = [&](uint8_t *half, int ks, int to, int r) {
-        fc[to][r] = *reinterpret_cast<const u32x4 *>(half + (r < MI ? frag_at[0][ks] + r * 4096 : frag_at[1][ks] + (r - MI) * 4096));
+    auto read = [&](uint32_t half, int ks, int to, int r) {
+        fc[to][r] = *reinterpret_cast<const u32x4 *>(lds + (r < MI ? frag_at[0][ks] + half * kA + r * 4096 : frag_at[1][ks] + half * kB + (r - MI) * 4096));
     };
-    auto read_scale = [&](uint8_t *half, int r) {
+    auto read_scale = [&](uint32_t half, int r) {
         const uint32_t row = r < MI ? wm + r * 32 : BM + wn + (r - MI) * 32;
-        next_scale[r] = *reinterpret_cast<const u32x2 *>(half + kA + kB + (row + (lane & 31)) * 8);
+        next_scale[r] = *reinterpret_cast<const u32x2 *>(lds + 2 * (kA + kB) + half * kS + (row + (lane & 31)) * 8);
     };
     const uint32_t shift = (lane >> 5) * 8;
     auto take_scale = [&](int r) {
@@ -715,7 +715,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto stage = [&](uint8_t *here, uint8_t *there, auto beside, auto last) {
+    auto stage = [&](uint32_t here, uint32_t there, auto beside, auto last) {
         auto early = [&](auto ks_) {
             constexpr int ks = decltype(ks_)::value;
             step(ks_, [&](int x) {
@@ -746,29 +746,28 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
     };
 
     if (s_begin < s_end) {
-        uint8_t *const h0 = lds, *const h1 = lds + kHalf;
-        auto put = [&](uint8_t *half) {
+        auto put = [&](uint32_t half) {
 #pragma unroll
             for (int y = 0; y < kItems; ++y)
                 write(half, y);
         };
         auto begin = [&](auto ld) {
             ld(s_begin);
-            put(h0);
+            put(0);
             if (s_begin + 1 < s_end)
                 ld(s_begin + 1);
             lds_barrier();
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                read_scale(h0, r);
-                read(h0, 0, 0, r);
+                read_scale(0, r);
+                read(0, 0, 0, r);
             }
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 take_scale(r);
         };
         uint32_t s = s_begin;
-        auto whole = [&](uint8_t *here, uint8_t *there) {
+        auto whole = [&](uint32_t here, uint32_t there) {
             stage(here, there, [&](int x) {
 #pragma unroll
                 for (int y = 0; y < kItems; ++y)
@@ -788,19 +787,18 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
             begin(load_whole);
             go_to(s + 2);
             do {
-                whole(h0, h1);
-                whole(h1, h0);
+                whole(0, 1);
+                whole(1, 0);
             } while (s + 3 < min(s_end, g.whole));
         } else {
             begin(load);
         }
         uint32_t h = 0;
         for (; s < s_end; ++s, h ^= 1) {
-            uint8_t *here = lds + h * kHalf, *there = lds + (h ^ 1) * kHalf;
-            stage(here, there, [&](int x) {
+            stage(h, h ^ 1, [&](int x) {
                 if (x == 3 * P - 1) {
                     if (s + 1 < s_end)
-                        put(there);
+                        put(h ^ 1);
                     if (s + 2 < s_end)
                         load(s + 2);
                 }
@@ -812,7 +810,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
     Out o = {g.c, g.ldc, g.ctype, 0, g.c_vec != 0};
     if (g.splits > 1)
         o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
-    put_tile<MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
+    put_tile<2, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
 Gemm4 plan4_of(const Mx4Product &p, int num_cu)
@@ -907,9 +905,9 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
 #define MX_GEMM(...)                                                                               \
     do {                                                                                           \
         if (r.tile == 256)                                                                         \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 4, 4>), grid, dim3(kThreads), 0, s, g);   \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 4, 4>), grid, dim3(256), 0, s, g);   \
         else                                                                                       \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 2>), grid, dim3(kThreads), 0, s, g);   \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);   \
     } while (0)
     if (p.op == kLinear)
         MX_GEMM(kMx4, false, false);
