@@ -26,12 +26,6 @@ struct MxRows {
     uint64_t ld;
 };
 
-// Rows that start on 16-byte boundaries.
-inline bool vec_rows(const MxRows &r, uint32_t type)
-{
-    return reinterpret_cast<uintptr_t>(r.p) % 16 == 0 && r.ld * mx_type_size(type) % 16 == 0;
-}
-
 struct MxMatrix {
     uint8_t *codes;
     uint8_t *scales;

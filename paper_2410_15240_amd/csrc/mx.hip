@@ -68,18 +68,18 @@ __device__ __forceinline__ void get(const MxMatrix &q, const Unit &u, float (&v)
         decode8_f32(reinterpret_cast<const u32x2 *>(q.codes)[u.block * 4 + u.lane], scale8_f32(e), v);
 }
 
-template <uint32_t FMT, uint32_t T, bool VEC>
+template <uint32_t FMT, uint32_t T>
 __global__ __launch_bounds__(kThreads) void quantize_kernel(Shape sh, MxRows x, MxMatrix q)
 {
     Unit u;
     if (!unit_of(sh, u))
         return;
     float v[8];
-    load8<T, VEC>(x.p, u.row * x.ld, u.c, sh.cols, v);
+    load8<T>(x.p, u.row * x.ld, u.c, sh.cols, v);
     put<FMT>(q, u, v);
 }
 
-template <uint32_t FMT, uint32_t T, bool VEC>
+template <uint32_t FMT, uint32_t T>
 __global__ __launch_bounds__(kThreads) void dequantize_kernel(Shape sh, MxMatrix q, MxRows out)
 {
     Unit u;
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(Shape sh, MxMatrix
         return;
     float v[8];
     get<FMT>(q, u, v);
-    store8<T, VEC>(out.p, u.row * out.ld, u.c, sh.cols, v);
+    store8<T>(out.p, u.row * out.ld, u.c, sh.cols, v);
 }
 
 // f and f' of the activation. FAST (16-bit types, whose own rounding is 2^-9 or 2^-12): the
@@ -108,7 +108,7 @@ __device__ __forceinline__ void act_of(float x, float &f, float &df)
     }
 }
 
-template <uint32_t ACT, uint32_t T, bool GATE, bool VEC>
+template <uint32_t ACT, uint32_t T, bool GATE>
 __global__ __launch_bounds__(kThreads) void act_kernel(Shape sh, MxRows x, MxRows gate, MxRows y, MxMatrix qx,
                                                        MxMatrix qg)
 {
@@ -116,22 +116,22 @@ __global__ __launch_bounds__(kThreads) void act_kernel(Shape sh, MxRows x, MxRow
     if (!unit_of(sh, u))
         return;
     float v[8], g[8], o[8];
-    load8<T, VEC>(x.p, u.row * x.ld, u.c, sh.cols, v);
+    load8<T>(x.p, u.row * x.ld, u.c, sh.cols, v);
     if (GATE)
-        load8<T, VEC>(gate.p, u.row * gate.ld, u.c, sh.cols, g);
+        load8<T>(gate.p, u.row * gate.ld, u.c, sh.cols, g);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float f, df;
         act_of<ACT, T != kFp32>(v[i], f, df);
         o[i] = GATE ? f * g[i] : f;
     }
-    store8<T, VEC>(y.p, u.row * y.ld, u.c, sh.cols, o);
+    store8<T>(y.p, u.row * y.ld, u.c, sh.cols, o);
     put<kMx8>(qx, u, v);
     if (GATE)
         put<kMx8>(qg, u, g);
 }
 
-template <uint32_t ACT, uint32_t T, bool GATE, bool VEC>
+template <uint32_t ACT, uint32_t T, bool GATE>
 __global__ __launch_bounds__(kThreads) void act_grad_kernel(Shape sh, MxRows dy, MxMatrix qx, MxMatrix qg, MxRows dx,
                                                             MxRows dgate)
 {
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(Shape sh, MxRows dy,
     if (!unit_of(sh, u))
         return;
     float v[8], g[8], d[8];
-    load8<T, VEC>(dy.p, u.row * dy.ld, u.c, sh.cols, d);
+    load8<T>(dy.p, u.row * dy.ld, u.c, sh.cols, d);
     get<kMx8>(qx, u, v);
     if (GATE)
         get<kMx8>(qg, u, g);
@@ -150,9 +150,9 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(Shape sh, MxRows dy,
         v[i] = GATE ? d[i] * g[i] * df : d[i] * df;
         g[i] = d[i] * f;
     }
-    store8<T, VEC>(dx.p, u.row * dx.ld, u.c, sh.cols, v);
+    store8<T>(dx.p, u.row * dx.ld, u.c, sh.cols, v);
     if (GATE)
-        store8<T, VEC>(dgate.p, u.row * dgate.ld, u.c, sh.cols, g);
+        store8<T>(dgate.p, u.row * dgate.ld, u.c, sh.cols, g);
 }
 
 // Calls launch(shape, grid) for row ranges of fewer than 2^32 units each.
@@ -194,24 +194,22 @@ using namespace mx;
 hipError_t launch_mx_quantize(uint32_t fmt, uint32_t type, MxRows x, uint64_t rows, uint64_t cols, MxMatrix q,
                               hipStream_t s)
 {
-    const bool vec = vec_rows(x, type);
     return over_rows(rows, cols, [&](const Shape &sh, dim3 grid) {
-        MX_TYPE(type, MX_BOOL(VEC, vec, MX_BOOL(M4, fmt == kMx4, {
+        MX_TYPE(type, MX_BOOL(M4, fmt == kMx4, {
             constexpr uint32_t F = M4 ? kMx4 : kMx8;
-            hipLaunchKernelGGL((quantize_kernel<F, T, VEC>), grid, dim3(kThreads), 0, s, sh, x, q);
-        })));
+            hipLaunchKernelGGL((quantize_kernel<F, T>), grid, dim3(kThreads), 0, s, sh, x, q);
+        }));
     });
 }
 
 hipError_t launch_mx_dequantize(uint32_t fmt, uint32_t type, MxMatrix q, uint64_t rows, uint64_t cols, MxRows out,
                                 hipStream_t s)
 {
-    const bool vec = vec_rows(out, type);
     return over_rows(rows, cols, [&](const Shape &sh, dim3 grid) {
-        MX_TYPE(type, MX_BOOL(VEC, vec, MX_BOOL(M4, fmt == kMx4, {
+        MX_TYPE(type, MX_BOOL(M4, fmt == kMx4, {
             constexpr uint32_t F = M4 ? kMx4 : kMx8;
-            hipLaunchKernelGGL((dequantize_kernel<F, T, VEC>), grid, dim3(kThreads), 0, s, sh, q, out);
-        })));
+            hipLaunchKernelGGL((dequantize_kernel<F, T>), grid, dim3(kThreads), 0, s, sh, q, out);
+        }));
     });
 }
 
@@ -219,12 +217,11 @@ hipError_t launch_mx_act(uint32_t act, uint32_t type, MxRows x, MxRows gate, uin
                          MxMatrix qx, MxMatrix qg, hipStream_t s)
 {
     const bool has_gate = gate.p != nullptr;
-    const bool vec = vec_rows(x, type) && vec_rows(y, type) && (!has_gate || vec_rows(gate, type));
     return over_rows(rows, cols, [&](const Shape &sh, dim3 grid) {
-        MX_TYPE(type, MX_BOOL(VEC, vec, MX_BOOL(GATE, has_gate, MX_BOOL(SILU, act == kSilu, {
+        MX_TYPE(type, MX_BOOL(GATE, has_gate, MX_BOOL(SILU, act == kSilu, {
             constexpr uint32_t A = SILU ? kSilu : kGelu;
-            hipLaunchKernelGGL((act_kernel<A, T, GATE, VEC>), grid, dim3(kThreads), 0, s, sh, x, gate, y, qx, qg);
-        }))));
+            hipLaunchKernelGGL((act_kernel<A, T, GATE>), grid, dim3(kThreads), 0, s, sh, x, gate, y, qx, qg);
+        })));
     });
 }
 
@@ -232,13 +229,12 @@ hipError_t launch_mx_act_grad(uint32_t act, uint32_t type, MxRows dy, MxMatrix q
                               uint64_t cols, MxRows dx, MxRows dgate, hipStream_t s)
 {
     const bool has_gate = qg.codes != nullptr;
-    const bool vec = vec_rows(dy, type) && vec_rows(dx, type) && (!has_gate || vec_rows(dgate, type));
     return over_rows(rows, cols, [&](const Shape &sh, dim3 grid) {
-        MX_TYPE(type, MX_BOOL(VEC, vec, MX_BOOL(GATE, has_gate, MX_BOOL(SILU, act == kSilu, {
+        MX_TYPE(type, MX_BOOL(GATE, has_gate, MX_BOOL(SILU, act == kSilu, {
             constexpr uint32_t A = SILU ? kSilu : kGelu;
-            hipLaunchKernelGGL((act_grad_kernel<A, T, GATE, VEC>), grid, dim3(kThreads), 0, s, sh, dy, qx, qg, dx,
+            hipLaunchKernelGGL((act_grad_kernel<A, T, GATE>), grid, dim3(kThreads), 0, s, sh, dy, qx, qg, dx,
                                dgate);
-        }))));
+        })));
     });
 }
 

@@ -25,28 +25,19 @@ template <> struct Elem<kBf16> { typedef __bf16 type; };
 template <> struct Elem<kFp16> { typedef _Float16 type; };
 template <> struct Elem<kFp32> { typedef float type; };
 
-// Elements [c, c + 8) of a row as floats, zero past `cols`. VEC: the row starts on a 16-byte
-// boundary, and a whole unit is loaded 16 bytes at a time.
-template <uint32_t T, bool VEC>
+// Elements [c, c + 8) of a row as floats, zero past `cols`. A whole unit is loaded 16 bytes at a
+// time wherever it starts: the hardware takes any alignment.
+template <uint32_t T>
 __device__ __forceinline__ void load8(const void *base, uint64_t row_off, uint32_t c, uint32_t cols, float (&v)[8])
 {
     typedef typename Elem<T>::type E;
     const E *p = reinterpret_cast<const E *>(base) + row_off + c;
-    if (VEC && c + 8 <= cols) {
-        if (T == kFp32) {
-            const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+    if (c + 8 <= cols) {
+        E e[8];
+        __builtin_memcpy(e, p, sizeof e);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = a[i];
-                v[4 + i] = b[i];
-            }
-        } else {
-            typedef E Ex8 __attribute__((ext_vector_type(8)));
-            const Ex8 a = *reinterpret_cast<const Ex8 *>(p);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = (float)a[i];
-        }
+        for (int i = 0; i < 8; ++i)
+            v[i] = (float)e[i];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -55,22 +46,25 @@ __device__ __forceinline__ void load8(const void *base, uint64_t row_off, uint32
 }
 
 // Rounded to the output's type once, to nearest even (what the conversion does).
-template <uint32_t T, bool VEC>
+template <uint32_t T>
 __device__ __forceinline__ void store8(void *base, uint64_t row_off, uint32_t c, uint32_t cols, const float (&v)[8])
 {
     typedef typename Elem<T>::type E;
     E *p = reinterpret_cast<E *>(base) + row_off + c;
-    if (VEC && c + 8 <= cols) {
-        if (T == kFp32) {
-            reinterpret_cast<f32x4 *>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-            reinterpret_cast<f32x4 *>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
-        } else {
-            typedef E Ex8 __attribute__((ext_vector_type(8)));
-            Ex8 o;
+    if (c + 8 <= cols) {
+        // As words: the compiler would take eight elements apart again, and join the last of them
+        // with the branch below.
+        typedef E Ex8 __attribute__((ext_vector_type(8)));
+        typedef uint32_t Words __attribute__((ext_vector_type(sizeof(E) * 2)));
+        Ex8 e;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                o[i] = (E)v[i];
-            *reinterpret_cast<Ex8 *>(p) = o;
+        for (int i = 0; i < 8; ++i)
+            e[i] = (E)v[i];
+        const Words w = __builtin_bit_cast(Words, e);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(E) / 2; ++i) {
+            const u32x4 part = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+            __builtin_memcpy(reinterpret_cast<uint8_t *>(p) + 16 * i, &part, 16);
         }
     } else {
 #pragma unroll

@@ -9,6 +9,7 @@
 
 #include "mx.h"
 #include "mx_dev.h"
+#include "mx_gemm_dev.h"
 
 namespace fastrack {
 namespace mx {
@@ -37,24 +38,8 @@ struct Gemm {
     uint64_t ldc;
     uint32_t ctype;
     uint32_t accumulate;
-    uint32_t c_vec;          // rows of c start on 16-byte boundaries
     float *parts;            // [splits][m][n] where splits > 1
 };
-
-// 16-byte chunk c of row r of a tile whose rows are 128 bytes: bits 1 to 3 of the row turn the
-// chunk's place, so that one chunk of 16 rows in turn lies in all 64 banks, once in each.
-__device__ __forceinline__ uint32_t at_k(uint32_t r, uint32_t c) { return r * 128 + ((c ^ ((r >> 1) & 7)) << 4); }
-
-// A tile stored along the output axis, rows of W columns: 64-byte groups of a row are turned
-// by its low two bits, since a transposing read takes 4 rows of one 64-byte group at once.
-template <int W>
-__device__ __forceinline__ uint32_t at_t(uint32_t r, uint32_t col)
-{
-    return r * (W * 2) + ((col * 2) ^ ((r & 3) << 6));
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // Tile of workgroup `id`. Workgroups go to the 8 XCDs in turn, each with its own L2: an XCD
 // takes a run of neighbouring tiles, in bands of 8 tile rows, so that the tiles it works on at
@@ -67,81 +52,6 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
     const uint32_t band = i / (kBand * tn), first = band * kBand, rows = min(kBand, tm - first), j = i - first * tn;
     m = first + j % rows;
     n = j / rows;
-}
-
-// Offsets of a lane's reads of the matrix instruction's 32 x 16 operands, where lane l holds 8
-// consecutive values of the summed axis, from 8 (l / 32), of row l % 32. In a tile stored along
-// the summed axis they differ by the step (16 values) in the turned bits, and squares of 32
-// rows follow each other.
-__device__ __forceinline__ uint32_t frag_k_at(uint32_t row0, uint32_t ks, uint32_t lane)
-{
-    return at_k(row0 + (lane & 31), ks * 2 + (lane >> 5));
-}
-
-// In a tile stored along the output axis: in each group of 16 lanes, lane j gives the address
-// of 4 columns of row j / 4 and receives column j of the 4 rows. Squares of 32 columns differ
-// in the turned bits, and steps of 16 rows follow each other.
-template <int W>
-__device__ __forceinline__ uint32_t frag_t_at(uint32_t col0, uint32_t lane)
-{
-    const uint32_t j = lane & 15;
-    return at_t<W>((lane >> 5) * 8 + (j >> 2), col0 + ((lane >> 4) & 1) * 16 + (j & 3) * 4);
-}
-
-__device__ __forceinline__ bf16x8 read_k(const uint8_t *p) { return *reinterpret_cast<const bf16x8 *>(p); }
-
-template <int W>
-__device__ __forceinline__ bf16x8 read_t(uint8_t *p)
-{
-    typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * W * 2));
-    return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
-// Memory from one address for the whole wave, read at 32-bit offsets of its lanes. (Through
-// plain pointers the compiler keeps every lane's offset in 64 bits and adds it to the address
-// at each load.)
-typedef __amdgpu_buffer_rsrc_t Buffer;
-__device__ __forceinline__ Buffer buffer_at(const void *p)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0xFFFFFFFFu, 0x00027000);
-}
-
-// All waves' LDS accesses before it are done. (Loads from memory may still be on their way.)
-__device__ __forceinline__ void lds_barrier()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
-// Where a product's results go: parts of a sum as 32-bit floats, or c itself.
-struct Out {
-    void *p;
-    uint64_t ld;
-    uint32_t type, accumulate;
-    bool vec;   // rows start on 16-byte boundaries
-};
-
-// Columns [c, c + 8) of a row.
-__device__ __forceinline__ void put8(const Out &o, uint32_t row, uint32_t c, uint32_t cols, float (&v)[8])
-{
-    const uint64_t at = row * o.ld;
-    if (o.type == kFp32) {
-        if (o.accumulate) {
-            float w[8];
-            load8<kFp32, false>(o.p, at, c, cols, w);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] += w[i];
-        }
-        o.vec ? store8<kFp32, true>(o.p, at, c, cols, v) : store8<kFp32, false>(o.p, at, c, cols, v);
-    } else if (o.type == kBf16) {
-        o.vec ? store8<kBf16, true>(o.p, at, c, cols, v) : store8<kBf16, false>(o.p, at, c, cols, v);
-    } else {
-        o.vec ? store8<kFp16, true>(o.p, at, c, cols, v) : store8<kFp16, false>(o.p, at, c, cols, v);
-    }
 }
 
 // A workgroup's results, 2 x 2 waves of MI x NJ squares of 32: lane l of a wave holds column
@@ -319,8 +229,7 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
         for (int i = 0; i < UA; ++i) {
             const uint32_t u = i * TH + t;
             const uint32_t row = TA ? k0 + u / (BM / 8) : m0 + u / 8, col = TA ? m0 + u % (BM / 8) * 8 : k0 + u % 8 * 8;
-            const bool in = row < (TA ? g.k : g.m) && col < (TA ? g.m : g.k);
-            ra[i] = in ? *reinterpret_cast<const u32x4 *>(a + row * g.lda + col) : u32x4{0, 0, 0, 0};
+            ra[i] = row < (TA ? g.k : g.m) ? chunk_at(a + row * g.lda, col, TA ? g.m : g.k) : u32x4{0, 0, 0, 0};
         }
 #pragma unroll
         for (int i = 0; i < UB; ++i) {
@@ -450,9 +359,9 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
         lds_barrier();
     }
 
-    Out o = {g.c, g.ldc, g.ctype, g.accumulate, g.c_vec != 0};
+    Out o = {g.c, g.ldc, g.ctype, g.accumulate};
     if (g.splits > 1)
-        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
+        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
     put_tile<WN, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
@@ -480,7 +389,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float *parts, uint
 // The bf16 terms of a float matrix, rows padded with zeros to ld (a multiple of 8): each term
 // is what is left cut to its upper 16 bits, so that 3 terms of 8 significant bits (2 for
 // 11 bits) add up to the value exactly. A NaN or an infinity is all in the first term.
-template <uint32_t T, bool VEC>
+template <uint32_t T>
 __global__ __launch_bounds__(kThreads) void terms_kernel(MxRows a, uint64_t rows, uint32_t cols, uint16_t *out, uint64_t ld,
                                                          uint64_t plane)
 {
@@ -491,7 +400,7 @@ __global__ __launch_bounds__(kThreads) void terms_kernel(MxRows a, uint64_t rows
         return;
     const uint32_t c = (uint32_t)(i - r * per) * 8;
     float v[8];
-    load8<T, VEC>(a.p, r * a.ld, c, cols, v);
+    load8<T>(a.p, r * a.ld, c, cols, v);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         uint32_t h[8];
@@ -532,8 +441,10 @@ Plan plan_of(const MxProduct &p, int num_cu)
     r.k = p.op == kLinear ? p.k : ta ? p.m : p.n;
     r.a_rows = p.m;
     r.a_cols = p.op == kLinear ? p.k : p.n;
-    // 16-byte chunks of a row: all of a chunk's values lie in the row, or none.
-    r.in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 16 == 0 && p.a.ld % 8 == 0 && r.a_cols % 8 == 0;
+    // Whole stages are read 16 bytes at a time at multiples of 4. Along its rows a may end
+    // anywhere (the short stage looks at each value); across them, whole chunks.
+    r.in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
+                 (!ta || r.a_cols % 8 == 0);
     r.a_ld = round_up(r.a_cols, 8);
     r.a_bytes = r.in_place ? 0 : round_up(planes_of(p.type) * r.a_rows * r.a_ld * 2, 256);
     r.planes = r.in_place ? 1 : planes_of(p.type);
@@ -568,7 +479,6 @@ struct Gemm4 {
     void *c;
     uint64_t ldc;
     uint32_t ctype;
-    uint32_t c_vec;
     float *parts;
 };
 
@@ -807,9 +717,9 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
         lds_barrier();
     }
 
-    Out o = {g.c, g.ldc, g.ctype, 0, g.c_vec != 0};
+    Out o = {g.c, g.ldc, g.ctype, 0};
     if (g.splits > 1)
-        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, g.n % 4 == 0};
+        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
     put_tile<2, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
@@ -859,17 +769,10 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
         g.lda = r.a_ld;
         g.a_plane = r.a_rows * r.a_ld;
         const uint64_t units = r.a_rows * (r.a_ld / 8);
-        const bool vec = vec_rows(p.a, p.type);
         const dim3 grid((uint32_t)((units + kThreads - 1) / kThreads));
-#define MX_TERMS(T)                                                                                                   \
-    do {                                                                                                              \
-        if (vec)                                                                                                      \
-            hipLaunchKernelGGL((terms_kernel<T, true>), grid, dim3(kThreads), 0, s, p.a, r.a_rows, (uint32_t)r.a_cols, \
-                               out, r.a_ld, g.a_plane);                                                               \
-        else                                                                                                          \
-            hipLaunchKernelGGL((terms_kernel<T, false>), grid, dim3(kThreads), 0, s, p.a, r.a_rows,                   \
-                               (uint32_t)r.a_cols, out, r.a_ld, g.a_plane);                                           \
-    } while (0)
+#define MX_TERMS(T)                                                                                              \
+    hipLaunchKernelGGL((terms_kernel<T>), grid, dim3(kThreads), 0, s, p.a, r.a_rows, (uint32_t)r.a_cols, out, r.a_ld, \
+                       g.a_plane)
         if (p.type == kBf16)
             MX_TERMS(kBf16);
         else if (p.type == kFp16)
@@ -899,7 +802,6 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     g.ldc = p.c.ld;
     g.ctype = p.ctype;
     g.accumulate = p.accumulate;
-    g.c_vec = vec_rows(p.c, p.ctype);
     g.parts = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.work) + r.a_bytes);
     const dim3 grid(r.tm * r.tn * r.splits);
 #define MX_GEMM(...)                                                                               \
@@ -939,7 +841,6 @@ hipError_t launch_mx4_product(const Mx4Product &p, int num_cu, hipStream_t s)
     g.c = p.c.p;
     g.ldc = p.c.ld;
     g.ctype = p.ctype;
-    g.c_vec = vec_rows(p.c, p.ctype);
     g.parts = reinterpret_cast<float *>(p.work);
     const dim3 grid(g.tm * g.tn * g.splits);
     if (g.tile == 256)
