@@ -131,6 +131,12 @@ __device__ __forceinline__ uint32_t decode8_pair(uint32_t word, int upper, float
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
+__device__ __forceinline__ u32x4 decode8_bf16(u32x2 codes, float scale)
+{
+    return u32x4{decode8_pair(codes[0], 0, scale), decode8_pair(codes[0], 1, scale), decode8_pair(codes[1], 0, scale),
+                 decode8_pair(codes[1], 1, scale)};
+}
+
 // The largest magnitude of a block, as the bits of |v| (ordered like the values, infinity and
 // then NaN on top), shared by the four lanes that hold 8 of its values each.
 __device__ __forceinline__ uint32_t block_top(const float (&v)[8])

@@ -10,14 +10,10 @@
 #include "mx.h"
 #include "mx_dev.h"
 #include "mx_gemm_dev.h"
+#include "mx_small.h"
 
 namespace fastrack {
 namespace mx {
-
-template <int V>
-struct Const {
-    static constexpr int value = V;
-};
 
 constexpr int kThreads = 256;   // 4 waves, 2 x 2 over the output tile
 constexpr uint32_t kBK = 64;    // of the summed axis, at a time
@@ -423,7 +419,10 @@ uint32_t planes_of(uint32_t type) { return type == kBf16 ? 1 : type == kFp16 ? 2
 uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
 // How a product runs: whether a is read in place, and into how many parts its sum is cut.
+enum Path : int { kTiles, kSmall, kRows };
+
 struct Plan {
+    Path path;
     bool in_place;
     uint64_t a_rows, a_cols, a_ld, a_bytes;   // a's terms in the workspace, where not in place
     uint32_t planes, stages, splits, per, tm, tn;
@@ -431,6 +430,10 @@ struct Plan {
     uint64_t m, n, k;                         // output m x n, summed axis k
     uint64_t bytes() const { return a_bytes + (splits > 1 ? (uint64_t)splits * m * n * 4 : 0); }
 };
+
+// Tokens up to which the weights are read row by row; slices of a sum that are worth a
+// workgroup of their own.
+constexpr uint64_t kMaxRows = 16, kMinCut = 32;
 
 Plan plan_of(const MxProduct &p, int num_cu)
 {
@@ -441,6 +444,31 @@ Plan plan_of(const MxProduct &p, int num_cu)
     r.k = p.op == kLinear ? p.k : ta ? p.m : p.n;
     r.a_rows = p.m;
     r.a_cols = p.op == kLinear ? p.k : p.n;
+    if (p.op == kLinear && p.m <= kMaxRows && p.k >= 8) {
+        r.path = kRows;
+        r.splits = 1;
+        return r;
+    }
+    const uint64_t large = (r.m + 255) / 256 * ((r.n + 255) / 256);
+    const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
+    if (large < (uint64_t)num_cu / 2 && span < 1ull << 31 && r.a_cols >= 8 && r.k) {
+        r.path = kSmall;
+        r.tile = (r.m + 63) / 64 * ((r.n + 63) / 64) >= (uint64_t)num_cu / 2 ? 64 : 32;
+        r.tm = (uint32_t)((r.m + r.tile - 1) / r.tile);
+        r.tn = (uint32_t)((r.n + r.tile - 1) / r.tile);
+        r.stages = (uint32_t)((r.k + 63) / 64);
+        const uint64_t tiles = (uint64_t)r.tm * r.tn;
+        uint64_t cuts = tiles * 2 <= (uint64_t)num_cu ? (uint64_t)num_cu / tiles : 1;
+        if (cuts > r.stages / kMinCut)
+            cuts = r.stages / kMinCut;
+        if (cuts < 1)
+            cuts = 1;
+        r.per = (uint32_t)((r.stages + cuts - 1) / cuts);
+        if (r.per == 0)
+            r.per = 1;
+        r.splits = r.stages ? (r.stages + r.per - 1) / r.per : 1;
+        return r;
+    }
     // Whole stages are read 16 bytes at a time at multiples of 4. Along its rows a may end
     // anywhere (the short stage looks at each value); across them, whole chunks.
     r.in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
@@ -753,6 +781,14 @@ Gemm4 plan4_of(const Mx4Product &p, int num_cu)
 
 using namespace mx;
 
+static hipError_t join(const float *parts, const Plan &r, const MxProduct &p, hipStream_t s)
+{
+    const uint64_t total = r.m * r.n;
+    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((total + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, parts,
+                       r.splits, (uint32_t)r.m, (uint32_t)r.n, p.c.p, p.c.ld, p.ctype, (uint32_t)p.accumulate);
+    return hipGetLastError();
+}
+
 uint64_t mx_product_work(const MxProduct &p, int num_cu) { return plan_of(p, num_cu).bytes(); }
 
 hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
@@ -760,6 +796,25 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     const Plan r = plan_of(p, num_cu);
     if (r.m == 0 || r.n == 0)
         return hipSuccess;
+    hipError_t e;
+    if (r.path != kTiles) {
+        SmallProduct g = {};
+        g.a = p.a;
+        g.q = p.q;
+        g.nb = (uint32_t)mx_blocks(p.k);
+        g.m = (uint32_t)r.m;
+        g.n = (uint32_t)r.n;
+        g.k = (uint32_t)r.k;
+        g.tm = r.tm;
+        g.tn = r.tn;
+        g.slices = r.stages;
+        g.cuts = r.splits;
+        g.per = r.per;
+        g.out = {p.c.p, p.c.ld, p.ctype, p.accumulate};
+        g.parts = reinterpret_cast<float *>(p.work);
+        e = r.path == kRows ? launch_mx_rows(g, p.type, s) : launch_mx_small(g, p.op, p.type, r.tile, s);
+        return e == hipSuccess && r.splits > 1 ? join(g.parts, r, p, s) : e;
+    }
     Gemm g = {};
     g.a = reinterpret_cast<const uint16_t *>(p.a.p);
     g.lda = p.a.ld;
@@ -780,7 +835,7 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
         else
             MX_TERMS(kFp32);
 #undef MX_TERMS
-        const hipError_t e = hipGetLastError();
+        e = hipGetLastError();
         if (e != hipSuccess)
             return e;
     }
@@ -818,13 +873,8 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     else
         MX_GEMM(kMx8, true, true);
 #undef MX_GEMM
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || r.splits == 1)
-        return e;
-    const uint64_t total = r.m * r.n;
-    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((total + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, g.parts,
-                       r.splits, g.m, g.n, g.c, g.ldc, g.ctype, g.accumulate);
-    return hipGetLastError();
+    e = hipGetLastError();
+    return e == hipSuccess && r.splits > 1 ? join(g.parts, r, p, s) : e;
 }
 
 uint64_t mx4_product_work(const Mx4Product &p, int num_cu)

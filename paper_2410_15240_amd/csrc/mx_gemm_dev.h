@@ -2,9 +2,16 @@
 // results on their way out.
 #pragma once
 #include "mx_dev.h"
+#include "mx_small.h"
 
 namespace fastrack {
 namespace mx {
+
+// A constant as an argument of a lambda.
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
 
 // 16-byte chunk c of row r of a tile whose rows are 128 bytes: bits 1 to 3 of the row turn the
 // chunk's place, so that one chunk of 16 rows in turn lies in all 64 banks, once in each.
@@ -42,14 +49,16 @@ __device__ __forceinline__ uint32_t frag_t_at(uint32_t col0, uint32_t lane)
 
 __device__ __forceinline__ bf16x8 read_k(const uint8_t *p) { return *reinterpret_cast<const bf16x8 *>(p); }
 
-template <int W>
-__device__ __forceinline__ bf16x8 read_t(uint8_t *p)
+__device__ __forceinline__ bf16x8 read_t2(uint8_t *first, uint8_t *second)
 {
     typedef short s16x8 __attribute__((ext_vector_type(8)));
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 4 * W * 2));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)first);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)second);
     return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
+
+template <int W>
+__device__ __forceinline__ bf16x8 read_t(uint8_t *p) { return read_t2(p, p + 4 * W * 2); }
 
 // 16-bit values [c, c + 8) of a row, zero past `cols`.
 __device__ __forceinline__ u32x4 chunk_at(const uint16_t *row, uint32_t c, uint32_t cols)
@@ -75,6 +84,15 @@ __device__ __forceinline__ Buffer buffer_at(const void *p)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0xFFFFFFFFu, 0x00027000);
 }
 
+// This wave's LDS accesses before it come before those after it. (The LDS takes a wave's accesses
+// in order; what is held back is the compiler.)
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // All waves' LDS accesses before it are done. (Loads from memory may still be on their way.)
 __device__ __forceinline__ void lds_barrier()
 {
@@ -83,12 +101,18 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Where a product's results go: parts of a sum as 32-bit floats, or c itself.
-struct Out {
-    void *p;
-    uint64_t ld;
-    uint32_t type, accumulate;
-};
+__device__ __forceinline__ void put1(const Out &o, uint32_t row, uint32_t c, float v)
+{
+    const uint64_t at = row * o.ld + c;
+    if (o.type == kFp32) {
+        float *p = reinterpret_cast<float *>(o.p) + at;
+        *p = o.accumulate ? *p + v : v;
+    } else if (o.type == kBf16) {
+        reinterpret_cast<__bf16 *>(o.p)[at] = (__bf16)v;
+    } else {
+        reinterpret_cast<_Float16 *>(o.p)[at] = (_Float16)v;
+    }
+}
 
 // Columns [c, c + 8) of a row.
 __device__ __forceinline__ void put8(const Out &o, uint32_t row, uint32_t c, uint32_t cols, float (&v)[8])

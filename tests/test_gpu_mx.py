@@ -437,8 +437,8 @@ def test_products_refuse_what_does_not_fit():
         with pytest.raises(ValueError, match=match):
             call()
     with pytest.raises(F.FastrackError, match="workspace"):
-        F.mx4_linear(x[:, :64].half()[:, 1:].contiguous(), F.mx4_quantize(torch.zeros(10, 63, device="cuda")),
-                     work=torch.zeros(16, dtype=torch.uint8, device="cuda"))
+        big = torch.zeros(4096, 63, device="cuda", dtype=torch.float16)
+        F.mx4_linear(big, F.mx4_quantize(big), work=torch.zeros(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(F.FastrackError, match="overlaps"):
         F.mx4_linear(x, F.mx4_quantize(torch.zeros(64, 64, device="cuda")), out=x)
 

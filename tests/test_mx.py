@@ -148,9 +148,10 @@ def linear(L, fn="fastrack_mx_linear", type=0, x=A, ld=64, codes=B, scales=C, m=
 @pytest.mark.parametrize("fn", ["fastrack_mx_linear", "fastrack_mx_linear_grad_input"])
 @pytest.mark.parametrize("kw", [dict(type=3), dict(out_type=3), dict(x=None), dict(x=A + 1), dict(codes=None), dict(codes=B + 8),
                                 dict(scales=None), dict(y=None), dict(y=A), dict(y=B), dict(ldy=63), dict(m=1 << 31),
-                                dict(type=2),                      # its terms need a workspace
-                                dict(type=2, work=A + 0x100000, nwork=64),
-                                dict(type=2, work=A + 0x100008, nwork=1 << 20),
+                                # many outputs: the terms of a float operand need a workspace
+                                dict(type=2, m=4096, n=4096, k=4096, ld=4096, ldy=4096),
+                                dict(type=2, m=4096, n=4096, k=4096, ld=4096, ldy=4096, work=A + 0x100000, nwork=64),
+                                dict(type=2, m=4096, n=4096, k=4096, ld=4096, ldy=4096, work=A + 0x100008, nwork=1 << 30),
                                 dict(m=1 << 30, n=1 << 20, k=1 << 20)])
 def test_products_reject_bad_arguments(L, fn, kw):
     assert linear(L, fn, **kw) == -1 and L.fastrack_last_error()
