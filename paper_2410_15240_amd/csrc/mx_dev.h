@@ -193,5 +193,36 @@ __device__ __forceinline__ u32x2 encode8(const float (&v)[8], uint32_t e)
     return u32x2{b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24};
 }
 
+// The upper halves of eight floats: bf16 values cut, not rounded, so that what is left of each
+// (left: v becomes it) has 8 significant bits less and the terms add up exactly.
+__device__ __forceinline__ u32x4 upper_halves(const float (&v)[8])
+{
+    u32x4 h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        h[i] = __builtin_amdgcn_perm(f32_bits(v[2 * i + 1]), f32_bits(v[2 * i]), 0x07060302u);
+    return h;
+}
+
+__device__ __forceinline__ void leave_lower(float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] -= bits_f32(f32_bits(v[i]) & 0xFFFF0000u);
+}
+
+// The first term of values that have more, and what is left of them. An infinity goes into the
+// first term whole (the subtraction alone would leave a NaN; of a NaN it leaves one rightly).
+__device__ __forceinline__ u32x4 first_term(float (&v)[8])
+{
+    const u32x4 h = upper_halves(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float left = v[i] - bits_f32(f32_bits(v[i]) & 0xFFFF0000u);
+        v[i] = __builtin_fabsf(v[i]) == __builtin_inff() ? 0.0f : left;
+    }
+    return h;
+}
+
 }  // namespace mx
 }  // namespace fastrack

@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "launch.h"
 #include "mx.h"
 #include "mx_dev.h"
 #include "mx_gemm_dev.h"
@@ -384,33 +385,31 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float *parts, uint
 
 // The bf16 terms of a float matrix, rows padded with zeros to ld (a multiple of 8): each term
 // is what is left cut to its upper 16 bits, so that 3 terms of 8 significant bits (2 for
-// 11 bits) add up to the value exactly. A NaN or an infinity is all in the first term.
+// 11 bits) add up to the value exactly.
+struct Terms {
+    MxRows a;
+    uint64_t row0;
+    uint32_t units, per_row, recip, cols;   // 8 values each, of this launch; of a row
+    uint16_t *out;
+    uint64_t ld, plane;
+};
+
 template <uint32_t T>
-__global__ __launch_bounds__(kThreads) void terms_kernel(MxRows a, uint64_t rows, uint32_t cols, uint16_t *out, uint64_t ld,
-                                                         uint64_t plane)
+__global__ __launch_bounds__(kThreads) void terms_kernel(Terms g)
 {
-    constexpr int P = T == kBf16 ? 1 : T == kFp16 ? 2 : 3;
-    const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x, per = ld / 8;
-    const uint64_t r = i / per;
-    if (r >= rows)
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
+    if (i >= g.units)
         return;
-    const uint32_t c = (uint32_t)(i - r * per) * 8;
+    const uint32_t r = div_recip(i, g.per_row, g.recip), c = (i - r * g.per_row) * 8;
     float v[8];
-    load8<T>(a.p, r * a.ld, c, cols, v);
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        uint32_t h[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t u = f32_bits(v[j]);
-            const bool odd = (u & 0x7F800000u) == 0x7F800000u;   // NaN or infinity
-            h[j] = u >> 16;
-            if (odd && (u & 0x007FFFFFu))
-                h[j] |= 0x40u;   // stays a NaN
-            v[j] = odd ? 0.0f : v[j] - bits_f32(u & 0xFFFF0000u);
-        }
-        *reinterpret_cast<u32x4 *>(out + p * plane + r * ld + c) =
-            u32x4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+    load8<T>(g.a.p, (g.row0 + r) * g.a.ld, c, g.cols, v);
+    uint16_t *out = g.out + (g.row0 + r) * g.ld + c;
+    *reinterpret_cast<u32x4 *>(out) = T == kBf16 ? upper_halves(v) : first_term(v);
+    if (T != kBf16)
+        *reinterpret_cast<u32x4 *>(out + g.plane) = upper_halves(v);
+    if (T == kFp32) {
+        leave_lower(v);
+        *reinterpret_cast<u32x4 *>(out + 2 * g.plane) = upper_halves(v);
     }
 }
 
@@ -418,80 +417,103 @@ uint32_t planes_of(uint32_t type) { return type == kBf16 ? 1 : type == kFp16 ? 2
 
 uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
-// How a product runs: whether a is read in place, and into how many parts its sum is cut.
-enum Path : int { kTiles, kSmall, kRows };
+// How a product runs.
+enum Path : int {
+    kDot,     // mx_small.hip, up to 2 tokens
+    kSmall,   // mx_small.hip, tiles of 32 or 64
+    kTiles,   // gemm_kernel, tiles of 128 or 256
+};
 
 struct Plan {
     Path path;
-    bool in_place;
-    uint64_t a_rows, a_cols, a_ld, a_bytes;   // a's terms in the workspace, where not in place
-    uint32_t planes, stages, splits, per, tm, tn;
-    int tile;                                 // side of an output tile
+    uint32_t tile;                            // side of an output tile
+    uint32_t tm, tn;                          // tiles
     uint64_t m, n, k;                         // output m x n, summed axis k
+    uint64_t a_rows, a_cols;
+    // Where a is read as bf16 terms from the workspace: their number, layout and bytes.
+    bool laid_out;
+    uint32_t planes;
+    uint64_t a_ld, a_bytes;
+    uint32_t stages, splits, per;             // of 64 summed values; parts of the sum, stages in each
     uint64_t bytes() const { return a_bytes + (splits > 1 ? (uint64_t)splits * m * n * 4 : 0); }
 };
 
-// Tokens up to which the weights are read row by row; slices of a sum that are worth a
-// workgroup of their own.
-constexpr uint64_t kMaxRows = 16, kMinCut = 32;
-
-Plan plan_of(const MxProduct &p, int num_cu)
+// One way to run a product, its sum in up to `splits` parts.
+Plan plan_as(const MxProduct &p, Path path, uint32_t tile, bool laid_out, uint64_t splits)
 {
     Plan r = {};
     const bool ta = p.op == kWeightGrad;
+    r.path = path;
+    r.tile = tile;
     r.m = ta ? p.n : p.m;
     r.n = p.op == kLinear ? p.n : p.k;
     r.k = p.op == kLinear ? p.k : ta ? p.m : p.n;
     r.a_rows = p.m;
     r.a_cols = p.op == kLinear ? p.k : p.n;
-    if (p.op == kLinear && p.m <= kMaxRows && p.k >= 8) {
-        r.path = kRows;
-        r.splits = 1;
-        return r;
-    }
-    const uint64_t large = (r.m + 255) / 256 * ((r.n + 255) / 256);
-    const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
-    if (large < (uint64_t)num_cu / 2 && span < 1ull << 31 && r.a_cols >= 8 && r.k) {
-        r.path = kSmall;
-        r.tile = (r.m + 63) / 64 * ((r.n + 63) / 64) >= (uint64_t)num_cu / 2 ? 64 : 32;
-        r.tm = (uint32_t)((r.m + r.tile - 1) / r.tile);
-        r.tn = (uint32_t)((r.n + r.tile - 1) / r.tile);
-        r.stages = (uint32_t)((r.k + 63) / 64);
-        const uint64_t tiles = (uint64_t)r.tm * r.tn;
-        uint64_t cuts = tiles * 2 <= (uint64_t)num_cu ? (uint64_t)num_cu / tiles : 1;
-        if (cuts > r.stages / kMinCut)
-            cuts = r.stages / kMinCut;
-        if (cuts < 1)
-            cuts = 1;
-        r.per = (uint32_t)((r.stages + cuts - 1) / cuts);
-        if (r.per == 0)
-            r.per = 1;
-        r.splits = r.stages ? (r.stages + r.per - 1) / r.per : 1;
-        return r;
-    }
-    // Whole stages are read 16 bytes at a time at multiples of 4. Along its rows a may end
-    // anywhere (the short stage looks at each value); across them, whole chunks.
-    r.in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
-                 (!ta || r.a_cols % 8 == 0);
+    r.tm = (uint32_t)((r.m + tile - 1) / tile);
+    r.tn = (uint32_t)((r.n + tile - 1) / tile);
+    r.laid_out = laid_out && r.k;
+    r.planes = r.laid_out ? planes_of(p.type) : 1;
     r.a_ld = round_up(r.a_cols, 8);
-    r.a_bytes = r.in_place ? 0 : round_up(planes_of(p.type) * r.a_rows * r.a_ld * 2, 256);
-    r.planes = r.in_place ? 1 : planes_of(p.type);
+    r.a_bytes = r.laid_out ? round_up(r.planes * r.a_rows * r.a_ld * 2, 256) : 0;
     r.stages = (uint32_t)((r.k + kBK - 1) / kBK) * r.planes;
-    r.tile = (r.m + 255) / 256 * ((r.n + 255) / 256) >= (uint64_t)num_cu / 2 ? 256 : 128;
-    r.tm = (uint32_t)((r.m + r.tile - 1) / r.tile);
-    r.tn = (uint32_t)((r.n + r.tile - 1) / r.tile);
-    // Fewer tiles than CUs: cut the sum, down to 4 stages a part.
-    const uint64_t tiles = (uint64_t)r.tm * r.tn;
-    uint64_t splits = tiles >= (uint64_t)num_cu ? 1 : (uint64_t)num_cu * 2 / (tiles ? tiles : 1);
-    if (splits > r.stages / 4)
-        splits = r.stages / 4;
-    if (splits < 1)
-        splits = 1;
-    r.per = (uint32_t)((r.stages + splits - 1) / splits);
-    if (r.per == 0)
-        r.per = 1;
-    r.splits = (uint32_t)(r.stages ? (r.stages + r.per - 1) / r.per : 1);
+    if (splits > r.stages)
+        splits = r.stages;
+    r.per = splits > 1 ? (uint32_t)((r.stages + splits - 1) / splits) : r.stages ? r.stages : 1;
+    r.splits = r.stages ? (r.stages + r.per - 1) / r.per : 1;
     return r;
+}
+
+Plan plan_of(const MxProduct &p, int num_cu)
+{
+    const uint64_t cu = (uint64_t)num_cu;
+    const bool ta = p.op == kWeightGrad;
+    const uint64_t m = ta ? p.n : p.m, n = p.op == kLinear ? p.n : p.k, a_cols = p.op == kLinear ? p.k : p.n;
+    const uint64_t k = p.op == kLinear ? p.k : ta ? p.m : p.n;
+    if (m == 0 || n == 0)
+        return plan_as(p, kTiles, 128, false, 1);   // no outputs: nothing is launched
+    if (p.op == kLinear && p.m <= 2 && p.k >= 512)
+        return plan_as(p, kDot, 1, false, 1);
+    // gemm_kernel reads whole stages 16 bytes at a time at multiples of 4. Along its rows a may end
+    // anywhere (the short stage looks at each value); across them, whole chunks.
+    const bool in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
+                          (!ta || a_cols % 8 == 0);
+    const uint64_t stages = (k + kBK - 1) / kBK, terms = planes_of(p.type);
+
+    // gemm_kernel: tiles of 256 where they give half the CUs work and the sum is long enough to
+    // pay for a tile's ends (64 tokens' gradient of 8192 x 8192 weights: 67 us with tiles of
+    // 128, 85 with 256; 300 tokens' of 4000 x 4000: 29.5 and 27.9), else of 128 and the sum cut
+    // until there are two for every CU, down to 4 stages a part.
+    const uint64_t large = (m + 255) / 256 * ((n + 255) / 256);
+    const uint32_t tile = large >= cu / 2 && stages >= 4 ? 256 : 128;
+    const uint64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), sum = stages * (in_place ? 1 : terms);
+    uint64_t splits = tiles >= cu ? 1 : cu * 2 / (tiles ? tiles : 1);
+    splits = splits < sum / 4 ? splits : sum / 4;
+    const Plan as_tiles = plan_as(p, kTiles, tile, !in_place, splits);
+    const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
+    if (tile == 256 || span >= 1ull << 31 || a_cols < 8 || k == 0)
+        return as_tiles;
+
+    // Small tiles or gemm_kernel's of 128, by estimates of their times in us. A workgroup of small
+    // tiles takes 3 and an eighth of what its slices were measured to take a wave; those of 32
+    // run two to a CU. Slower where a tile reads a few bytes each of long rows of the MX matrix.
+    // gemm_kernel takes 15, 4 more to lay out a's terms, and what its whole tiles' products take
+    // at 1 PFLOP/s. (Both sides: linear, 1000 x 2000 x 1000 of bf16: 12 and 26; 128 tokens, 8192 x
+    // 8192 of fp32: 125 and 71; gradient of 32 tokens, 8192 x 8192 of bf16: 48 and 25; weight
+    // gradient of 64 tokens, 8192 x 8192: 216 and 67, of 3000 tokens, 1000 x 1000: 20 and 27.)
+    const uint64_t tiles64 = (m + 63) / 64 * ((n + 63) / 64), tiles32 = (m + 31) / 32 * ((n + 31) / 32);
+    const bool by64 = tiles64 >= cu / 2 && p.type != kFp32;
+    const uint64_t count = by64 ? tiles64 : tiles32, at_once = by64 ? cu : 2 * cu;
+    const double across = p.op == kWeightGrad ? 2.6 : mx_blocks(p.k) < 128 ? 1.5 : 2.6;
+    const double slice = (p.op == kLinear ? (by64 ? 1.8 : 0.7) : by64 ? (p.op == kGradInput ? 2.2 : 3.0) : count <= 64 ? 1.0 : across) *
+                         (p.type == kBf16 ? 1.0 : p.type == kFp16 ? 1.4 : p.op == kLinear ? 4.0 : 2.5);
+    uint64_t cuts = count <= cu / 2 ? cu / count : 1;   // few tiles: parts of the sum, 16 slices each and more
+    cuts = cuts < stages / 16 ? cuts : stages / 16;
+    cuts = cuts < 1 ? 1 : cuts;
+    const double small = (double)((count * cuts + at_once - 1) / at_once) * (3.0 + slice * (double)stages / (8.0 * (double)cuts)) +
+                         (cuts > 1 ? 4.0 : 0.0);
+    const double large_us = 15.0 + (in_place ? 0.0 : 4.0) + 2e-9 * 128.0 * 128.0 * (double)tiles * (double)(sum * kBK);
+    return small <= large_us ? plan_as(p, kSmall, by64 ? 64 : 32, false, cuts) : as_tiles;
 }
 
 // ---- MX4 x MX4 -------------------------------------------------------------------------
@@ -789,56 +811,41 @@ static hipError_t join(const float *parts, const Plan &r, const MxProduct &p, hi
     return hipGetLastError();
 }
 
-uint64_t mx_product_work(const MxProduct &p, int num_cu) { return plan_of(p, num_cu).bytes(); }
-
-hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
+// a's terms into the workspace; g and its planes as laid out there.
+static hipError_t lay_out(const MxProduct &p, const Plan &r, hipStream_t s)
 {
-    const Plan r = plan_of(p, num_cu);
-    if (r.m == 0 || r.n == 0)
-        return hipSuccess;
-    hipError_t e;
-    if (r.path != kTiles) {
-        SmallProduct g = {};
-        g.a = p.a;
-        g.q = p.q;
-        g.nb = (uint32_t)mx_blocks(p.k);
-        g.m = (uint32_t)r.m;
-        g.n = (uint32_t)r.n;
-        g.k = (uint32_t)r.k;
-        g.tm = r.tm;
-        g.tn = r.tn;
-        g.slices = r.stages;
-        g.cuts = r.splits;
-        g.per = r.per;
-        g.out = {p.c.p, p.c.ld, p.ctype, p.accumulate};
-        g.parts = reinterpret_cast<float *>(p.work);
-        e = r.path == kRows ? launch_mx_rows(g, p.type, s) : launch_mx_small(g, p.op, p.type, r.tile, s);
-        return e == hipSuccess && r.splits > 1 ? join(g.parts, r, p, s) : e;
-    }
-    Gemm g = {};
-    g.a = reinterpret_cast<const uint16_t *>(p.a.p);
-    g.lda = p.a.ld;
-    if (!r.in_place && r.k) {
-        uint16_t *out = reinterpret_cast<uint16_t *>(p.work);
-        g.a = out;
-        g.lda = r.a_ld;
-        g.a_plane = r.a_rows * r.a_ld;
-        const uint64_t units = r.a_rows * (r.a_ld / 8);
-        const dim3 grid((uint32_t)((units + kThreads - 1) / kThreads));
-#define MX_TERMS(T)                                                                                              \
-    hipLaunchKernelGGL((terms_kernel<T>), grid, dim3(kThreads), 0, s, p.a, r.a_rows, (uint32_t)r.a_cols, out, r.a_ld, \
-                       g.a_plane)
+    Terms g = {};
+    g.a = p.a;
+    g.per_row = (uint32_t)(r.a_ld / 8);
+    g.recip = div_recip_of(g.per_row);
+    g.cols = (uint32_t)r.a_cols;
+    g.out = reinterpret_cast<uint16_t *>(p.work);
+    g.ld = r.a_ld;
+    g.plane = r.a_rows * r.a_ld;
+    const uint64_t most = 0xFFFFFF00u / g.per_row;   // rows of a launch: thread indices in 32 bits
+    for (g.row0 = 0; g.row0 < r.a_rows; g.row0 += most) {
+        const uint64_t rows = r.a_rows - g.row0 < most ? r.a_rows - g.row0 : most;
+        g.units = (uint32_t)(rows * g.per_row);
+        const dim3 grid((g.units + kThreads - 1) / kThreads);
         if (p.type == kBf16)
-            MX_TERMS(kBf16);
+            hipLaunchKernelGGL((terms_kernel<kBf16>), grid, dim3(kThreads), 0, s, g);
         else if (p.type == kFp16)
-            MX_TERMS(kFp16);
+            hipLaunchKernelGGL((terms_kernel<kFp16>), grid, dim3(kThreads), 0, s, g);
         else
-            MX_TERMS(kFp32);
-#undef MX_TERMS
-        e = hipGetLastError();
+            hipLaunchKernelGGL((terms_kernel<kFp32>), grid, dim3(kThreads), 0, s, g);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
     }
+    return hipSuccess;
+}
+
+static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &a, float *parts, hipStream_t s)
+{
+    Gemm g = {};
+    g.a = reinterpret_cast<const uint16_t *>(a.p);
+    g.lda = a.ld;
+    g.a_plane = r.a_rows * r.a_ld;
     g.q = p.q;
     g.nb = (uint32_t)mx_blocks(p.k);
     g.m = (uint32_t)r.m;
@@ -857,14 +864,14 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     g.ldc = p.c.ld;
     g.ctype = p.ctype;
     g.accumulate = p.accumulate;
-    g.parts = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.work) + r.a_bytes);
+    g.parts = parts;
     const dim3 grid(r.tm * r.tn * r.splits);
-#define MX_GEMM(...)                                                                               \
-    do {                                                                                           \
-        if (r.tile == 256)                                                                         \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 4, 4>), grid, dim3(256), 0, s, g);   \
-        else                                                                                       \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);   \
+#define MX_GEMM(...)                                                                                 \
+    do {                                                                                             \
+        if (r.tile == 256)                                                                           \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 4, 4>), grid, dim3(kThreads), 0, s, g);  \
+        else                                                                                         \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);  \
     } while (0)
     if (p.op == kLinear)
         MX_GEMM(kMx4, false, false);
@@ -873,8 +880,47 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     else
         MX_GEMM(kMx8, true, true);
 #undef MX_GEMM
-    e = hipGetLastError();
-    return e == hipSuccess && r.splits > 1 ? join(g.parts, r, p, s) : e;
+    return hipGetLastError();
+}
+
+uint64_t mx_product_work(const MxProduct &p, int num_cu) { return plan_of(p, num_cu).bytes(); }
+
+hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
+{
+    const Plan r = plan_of(p, num_cu);
+    if (r.m == 0 || r.n == 0)
+        return hipSuccess;
+    MxRows a = p.a;
+    uint32_t type = p.type;
+    float *parts = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.work) + r.a_bytes);
+    if (r.laid_out) {
+        const hipError_t e = lay_out(p, r, s);
+        if (e != hipSuccess)
+            return e;
+        a = {p.work, r.a_ld};
+        type = kBf16;
+    }
+    hipError_t e;
+    if (r.path == kTiles) {
+        e = launch_tiles(p, r, a, parts, s);
+    } else {
+        SmallProduct g = {};
+        g.a = a;
+        g.q = p.q;
+        g.nb = (uint32_t)mx_blocks(p.k);
+        g.m = (uint32_t)r.m;
+        g.n = (uint32_t)r.n;
+        g.k = (uint32_t)r.k;
+        g.tm = r.tm;
+        g.tn = r.tn;
+        g.slices = r.stages;
+        g.cuts = r.splits;
+        g.per = r.per;
+        g.out = {p.c.p, p.c.ld, p.ctype, p.accumulate};
+        g.parts = parts;
+        e = r.path == kDot ? launch_mx_dot(g, type, s) : launch_mx_small(g, p.op, type, r.tile, s);
+    }
+    return e == hipSuccess && r.splits > 1 ? join(parts, r, p, s) : e;
 }
 
 uint64_t mx4_product_work(const Mx4Product &p, int num_cu)

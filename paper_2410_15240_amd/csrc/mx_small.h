@@ -23,9 +23,10 @@ struct SmallProduct {
     float *parts;            // [cuts][m][n] where cuts > 1
 };
 
-// linear alone, m up to 16 and k from 8.
-hipError_t launch_mx_rows(const SmallProduct &g, uint32_t type, hipStream_t s);
-// Tiles of side 32 or 64; a's rows of 8 values and more.
+// linear alone, m up to 2 and k from 8.
+hipError_t launch_mx_dot(const SmallProduct &g, uint32_t type, hipStream_t s);
+// Tiles of side 32, or of 64 where a is not fp32 (its terms of 64 rows do not fit the registers);
+// a's rows of 8 values and more.
 hipError_t launch_mx_small(const SmallProduct &g, uint32_t op, uint32_t type, uint32_t side, hipStream_t s);
 
 }  // namespace fastrack

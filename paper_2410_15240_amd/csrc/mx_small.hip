@@ -19,37 +19,6 @@ namespace mx {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
-// The upper halves of eight floats: bf16 values cut, not rounded, so that what is left of each
-// (left: v becomes it) has 8 significant bits less and the terms add up exactly.
-__device__ __forceinline__ u32x4 upper_halves(const float (&v)[8])
-{
-    u32x4 h;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        h[i] = __builtin_amdgcn_perm(f32_bits(v[2 * i + 1]), f32_bits(v[2 * i]), 0x07060302u);
-    return h;
-}
-
-__device__ __forceinline__ void leave_lower(float (&v)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        v[i] -= bits_f32(f32_bits(v[i]) & 0xFFFF0000u);
-}
-
-// The first term of values that have more, and what is left of them. An infinity goes into the
-// first term whole (the subtraction alone would leave a NaN; of a NaN it leaves one rightly).
-__device__ __forceinline__ u32x4 first_term(float (&v)[8])
-{
-    const u32x4 h = upper_halves(v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float left = v[i] - bits_f32(f32_bits(v[i]) & 0xFFFF0000u);
-        v[i] = __builtin_fabsf(v[i]) == __builtin_inff() ? 0.0f : left;
-    }
-    return h;
-}
-
 // Eight elements of a float operand as they lie in memory, and taken apart into bf16 terms.
 template <uint32_t T> struct Unit8 {
     static constexpr int kTerms = T == kBf16 ? 1 : T == kFp16 ? 2 : 3;
@@ -135,98 +104,118 @@ template <uint32_t T> struct Unit8 {
     }
 };
 
-// ---- one token, or up to 16 of them ---------------------------------------------------------
+// ---- a few tokens ----------------------------------------------------------------------------
 //
-// y[m][n] = sum over k of x[m][k] w[n][k]. The weights are read once, 16 rows of them to a
-// workgroup: lane l takes block l / 16 of every four of row l % 16, 16 bytes at once, and what
-// it decodes is an operand of the 16 x 16 matrix instruction as it is (its lane holds 8
-// consecutive values). x's values of the same places are the other operand; columns past m
-// repeat the last token's. What bounds it is the reading of w: K / 2 + K / 32 bytes a row.
-template <uint32_t T>
-__global__ __launch_bounds__(kThreads, 4) void row_kernel(SmallProduct g)
+// y[m][n] = sum over k of x[m][k] w[n][k]. The weights as they lie in memory: a wave takes 64
+// blocks of a row at once, one to a lane (1 KB of codes that follow one another), of R rows
+// before it uses the first, and multiplies them with the x of those places, which it keeps in
+// registers for all R. bf16 by the pairwise product, 16 and 32-bit floats in 32 bits. The
+// lanes' sums meet in LDS. What bounds it is the reading of w, K / 2 + K / 32 bytes a row: 7.1
+// us for 8192 x 8192, 5 TB/s. (Lanes that read 64 bytes each of 16 rows, as the matrix
+// instruction takes them, took twice that: rows a power of two apart are one memory channel's
+// work at a time.)
+constexpr int kDotWaves = 4;
+
+// Rows at once: as many as leave the registers to 16 waves a CU.
+template <uint32_t T, int M> constexpr int dot_rows() { return 8 / M; }
+
+template <uint32_t T, int M>
+__global__ __launch_bounds__(64 * kDotWaves, 4) void dot_kernel(SmallProduct g)
 {
-    constexpr int NT = Unit8<T>::kTerms, U = T == kFp32 ? 2 : 4;   // chunks of 4 blocks read ahead
-    __shared__ float part[kWaves][256];
-    const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, r = lane & 15, q = lane >> 4;
-    const uint32_t n0 = blockIdx.x * 16;
-    const uint64_t row = (uint64_t)min(n0 + r, g.n - 1) * g.nb;
-    const u32x4 *codes = reinterpret_cast<const u32x4 *>(g.q.codes) + row;
-    const uint8_t *scales = g.q.scales + row;
+    constexpr int R = dot_rows<T, M>(), XW = T == kBf16 ? 16 : 32;
     constexpr uint32_t ES = Unit8<T>::kSize;
-    const uint8_t *x = reinterpret_cast<const uint8_t *>(g.a.p) + min(r, g.m - 1) * g.a.ld * ES;
-    const uint32_t chunks = (g.nb + 3) / 4, whole = g.k / 128;   // all of a chunk's values in the row
-
-    f32x4 acc = {0, 0, 0, 0};
-    u32x4 w[U];
-    uint32_t e[U];
-    Unit8<T> v[U][4];
-    auto load = [&](int i, uint32_t c) {
-        const uint32_t b = c * 4 + q;
-        w[i] = codes[b];
-        e[i] = scales[b];
+    __shared__ __align__(16) float part[kDotWaves][M][R][64];
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t n0 = blockIdx.x * R;
+    float acc[M][R] = {};
+    for (uint32_t b0 = wave * 64; b0 < g.nb; b0 += kDotWaves * 64) {
+        const uint32_t b = min(b0 + lane, g.nb - 1);
+        u32x4 w[R];
+        uint32_t e[R];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[i][j].load(x + (uint64_t)(b * 32 + j * 8) * ES);
-    };
-    // The last chunk: a block past the end is 0, a unit that the row ends in is read from its end.
-    auto load_last = [&](uint32_t c) {
-        const uint32_t b = c * 4 + q;
-        w[0] = codes[min(b, g.nb - 1)];
-        e[0] = scales[min(b, g.nb - 1)];
-        if (b >= g.nb) {
-            w[0] = u32x4{0, 0, 0, 0};
-            e[0] = 127;
+        for (int i = 0; i < R; ++i) {
+            const uint64_t at = (uint64_t)min(n0 + i, g.n - 1) * g.nb;
+            w[i] = reinterpret_cast<const u32x4 *>(g.q.codes + at * 16)[b];
+            e[i] = g.q.scales[at + b];
         }
+        uint32_t x[M][XW];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t k = b * 32 + j * 8, from = min(k, g.k - 8);
-            v[0][j].load(x + (uint64_t)from * ES);
-            v[0][j].move_down(k - from);
+        for (int m = 0; m < M; ++m) {
+            const uint8_t *row = reinterpret_cast<const uint8_t *>(g.a.p) + min((uint32_t)m, g.m - 1) * g.a.ld * ES;
+            const bool end = (b0 + 64) * 32 > g.k;   // of the sum, in these blocks
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                Unit8<T> u;
+                const uint32_t k = (b0 + lane) * 32 + j * 8, from = end ? min(k, g.k - 8) : k;
+                u.load(row + (uint64_t)from * ES);
+                if (end)
+                    u.move_down(k - from);
+                if (T == kBf16) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        x[m][j * 4 + i] = u.w[i];
+                } else {
+                    float f[8];
+                    u.floats(f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        x[m][(j * 8 + i) % XW] = f32_bits(f[i]);
+                }
+            }
         }
-    };
-    auto multiply = [&](int i) {
-        const float s = scale4_f32(e[i]);
+        const bool past = b0 + lane >= g.nb;   // no block: 0, whatever the last one holds
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bf16x8 d = __builtin_bit_cast(bf16x8, decode4_bf16(w[i][j], s));
-            u32x4 terms[NT];
-            v[i][j].terms(terms);
+        for (int i = 0; i < R; ++i) {
+            const float s = scale4_f32(past ? 127u : e[i]);
 #pragma unroll
-            for (int p = 0; p < NT; ++p)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d, __builtin_bit_cast(bf16x8, terms[p]), acc, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = past ? 0u : w[i][j];
+                if (T == kBf16) {
+                    const u32x4 d = decode4_bf16(c, s);
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            // (Left to see the conversion here, the compiler takes the
+                            // first of the four pairs for all of them.)
+                            uint32_t pair = d[y];
+                            asm("" : "+v"(pair));
+                            acc[m][i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair),
+                                                                        __builtin_bit_cast(bf16x2, x[m][j * 4 + y]),
+                                                                        acc[m][i], false);
+                        }
+                } else {
+                    float d[8];
+                    decode4_f32(c, s, d);
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int y = 0; y < 8; ++y)
+                            acc[m][i] = __builtin_fmaf(d[y], bits_f32(x[m][(j * 8 + y) % XW]), acc[m][i]);
+                }
+            }
         }
-    };
-    uint32_t c = wave;
-    for (; c + (U - 1) * kWaves < whole; c += U * kWaves) {
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-            load(i, c + i * kWaves);
-        __builtin_amdgcn_sched_barrier(0);   // all of them on their way before the first is used
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-            multiply(i);
     }
-    for (; c < chunks; c += kWaves) {
-        if (c < whole)
-            load(0, c);
-        else
-            load_last(c);
-        multiply(0);
-    }
-
-    // Lane l holds token l % 16 of rows 4 (l / 16) + i.
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        part[wave][r * 16 + q * 4 + i] = acc[i];
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            part[wave][m][i][lane] = acc[m][i];
     __syncthreads();
-    if (t < 256) {
-        const uint32_t m = t / 16, n = n0 + t % 16;
-        float s = part[0][t];
+    // 16 lanes to a result.
+    for (uint32_t i = t / 16; i < M * R; i += 4 * kDotWaves) {
+        const uint32_t m = i / R, r = i % R;
+        float s = 0.0f;
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i)
-            s += part[i][t];
-        if (m < g.m && n < g.n)
-            put1(g.out, m, n, s);
+        for (int v = 0; v < kDotWaves; ++v) {
+            const f32x4 p = *reinterpret_cast<const f32x4 *>(&part[v][m][r][t % 16 * 4]);
+            s += (p[0] + p[1]) + (p[2] + p[3]);
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2)
+            s += __shfl_xor(s, d, 64);
+        if (t % 16 == 0 && m < g.m && n0 + r < g.n)
+            put1(g.out, m, n0 + r, s);
     }
 }
 
@@ -443,30 +432,44 @@ using namespace mx;
         else { constexpr uint32_t T = kFp32; __VA_ARGS__; }                                        \
     } while (0)
 
-hipError_t launch_mx_rows(const SmallProduct &g, uint32_t type, hipStream_t s)
+template <uint32_t T, int M>
+static void dot(const SmallProduct &g, hipStream_t s)
 {
-    const dim3 grid((g.n + 15) / 16);
-    MX_TYPE(type, hipLaunchKernelGGL((row_kernel<T>), grid, dim3(kThreads), 0, s, g));
+    constexpr uint32_t R = dot_rows<T, M>();
+    hipLaunchKernelGGL((dot_kernel<T, M>), dim3((g.n + R - 1) / R), dim3(64 * kDotWaves), 0, s, g);
+}
+
+hipError_t launch_mx_dot(const SmallProduct &g, uint32_t type, hipStream_t s)
+{
+    MX_TYPE(type, {
+        if (g.m == 1)
+            dot<T, 1>(g, s);
+        else
+            dot<T, 2>(g, s);
+    });
     return hipGetLastError();
+}
+
+template <uint32_t FMT, bool TA, bool TB>
+static void small(const SmallProduct &g, uint32_t type, uint32_t side, hipStream_t s)
+{
+    const dim3 grid(g.tm * g.tn * g.cuts);
+    if (side == 32)
+        MX_TYPE(type, hipLaunchKernelGGL((small_kernel<FMT, TA, TB, T, 1>), grid, dim3(kThreads), 0, s, g));
+    else if (type == kBf16)
+        hipLaunchKernelGGL((small_kernel<FMT, TA, TB, kBf16, 2>), grid, dim3(kThreads), 0, s, g);
+    else
+        hipLaunchKernelGGL((small_kernel<FMT, TA, TB, kFp16, 2>), grid, dim3(kThreads), 0, s, g);
 }
 
 hipError_t launch_mx_small(const SmallProduct &g, uint32_t op, uint32_t type, uint32_t side, hipStream_t s)
 {
-    const dim3 grid(g.tm * g.tn * g.cuts);
-#define MX_SMALL(...)                                                                                       \
-    MX_TYPE(type, {                                                                                         \
-        if (side == 64)                                                                                     \
-            hipLaunchKernelGGL((small_kernel<__VA_ARGS__, T, 2>), grid, dim3(kThreads), 0, s, g);           \
-        else                                                                                                \
-            hipLaunchKernelGGL((small_kernel<__VA_ARGS__, T, 1>), grid, dim3(kThreads), 0, s, g);           \
-    })
     if (op == kLinear)
-        MX_SMALL(kMx4, false, false);
+        small<kMx4, false, false>(g, type, side, s);
     else if (op == kGradInput)
-        MX_SMALL(kMx4, false, true);
+        small<kMx4, false, true>(g, type, side, s);
     else
-        MX_SMALL(kMx8, true, true);
-#undef MX_SMALL
+        small<kMx8, true, true>(g, type, side, s);
     return hipGetLastError();
 }
 

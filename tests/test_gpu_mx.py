@@ -214,6 +214,28 @@ def test_products_are_exact_on_whole_numbers(op, name, m, n, k):
     assert torch.equal(got.cpu(), torch.from_numpy(want).to(torch.bfloat16))
 
 
+@pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("m", [1, 2, 3])
+@pytest.mark.parametrize("n,k", [(1, 512), (7, 600), (100, 2048), (33, 2049), (5, 4103), (130, 4096), (9, 4991)])
+def test_a_few_tokens_are_exact_on_whole_numbers(name, m, n, k):
+    """Each input's place on its own, and all of them at once; infinities in one token only."""
+    rng = np.random.default_rng(m + n + k)
+    q, v = random_mx(rng, n, k, 4, True)
+    for pad in (0, 8, 3):
+        x = whole(rng, m, k)
+        assert np.array_equal(f64(F.mx4_linear(gpu(x, TYPES[name], pad), q, dtype=torch.float32)), x @ v.T)
+    for at in rng.integers(0, k, 40):
+        x = np.zeros((m, k))
+        x[m - 1, at] = 1.0
+        assert np.array_equal(f64(F.mx4_linear(gpu(x, TYPES[name]), q, dtype=torch.float32)), x @ v.T), at
+    x = whole(rng, m, k)
+    x[0, k - 1] = np.inf
+    with np.errstate(invalid="ignore"):
+        want = x @ v.T
+    got = f64(F.mx4_linear(gpu(x, TYPES[name]), q, dtype=torch.float32))
+    assert np.array_equal(np.nan_to_num(got, nan=1e9, posinf=2e9, neginf=3e9), np.nan_to_num(want, nan=1e9, posinf=2e9, neginf=3e9))
+
+
 @pytest.mark.parametrize("op", ["linear", "grad", "weight"])
 @pytest.mark.parametrize("name", list(TYPES))
 @pytest.mark.parametrize("rows,cols,sums", [(3001, 2888, 136), (2900, 3009, 700), (4096, 2304, 64), (2823, 2817, 5),
@@ -223,6 +245,20 @@ def test_products_with_many_outputs_are_exact_on_whole_numbers(op, name, rows, c
     m, n, k = dict(linear=(rows, cols, sums), grad=(rows, sums, cols), weight=(sums, rows, cols))[op]
     rng = np.random.default_rng(rows + cols + sums)
     x, q, _, f = layer(rng, op, m, n, k, "whole")
+    want = torch.from_numpy(f(x)).float()
+    for pad in (0, 3):
+        got = product(op, gpu(x, TYPES[name], pad), q, dtype=torch.float32).cpu()
+        assert torch.equal(got, want), (pad, torch.nonzero(got != want)[:4].tolist())
+
+
+@pytest.mark.parametrize("op", ["linear", "grad", "weight"])
+@pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("m,n,k", [(6001, 500, 1111), (1000, 1001, 2000), (40, 8200, 4000), (77, 4100, 8192), (300, 3000, 3001)])
+def test_products_of_middling_sizes_are_exact_on_whole_numbers(op, name, m, n, k):
+    """Between small tiles and large ones: tiles of 64 and 128, sums cut into parts of uneven length."""
+    rng = np.random.default_rng(m + n + k)
+    x, q, _, f = layer(rng, op, m, n, k, "whole")
+    x = np.clip(x, -4, 4)   # |x q| <= 64: 8200 of them stay below 2^24
     want = torch.from_numpy(f(x)).float()
     for pad in (0, 3):
         got = product(op, gpu(x, TYPES[name], pad), q, dtype=torch.float32).cpu()

@@ -191,6 +191,9 @@ def test_empty_calls_are_no_ops(L):
 
 def test_workspace_of_a_product(L):
     work = L.fastrack_mx_work_bytes
+    for op in range(4):   # a size of 0 anywhere plans nothing
+        for m, n, k in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (0, 0, 0)):
+            assert work(op, 2, A, 8, m, n, k) == 0
     assert work(0, 0, A, 64, 4096, 8192, 8192) == 0           # read in place, a whole sum to a tile
     assert work(0, 2, A, 8192, 4096, 8192, 8192) >= 3 * 2 * 4096 * 8192   # three terms of every value
     assert work(0, 0, A, 8191, 4096, 8192, 8192) >= 2 * 4096 * 8192       # rows that are not 16-byte aligned
