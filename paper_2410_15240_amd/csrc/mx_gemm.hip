@@ -16,6 +16,9 @@
 namespace fastrack {
 namespace mx {
 
+// The MX matrix decoded to bf16 beforehand: its blocks are 64 bytes, its scales not read.
+constexpr uint32_t kDecoded = 16;
+
 constexpr int kThreads = 256;   // 4 waves, 2 x 2 over the output tile
 constexpr uint32_t kBK = 64;    // of the summed axis, at a time
 
@@ -101,7 +104,8 @@ template <uint32_t FMT, bool TA, bool TB, int WN, int MI, int NJ>
 __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gemm g)
 {
     constexpr int BM = 64 * MI, BN = 32 * WN * NJ, TH = 128 * WN, UA = BM * 8 / TH, UB = BN * 8 / TH;
-    constexpr uint32_t CB = FMT == kMx4 ? 4 : 8;   // bytes of 8 codes
+    constexpr uint32_t CB = FMT == kMx4 ? 4 : FMT == kMx8 ? 8 : 16;   // bytes of 8 codes, or bf16 values
+    typedef uint32_t Codes __attribute__((ext_vector_type(FMT == kDecoded ? 4 : 2)));
     // Two stages: both tiles of a, then both of the MX matrix, so that a lane's offsets within
     // either are a register and a constant of 16 bits.
     constexpr uint32_t kA = BM * kBK * 2, kB = BN * kBK * 2;
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
 
     f32x16 acc[MI][NJ] = {};
     u32x4 ra[UA];
-    u32x2 rb[UB];
+    Codes rb[UB];
     uint8_t re[UB];
 
     // Offsets in the LDS: of the reads (see frag_k_at, frag_t_at), and of this thread's writes.
@@ -175,16 +179,20 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
     };
     auto load_a = [&](int i) { ra[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer_at(pa), oa[i], 0, 0); };
     auto load_b = [&](int i) {
-        if (FMT == kMx4)
+        if constexpr (FMT == kDecoded) {
+            rb[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer_at(pc), ob[i], 0, 0);
+            return;
+        } else if constexpr (FMT == kMx4) {
             rb[i][0] = __builtin_amdgcn_raw_buffer_load_b32(buffer_at(pc), ob[i], 0, 0);
-        else
+        } else {
             rb[i] = __builtin_amdgcn_raw_buffer_load_b64(buffer_at(pc), ob[i], 0, 0);
+        }
         re[i] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(ps), oe[i], 0, 0);
     };
     // The next stage's way from registers to the LDS, in small items, and its registers' next
     // load: per group one or two units of the MX matrix (the scale, then the codes in pairs or
     // all of E2M1's, then the write) and as many of a.
-    constexpr int kPieces = FMT == kMx4 ? 2 : 6, kGroup = UB / (UB < UA ? UB : UA) * kPieces + 1, kItems = kGroup * UA;
+    constexpr int kPieces = FMT == kDecoded ? 1 : FMT == kMx4 ? 2 : 6, kGroup = UB / (UB < UA ? UB : UA) * kPieces + 1, kItems = kGroup * UA;
     static_assert(UA == UB, "groups of one unit each");
     float scale;
     u32x4 dec;
@@ -196,11 +204,13 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
                 load_a(i);
             return;
         }
-        if (p == 0)
+        if (FMT != kDecoded && p == 0)
             scale = FMT == kMx4 ? scale4_f32(re[i]) : scale8_f32(re[i]);
         if (FMT == kMx8 && p >= 1 && p <= 4)
             dec[p - 1] = decode8_pair(rb[i][(p - 1) / 2], (p - 1) % 2, scale);
         if (p == kPieces - 1) {
+            if constexpr (FMT == kDecoded)
+                dec = rb[i];
             if (FMT == kMx4)
                 dec = decode4_bf16(rb[i][0], scale);
             *reinterpret_cast<u32x4 *>(lds + wb_at + half * kB + i * TH * 16) = dec;
@@ -233,15 +243,16 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
             const uint32_t u = i * TH + t;
             const uint32_t row = TB ? k0 + u / (BN / 8) : n0 + u / 8;
             const uint32_t unit = TB ? n0 / 8 + u % (BN / 8) : k0 / 8 + u % 8;   // 8 codes, 4 to a block
-            rb[i] = u32x2{0, 0};
+            rb[i] = Codes(0);
             re[i] = 0;
             if (row < (TB ? g.k : g.n) && unit / 4 < g.nb) {
                 const uint64_t at = (uint64_t)row * g.nb;
-                re[i] = g.q.scales[at + unit / 4];
+                if (FMT != kDecoded)
+                    re[i] = g.q.scales[at + unit / 4];
                 if (FMT == kMx4)
                     rb[i][0] = reinterpret_cast<const uint32_t *>(g.q.codes)[at * 4 + unit];
                 else
-                    rb[i] = reinterpret_cast<const u32x2 *>(g.q.codes)[at * 4 + unit];
+                    rb[i] = reinterpret_cast<const Codes *>(g.q.codes)[at * 4 + unit];
             }
         }
     };
@@ -434,8 +445,10 @@ struct Plan {
     bool laid_out;
     uint32_t planes;
     uint64_t a_ld, a_bytes;
+    bool decoded;                             // the MX matrix is decoded there as well
+    uint64_t q_bytes;
     uint32_t stages, splits, per;             // of 64 summed values; parts of the sum, stages in each
-    uint64_t bytes() const { return a_bytes + (splits > 1 ? (uint64_t)splits * m * n * 4 : 0); }
+    uint64_t bytes() const { return a_bytes + q_bytes + (splits > 1 ? (uint64_t)splits * m * n * 4 : 0); }
 };
 
 // One way to run a product, its sum in up to `splits` parts.
@@ -489,7 +502,16 @@ Plan plan_of(const MxProduct &p, int num_cu)
     const uint64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), sum = stages * (in_place ? 1 : terms);
     uint64_t splits = tiles >= cu ? 1 : cu * 2 / (tiles ? tiles : 1);
     splits = splits < sum / 4 ? splits : sum / 4;
-    const Plan as_tiles = plan_as(p, kTiles, tile, !in_place, splits);
+    Plan as_tiles = plan_as(p, kTiles, tile, !in_place, splits);
+    // The kept input of a weight gradient is decoded by every row of tiles again, 24 instructions
+    // for 8 values, which only partly fit between the matrix instructions. Where there are many
+    // rows of tiles, once beforehand is less (8192 inputs, bf16, in the kernel and beforehand:
+    // 4096 tokens and 8192 outputs 485 and 441 us, 4096 outputs 252 and 239; 1000 tokens and
+    // 4096 outputs 92 and 87, 2048 outputs 46 and 49).
+    if (p.op == kWeightGrad && tile == 256 && as_tiles.planes * m >= 4096) {
+        as_tiles.decoded = true;
+        as_tiles.q_bytes = p.m * mx_blocks(p.k) * 64;
+    }
     const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
     if (tile == 256 || span >= 1ull << 31 || a_cols < 8 || k == 0)
         return as_tiles;
@@ -840,13 +862,14 @@ static hipError_t lay_out(const MxProduct &p, const Plan &r, hipStream_t s)
     return hipSuccess;
 }
 
-static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &a, float *parts, hipStream_t s)
+static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &a, const MxMatrix &q, float *parts,
+                               hipStream_t s)
 {
     Gemm g = {};
     g.a = reinterpret_cast<const uint16_t *>(a.p);
     g.lda = a.ld;
     g.a_plane = r.a_rows * r.a_ld;
-    g.q = p.q;
+    g.q = q;
     g.nb = (uint32_t)mx_blocks(p.k);
     g.m = (uint32_t)r.m;
     g.n = (uint32_t)r.n;
@@ -854,7 +877,7 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
     g.stages = r.stages;
     g.planes = r.planes;
     const bool ta = p.op == kWeightGrad, tb = p.op != kLinear;
-    const uint64_t span_a = (ta ? kBK : 256) * g.lda * 2 + 512, span_b = (tb ? kBK : 256) * (uint64_t)g.nb * 32 + 8192;
+    const uint64_t span_a = (ta ? kBK : 256) * g.lda * 2 + 512, span_b = (tb ? kBK : 256) * (uint64_t)g.nb * (r.decoded ? 64 : 32) + 8192;
     g.whole = span_a < 1ull << 32 && span_b < 1ull << 32 ? g.k / kBK : 0;
     g.splits = r.splits;
     g.per = r.per;
@@ -877,8 +900,10 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
         MX_GEMM(kMx4, false, false);
     else if (p.op == kGradInput)
         MX_GEMM(kMx4, false, true);
-    else
+    else if (!r.decoded)
         MX_GEMM(kMx8, true, true);
+    else
+        hipLaunchKernelGGL((gemm_kernel<kDecoded, true, true, 2, 4, 4>), grid, dim3(kThreads), 0, s, g);
 #undef MX_GEMM
     return hipGetLastError();
 }
@@ -892,7 +917,14 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
         return hipSuccess;
     MxRows a = p.a;
     uint32_t type = p.type;
-    float *parts = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.work) + r.a_bytes);
+    float *parts = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(p.work) + r.a_bytes + r.q_bytes);
+    MxMatrix q = p.q;
+    if (r.decoded) {
+        q = {reinterpret_cast<uint8_t *>(p.work) + r.a_bytes, nullptr};
+        const hipError_t e = launch_mx_dequantize(kMx8, kBf16, p.q, p.m, p.k, {q.codes, mx_blocks(p.k) * kMxBlock}, s);
+        if (e != hipSuccess)
+            return e;
+    }
     if (r.laid_out) {
         const hipError_t e = lay_out(p, r, s);
         if (e != hipSuccess)
@@ -902,7 +934,7 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     }
     hipError_t e;
     if (r.path == kTiles) {
-        e = launch_tiles(p, r, a, parts, s);
+        e = launch_tiles(p, r, a, q, parts, s);
     } else {
         SmallProduct g = {};
         g.a = a;
