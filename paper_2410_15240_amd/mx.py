@@ -11,7 +11,7 @@ import ctypes as _ct
 
 import torch as _torch
 
-from . import _call, _raw_stream, _used_on, lib
+from . import EINVAL, _call, _check, _raw_stream, _used_on, lib
 
 _Tensor, _uint8, _int8 = _torch.Tensor, _torch.uint8, _torch.int8
 _TYPES = {_torch.bfloat16: 0, _torch.float16: 1, _torch.float32: 2}
@@ -125,9 +125,10 @@ def _float(t, what, idx=None):
     code = _TYPES.get(t.dtype)
     if code is None:
         raise ValueError("%s must be bfloat16, float16 or float32, got %s" % (what, t.dtype))
-    if not t.is_cuda:
+    at = t.get_device()
+    if at < 0:
         raise ValueError("%s must be a CUDA tensor" % what)
-    if idx is not None and t.get_device() != idx:
+    if idx is not None and at != idx:
         raise ValueError("%s is on %s, the other operands on cuda:%d" % (what, t.device, idx))
     shape = t.shape
     if len(shape) == 2:
@@ -170,9 +171,12 @@ def _out(t, what, shape, dtype, device, idx):
 def _mx(q, what, cls, idx=None, rows=None, cols=None):
     if type(q) is not cls:
         raise ValueError("%s must be an %s" % (what, cls.__name__))
-    if not q.codes.is_cuda:
+    at = q.codes.get_device()
+    if at >= 0 and idx is None and rows is None and cols is None:
+        return q
+    if at < 0:
         raise ValueError("%s must be a CUDA tensor" % what)
-    if idx is not None and q.codes.get_device() != idx:
+    if idx is not None and at != idx:
         raise ValueError("%s is on %s, the other operands on cuda:%d" % (what, q.codes.device, idx))
     if (rows is not None and q.rows != rows) or (cols is not None and q.cols != cols):
         raise ValueError("%s is %d x %d, the call needs %s x %s"
@@ -248,22 +252,28 @@ def mx8_dequantize(q, dtype=None, out=None, stream=None):
     return _dequantize(MX8, q, dtype, out, stream)
 
 
-def _workspace(op, code, p, ld, m, n, k, work, device, idx, new):
-    """(address, bytes) of a product's workspace: the caller's, or a new one where it needs any."""
+def _product(fn, op, a, work, device, idx, new, stream, head, tail):
+    """Run a product's C entry: its arguments are head, the sizes and tail, the workspace and the stream. a is (type, address,
+    stride, m, n, k) of what its workspace depends on. Most small products need none, so the call is made without one
+    first; where it is refused for that, nothing was enqueued, and it is made again with one."""
+    raw = _raw_stream(stream, idx)
     if work is not None:
         if not isinstance(work, _Tensor) or work.dtype != _uint8 or not work.is_contiguous() or work.get_device() != idx:
             raise ValueError("work must be a contiguous uint8 tensor on the operands' device")
-        return work.data_ptr(), work.numel()
-    if _torch._C._cuda_getDevice() == idx:
-        need = lib().fastrack_mx_work_bytes(op, code, p, ld, m, n, k)
-    else:
+        _call(fn, idx, *head, *a[3:], *tail, work.data_ptr(), work.numel(), raw)
+        return
+    if _torch._C._cuda_getDevice() != idx:
         with _torch.cuda.device(idx):
-            need = lib().fastrack_mx_work_bytes(op, code, p, ld, m, n, k)
-    if need == 0:
-        return None, 0
-    work = _torch.empty(need, dtype=_uint8, device=device)
-    new.append(work)
-    return work.data_ptr(), need
+            return _product(fn, op, a, work, device, idx, new, raw, head, tail)
+    rc = fn(*head, *a[3:], *tail, None, 0, raw)
+    if rc == EINVAL:
+        need = lib().fastrack_mx_work_bytes(op, *a)
+        if need:
+            work = _torch.empty(need, dtype=_uint8, device=device)
+            new.append(work)
+            rc = fn(*head, *a[3:], *tail, work.data_ptr(), need, raw)
+    if rc:
+        _check(rc)
 
 
 def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
@@ -277,9 +287,8 @@ def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
         device, idx, m = w.codes.device, w.codes.get_device(), x.rows
         dtype = _dtype(dtype, _torch.bfloat16 if out is None else out.dtype)
         out, p, ld, fresh = _out(out, "out", (m, w.rows), dtype, device, idx)
-        wp, wn = _workspace(_LINEAR_MX, 0, None, 0, m, w.rows, w.cols, work, device, idx, new)
-        _call(lib().fastrack_mx_linear_mx, idx, x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(),
-              w.scales.data_ptr(), m, w.rows, w.cols, _TYPES[dtype], p, ld, wp, wn, _raw_stream(stream, idx))
+        _product(lib().fastrack_mx_linear_mx, _LINEAR_MX, (0, None, 0, m, w.rows, w.cols), work, device, idx, new, stream,
+                 (x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
     else:
         device, idx = w.codes.device, w.codes.get_device()
         xp, xld, m, k, code = _float(x, "x", idx)
@@ -287,9 +296,8 @@ def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
             raise ValueError("x has %d columns, the weights %d" % (k, w.cols))
         dtype = _dtype(dtype, x.dtype if out is None else out.dtype)
         out, p, ld, fresh = _out(out, "out", x.shape[:-1] + (w.rows,), dtype, device, idx)
-        wp, wn = _workspace(_LINEAR, code, xp, xld, m, w.rows, k, work, device, idx, new)
-        _call(lib().fastrack_mx_linear, idx, code, xp, xld, w.codes.data_ptr(), w.scales.data_ptr(), m, w.rows, k,
-              _TYPES[dtype], p, ld, wp, wn, _raw_stream(stream, idx))
+        _product(lib().fastrack_mx_linear, _LINEAR, (code, xp, xld, m, w.rows, k), work, device, idx, new, stream,
+                 (code, xp, xld, w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
     if fresh:
         new.append(out)
     _keep(new, stream, device)
@@ -306,9 +314,8 @@ def mx4_linear_grad_input(dy, w, dtype=None, out=None, work=None, stream=None):
         raise ValueError("dy has %d columns, the weights %d rows" % (n, w.rows))
     dtype = _dtype(dtype, dy.dtype if out is None else out.dtype)
     out, p, ld, fresh = _out(out, "out", dy.shape[:-1] + (w.cols,), dtype, device, idx)
-    wp, wn = _workspace(_GRAD_INPUT, code, yp, yld, m, n, w.cols, work, device, idx, new)
-    _call(lib().fastrack_mx_linear_grad_input, idx, code, yp, yld, w.codes.data_ptr(), w.scales.data_ptr(), m, n, w.cols,
-          _TYPES[dtype], p, ld, wp, wn, _raw_stream(stream, idx))
+    _product(lib().fastrack_mx_linear_grad_input, _GRAD_INPUT, (code, yp, yld, m, n, w.cols), work, device, idx, new, stream,
+             (code, yp, yld, w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
     if fresh:
         new.append(out)
     _keep(new, stream, device)
@@ -327,9 +334,9 @@ def mx8_weight_grad(dy, saved, dtype=None, out=None, accumulate=False, work=None
     if accumulate and (out is None or dtype != _torch.float32):
         raise ValueError("accumulate=True needs a float32 out to add to")
     out, p, ld, fresh = _out(out, "out", (n, saved.cols), dtype, device, idx)
-    wp, wn = _workspace(_WEIGHT_GRAD, code, yp, yld, m, n, saved.cols, work, device, idx, new)
-    _call(lib().fastrack_mx_weight_grad, idx, code, yp, yld, saved.codes.data_ptr(), saved.scales.data_ptr(), m, n,
-          saved.cols, _TYPES[dtype], p, ld, 1 if accumulate else 0, wp, wn, _raw_stream(stream, idx))
+    _product(lib().fastrack_mx_weight_grad, _WEIGHT_GRAD, (code, yp, yld, m, n, saved.cols), work, device, idx, new, stream,
+             (code, yp, yld, saved.codes.data_ptr(), saved.scales.data_ptr()),
+             (_TYPES[dtype], p, ld, 1 if accumulate else 0))
     if fresh:
         new.append(out)
     _keep(new, stream, device)
