@@ -90,11 +90,22 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds
     }
 }
 
-// One tile of c, or of one part of it, by 2 x 2 waves of 32 MI x 32 NJ outputs each. TA: a is
+// One tile of c, or of one part of it, by 2 x WN waves of 32 MI x 32 NJ outputs each. TA: a is
 // summed over its rows (a[k][m]) instead of along them (a[m][k]); TB: the same of the MX
 // matrix. While a stage of 64 summed values is multiplied out of one half of the LDS, the next
 // one is decoded from registers to bf16 in the other half, and the one after is on its way
 // from memory.
+//
+// The large tile is 256 x 256 with four waves of 128 x 128, one on each SIMD: a stage's 2048
+// cycles of products then need 1024 cycles of operand reads and 512 of writes from the LDS,
+// where waves of 64 x 64 in a tile of 128 need 3072 (661 us instead of 414 for 4096 tokens and
+// 8192 x 8192 weights of bf16; eight waves of 128 x 64, 414 too, and 572 instead of 490 where
+// both operands are read across their rows). A wave alone on its SIMD has only its own work to
+// put beside its products, so that is dealt out by hand, a few instructions after each
+// (compiled in its own order: 514). Measured for that layer: linear 405-415 us (1.33-1.36
+// PFLOP/s), input gradient 380-390 (1.41-1.45), weight gradient 439 with its decoding; the
+// library's bf16 product of these sizes 421. The matrix unit is busy 70-76% of the cycles; what
+// bounds them is power, which holds the clock near 1.7 GHz under this load.
 //
 // Stages of 64 whole values come first, of every term of a, then the terms' last, short ones.
 // A whole stage is read without a check: rows and columns past the matrices' ends read the
@@ -373,24 +384,34 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
     put_tile<WN, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
-// c = the sum of the parts, always in the same order.
+// c = the sum of the parts, always in their order; four values of a row to a thread, or fewer at
+// its end. (Products are cut only where they have fewer tiles than CUs: below 2^32 values.)
 __global__ __launch_bounds__(kThreads) void join_kernel(const float *parts, uint32_t splits, uint32_t m, uint32_t n,
-                                                        void *c, uint64_t ldc, uint32_t ctype, uint32_t accumulate)
+                                                        uint32_t per_row, uint32_t recip, Out o)
 {
-    const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x, total = (uint64_t)m * n;
-    if (i >= total)
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x, row = div_recip(i, per_row, recip), c = (i - row * per_row) * 4;
+    if (row >= m)
         return;
-    float v = 0.0f;
-    for (uint32_t s = 0; s < splits; ++s)
-        v += parts[s * total + i];
-    const uint64_t at = i / n * ldc + i % n;
-    if (ctype == kFp32) {
-        float *p = reinterpret_cast<float *>(c) + at;
-        *p = accumulate ? *p + v : v;
-    } else if (ctype == kBf16) {
-        reinterpret_cast<__bf16 *>(c)[at] = (__bf16)v;
+    const uint64_t total = (uint64_t)m * n;
+    const float *p = parts + (uint64_t)row * n + c;
+    if (c + 4 <= n) {
+        f32x4 v = {0, 0, 0, 0};
+#pragma unroll 4
+        for (uint32_t s = 0; s < splits; ++s) {
+            f32x4 w;
+            __builtin_memcpy(&w, p + s * total, 16);
+            v += w;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            put1(o, row, c + j, v[j]);
     } else {
-        reinterpret_cast<_Float16 *>(c)[at] = (_Float16)v;
+        for (uint32_t j = c; j < n; ++j) {
+            float v = 0.0f;
+            for (uint32_t s = 0; s < splits; ++s)
+                v += p[s * total + j - c];
+            put1(o, row, j, v);
+        }
     }
 }
 
@@ -561,7 +582,10 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // read like one of 64 bf16 values above (16 bytes are a block here), and its 8 scales of each
 // row beside it. A lane reads its row's 8 scales at once, and the instruction picks the byte:
 // blocks 2 ks of the lower lanes, 2 ks + 1 of the upper ones, whose words are shifted down by
-// one byte.
+// one byte. 143-148 us for 4096 tokens and 8192 x 8192 weights (3.7 PFLOP/s; tiles of 128 and one
+// stage in LDS took 538), the matrix unit busy 57% of the cycles: a stage brings 68 KB to a
+// workgroup in the time in which gemm_kernel brings 40 to 48, and its waits are what is left.
+// (The checked last stages spill a few registers; the main loop does not.)
 template <int MI, int NJ>
 __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Gemm4 g)
 {
@@ -825,15 +849,15 @@ Gemm4 plan4_of(const Mx4Product &p, int num_cu)
 
 using namespace mx;
 
-static hipError_t join(const float *parts, const Plan &r, const MxProduct &p, hipStream_t s)
+static hipError_t join(const float *parts, uint32_t splits, uint64_t m, uint64_t n, const Out &o, hipStream_t s)
 {
-    const uint64_t total = r.m * r.n;
-    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((total + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, parts,
-                       r.splits, (uint32_t)r.m, (uint32_t)r.n, p.c.p, p.c.ld, p.ctype, (uint32_t)p.accumulate);
+    const uint32_t per_row = (uint32_t)((n + 3) / 4);
+    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((m * per_row + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, parts,
+                       splits, (uint32_t)m, (uint32_t)n, per_row, div_recip_of(per_row), o);
     return hipGetLastError();
 }
 
-// a's terms into the workspace; g and its planes as laid out there.
+// a's bf16 terms into the workspace.
 static hipError_t lay_out(const MxProduct &p, const Plan &r, hipStream_t s)
 {
     Terms g = {};
@@ -952,7 +976,9 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
         g.parts = parts;
         e = r.path == kDot ? launch_mx_dot(g, type, s) : launch_mx_small(g, p.op, type, r.tile, s);
     }
-    return e == hipSuccess && r.splits > 1 ? join(parts, r, p, s) : e;
+    return e == hipSuccess && r.splits > 1
+               ? join(parts, r.splits, r.m, r.n, {p.c.p, p.c.ld, p.ctype, p.accumulate}, s)
+               : e;
 }
 
 uint64_t mx4_product_work(const Mx4Product &p, int num_cu)
@@ -976,12 +1002,7 @@ hipError_t launch_mx4_product(const Mx4Product &p, int num_cu, hipStream_t s)
     else
         hipLaunchKernelGGL((gemm4_kernel<2, 2>), grid, dim3(kThreads), 0, s, g);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || g.splits == 1)
-        return e;
-    const uint64_t total = p.m * p.n;
-    hipLaunchKernelGGL(join_kernel, dim3((uint32_t)((total + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, g.parts,
-                       g.splits, g.m, g.n, g.c, g.ldc, g.ctype, 0u);
-    return hipGetLastError();
+    return e == hipSuccess && g.splits > 1 ? join(g.parts, g.splits, p.m, p.n, {p.c.p, p.c.ld, p.ctype, 0}, s) : e;
 }
 
 }  // namespace fastrack

@@ -111,7 +111,7 @@ template <uint32_t T> struct Unit8 {
 // before it uses the first, and multiplies them with the x of those places, which it keeps in
 // registers for all R. bf16 by the pairwise product, 16 and 32-bit floats in 32 bits. The
 // lanes' sums meet in LDS. What bounds it is the reading of w, K / 2 + K / 32 bytes a row: 7.1
-// us for 8192 x 8192, 5 TB/s. (Lanes that read 64 bytes each of 16 rows, as the matrix
+// us for 8192 x 8192, 5 TB/s (6.6 alone). (Lanes that read 64 bytes each of 16 rows, as the matrix
 // instruction takes them, took twice that: rows a power of two apart are one memory channel's
 // work at a time.)
 constexpr int kDotWaves = 4;
@@ -227,7 +227,8 @@ __global__ __launch_bounds__(64 * kDotWaves, 4) void dot_kernel(SmallProduct g)
 // there. Nothing waits for another wave. Terms of a 16 or 32-bit float go through the same
 // bytes one after the other. The slice after is on its way from memory meanwhile. What bounds
 // it is the issue of instructions: the splitting and decoding are repeated by every tile along
-// the other axis.
+// the other axis. 90 tokens and 700 x 700 weights of bf16 4.2 us (gemm_kernel and its joining of
+// parts 12.4), 77 tokens of fp32 and 1000 x 1111 9.1 (20), 29 of fp16 and 2777 x 5003 13 (26).
 
 // Place of chunk c (8 values) of row r: rows of 8 chunks as in at_k, rows of 4 with the chunks
 // turned by bits 2 and 3 of the row, which again spreads 16 rows over all banks.

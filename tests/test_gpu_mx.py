@@ -353,6 +353,25 @@ def test_infinities_and_nans_reach_the_rows_they_belong_to(op, name, m):
     assert np.array_equal(np.nan_to_num(got, nan=1e9), np.nan_to_num(want, nan=1e9)) and np.isnan(got).any()
 
 
+@pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("op", ["linear", "grad", "weight"])
+def test_infinities_and_nans_among_many_outputs(op, name):
+    rng = np.random.default_rng(13)
+    rows, cols, sums = 2900, 3000, 330
+    m, n, k = dict(linear=(rows, cols, sums), grad=(rows, sums, cols), weight=(sums, rows, cols))[op]
+    x, q, v, f = layer(rng, op, m, n, k, "whole")
+    x[0, 5], x[300, 7], x[m - 1, x.shape[1] - 1] = np.inf, np.nan, -np.inf
+    scales = q.scales.clone()
+    scales[q.rows - 1, 2] = 255
+    v[q.rows - 1, 64:96] = np.nan
+    with np.errstate(invalid="ignore"):
+        want = f(x)
+    for pad in (0, 3):
+        got = f64(product(op, gpu(x, TYPES[name], pad), type(q)(q.codes, scales, k), dtype=torch.float32))
+        assert np.array_equal(np.nan_to_num(got, nan=1e9, posinf=2e9, neginf=3e9),
+                              np.nan_to_num(want, nan=1e9, posinf=2e9, neginf=3e9))
+
+
 def test_product_of_two_mx4_with_a_nan_block():
     rng = np.random.default_rng(12)
     qx, vx = random_mx(rng, 40, 160, 4, True)
