@@ -26,6 +26,7 @@ struct Gemm {
     const uint16_t *a;       // bf16 terms of the float matrix, `planes` of them
     uint64_t a_plane;        // elements between them
     uint64_t lda;
+    uint32_t a_cols;         // values of a row that may be read: laid-out rows end in zeros
     MxMatrix q;
     uint32_t nb;             // blocks in a row of q
     uint32_t m, n, k;        // output m x n, summed axis k
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
         for (int i = 0; i < UA; ++i) {
             const uint32_t u = i * TH + t;
             const uint32_t row = TA ? k0 + u / (BM / 8) : m0 + u / 8, col = TA ? m0 + u % (BM / 8) * 8 : k0 + u % 8 * 8;
-            ra[i] = row < (TA ? g.k : g.m) ? chunk_at(a + row * g.lda, col, TA ? g.m : g.k) : u32x4{0, 0, 0, 0};
+            ra[i] = row < (TA ? g.k : g.m) ? chunk_at(a + row * g.lda, col, g.a_cols) : u32x4{0, 0, 0, 0};
         }
 #pragma unroll
         for (int i = 0; i < UB; ++i) {
@@ -892,6 +893,7 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
     Gemm g = {};
     g.a = reinterpret_cast<const uint16_t *>(a.p);
     g.lda = a.ld;
+    g.a_cols = (uint32_t)(r.laid_out ? r.a_ld : r.a_cols);
     g.a_plane = r.a_rows * r.a_ld;
     g.q = q;
     g.nb = (uint32_t)mx_blocks(p.k);
