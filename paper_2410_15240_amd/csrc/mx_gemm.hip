@@ -499,6 +499,28 @@ Plan plan_as(const MxProduct &p, Path path, uint32_t tile, bool laid_out, uint64
     return r;
 }
 
+// A product's time in us beyond its ends when its sum is cut: the longest part, the parts in fp32
+// written and read at 4 TB/s, and the joining launch.
+double cut_us(double whole_us, uint64_t cuts, uint64_t outputs)
+{
+    return whole_us / (double)cuts + (cuts > 1 ? 3.0 + 8e-6 / 4.0 * (double)(outputs * cuts) : 0.0);
+}
+
+// The number of parts of a sum for which that is least, up to one part for every CU (a second
+// round adds parts without shortening any) and down to 4 stages a part. (Parts: us. bf16 linear,
+// 3000 tokens, 1000 x 1000, 192 tiles: 1: 16, 2: 27; 300 tokens, 5000 x 5000, 120 tiles: 1: 51, 2: 38,
+// 4: 39. MX4 by MX4, 512 tokens, 4096 x 4096, 128 tiles: 1: 13, 2: 23, 4: 25; 64 tokens, 8192 x 8192,
+// 64 tiles: 1: 20, 4: 15, 8: 18; 128 tokens, 16384 x 1024, 8 tiles: 1: 30, 8: 13, 16: 14.)
+uint64_t cuts_of(double whole_us, uint64_t tiles, uint64_t stages, uint64_t outputs, uint64_t cu)
+{
+    uint64_t most = tiles ? cu / tiles : 1, best = 1;
+    most = most < stages / 4 ? most : stages / 4;
+    for (uint64_t c = 2; c <= most; c++)
+        if (cut_us(whole_us, c, outputs) < cut_us(whole_us, best, outputs))
+            best = c;
+    return best;
+}
+
 Plan plan_of(const MxProduct &p, int num_cu)
 {
     const uint64_t cu = (uint64_t)num_cu;
@@ -515,15 +537,18 @@ Plan plan_of(const MxProduct &p, int num_cu)
                           (!ta || a_cols % 8 == 0);
     const uint64_t stages = (k + kBK - 1) / kBK, terms = planes_of(p.type);
 
-    // gemm_kernel: tiles of 256 where they give half the CUs work and the sum is long enough to
-    // pay for a tile's ends (64 tokens' gradient of 8192 x 8192 weights: 67 us with tiles of
-    // 128, 85 with 256; 300 tokens' of 4000 x 4000: 29.5 and 27.9), else of 128 and the sum cut
-    // until there are two for every CU, down to 4 stages a part.
+    // gemm_kernel: tiles of 256 where they give more than half the CUs work and the sum is long
+    // enough to pay for a tile's ends (64 tokens' gradient of 8192 x 8192 weights: 67 us with tiles
+    // of 128, 85 with 256; 300 tokens' of 4000 x 4000: 29.5 and 27.9), else of 128. Up to half the
+    // CUs, tiles of 128, two to a CU, still fit in one round. (bf16 linear, 128 and 256: 2048
+    // tokens, 4096 x 4096 79 and 92 us; 3000 tokens, 3000 x 4000 104 and 81; 1500 tokens, 6000 x
+    // 6000 167 and 124.) A stage of a tile of 128 alone on its CU takes 0.4 us, 0.65 where the
+    // operands are transposed, and the sum of each is cut where that pays.
     const uint64_t large = (m + 255) / 256 * ((n + 255) / 256);
-    const uint32_t tile = large >= cu / 2 && stages >= 4 ? 256 : 128;
+    const uint32_t tile = large > cu / 2 && stages >= 4 ? 256 : 128;
     const uint64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), sum = stages * (in_place ? 1 : terms);
-    uint64_t splits = tiles >= cu ? 1 : cu * 2 / (tiles ? tiles : 1);
-    splits = splits < sum / 4 ? splits : sum / 4;
+    const double whole_us = (ta ? 0.65 : 0.4) * (double)sum;
+    const uint64_t splits = tile == 256 ? 1 : cuts_of(whole_us, tiles, sum, m * n, cu);
     Plan as_tiles = plan_as(p, kTiles, tile, !in_place, splits);
     // The kept input of a weight gradient is decoded by every row of tiles again, 24 instructions
     // for 8 values, which only partly fit between the matrix instructions. Where there are many
@@ -541,8 +566,8 @@ Plan plan_of(const MxProduct &p, int num_cu)
     // Small tiles or gemm_kernel's of 128, by estimates of their times in us. A workgroup of small
     // tiles takes 3 and an eighth of what its slices were measured to take a wave; those of 32
     // run two to a CU. Slower where a tile reads a few bytes each of long rows of the MX matrix.
-    // gemm_kernel takes 15, 4 more to lay out a's terms, and what its whole tiles' products take
-    // at 1 PFLOP/s. (Both sides: linear, 1000 x 2000 x 1000 of bf16: 12 and 26; 128 tokens, 8192 x
+    // gemm_kernel takes 8, 4 more to lay out a's terms, and its sum's time as above, a quarter more
+    // for every round of several. (Both sides: linear, 1000 x 2000 x 1000 of bf16: 12 and 26; 128 tokens, 8192 x
     // 8192 of fp32: 125 and 71; gradient of 32 tokens, 8192 x 8192 of bf16: 48 and 25; weight
     // gradient of 64 tokens, 8192 x 8192: 216 and 67, of 3000 tokens, 1000 x 1000: 20 and 27.)
     const uint64_t tiles64 = (m + 63) / 64 * ((n + 63) / 64), tiles32 = (m + 31) / 32 * ((n + 31) / 32);
@@ -556,7 +581,8 @@ Plan plan_of(const MxProduct &p, int num_cu)
     cuts = cuts < 1 ? 1 : cuts;
     const double small = (double)((count * cuts + at_once - 1) / at_once) * (3.0 + slice * (double)stages / (8.0 * (double)cuts)) +
                          (cuts > 1 ? 4.0 : 0.0);
-    const double large_us = 15.0 + (in_place ? 0.0 : 4.0) + 2e-9 * 128.0 * 128.0 * (double)tiles * (double)(sum * kBK);
+    const double rounds = tiles <= cu ? 1.0 : 1.25 * (double)((tiles + cu - 1) / cu);
+    const double large_us = 8.0 + (in_place ? 0.0 : 4.0) + cut_us(whole_us * rounds, splits, m * n);
     return small <= large_us ? plan_as(p, kSmall, by64 ? 64 : 32, false, cuts) : as_tiles;
 }
 
@@ -830,15 +856,15 @@ Gemm4 plan4_of(const Mx4Product &p, int num_cu)
     g.n = (uint32_t)p.n;
     g.whole = 256ull * g.nb * 16 + 128 < 1ull << 32 ? g.nb / 8 : 0;   // a tile's offsets in 32 bits
     g.stages = (g.nb + 7) / 8;
-    g.tile = (p.m + 255) / 256 * ((p.n + 255) / 256) >= (uint64_t)num_cu / 2 ? 256 : 128;
+    // Tiles of 256 where they give more than half the CUs work, as for gemm_kernel (128 and 256:
+    // 2048 tokens, 4096 x 4096 29 and 36 us; 3000 tokens, 3000 x 4000 43 and 42; 1500 tokens, 6000 x
+    // 6000 61 and 55), uncut. A stage of a tile of 128 takes 0.5 us.
+    g.tile = (p.m + 255) / 256 * ((p.n + 255) / 256) > (uint64_t)num_cu / 2 ? 256 : 128;
     g.tm = (uint32_t)((p.m + g.tile - 1) / g.tile);
     g.tn = (uint32_t)((p.n + g.tile - 1) / g.tile);
     const uint64_t tiles = (uint64_t)g.tm * g.tn;
-    uint64_t splits = tiles >= (uint64_t)num_cu ? 1 : (uint64_t)num_cu * 2 / (tiles ? tiles : 1);
-    if (splits > g.stages / 4)
-        splits = g.stages / 4;
-    if (splits < 1)
-        splits = 1;
+    const uint64_t splits =
+        g.tile == 256 ? 1 : cuts_of(0.5 * (double)g.stages, tiles, g.stages, p.m * p.n, (uint64_t)num_cu);
     g.per = (uint32_t)((g.stages + splits - 1) / splits);
     if (g.per == 0)
         g.per = 1;

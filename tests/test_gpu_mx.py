@@ -267,6 +267,33 @@ def test_products_of_middling_sizes_are_exact_on_whole_numbers(op, name, m, n, k
 
 @pytest.mark.parametrize("op", ["linear", "grad", "weight"])
 @pytest.mark.parametrize("name", list(TYPES))
+@pytest.mark.parametrize("rows,cols,sums", [(2048, 4093, 333), (2049, 4096, 333), (1021, 4001, 1000), (3000, 1003, 200),
+                                            (64, 8190, 6001), (130, 900, 9000)])
+def test_products_about_one_round_of_tiles_are_exact_on_whole_numbers(op, name, rows, cols, sums):
+    """The largest tiles for just up to half the CUs and for one more row, tiles of 128 for most of
+    them, and so few that the sum is cut."""
+    m, n, k = dict(linear=(rows, cols, sums), grad=(rows, sums, cols), weight=(sums, rows, cols))[op]
+    rng = np.random.default_rng(rows + cols + sums)
+    x, q, _, f = layer(rng, op, m, n, k, "whole")
+    x = np.clip(x, -4, 4)   # |x q| <= 64: 9000 of them stay below 2^24
+    want = torch.from_numpy(f(x)).float()
+    for pad in (0, 3):
+        got = product(op, gpu(x, TYPES[name], pad), q, dtype=torch.float32).cpu()
+        assert torch.equal(got, want), (pad, torch.nonzero(got != want)[:4].tolist())
+
+
+@pytest.mark.parametrize("m,n,k", [(2048, 4093, 700), (2049, 4096, 700), (515, 4100, 1300), (65, 8190, 5000), (130, 900, 4999)])
+def test_product_of_two_mx4_about_one_round_of_tiles(m, n, k):
+    rng = np.random.default_rng(m + n + k)
+    qx, vx = random_mx(rng, m, k, 4, True)
+    qw, vw = random_mx(rng, n, k, 4, True)
+    want = torch.from_numpy(vx @ vw.T).float()
+    got = F.mx4_linear(qx, qw, dtype=torch.float32).cpu()
+    assert torch.equal(got, want), torch.nonzero(got != want)[:4].tolist()
+
+
+@pytest.mark.parametrize("op", ["linear", "grad", "weight"])
+@pytest.mark.parametrize("name", list(TYPES))
 @pytest.mark.parametrize("out", list(TYPES))
 @pytest.mark.parametrize("m,n,k", [(1, 96, 700), (29, 200, 333), (150, 140, 260), (300, 30, 70)])
 def test_products_of_normal_inputs(op, name, out, m, n, k):
