@@ -242,6 +242,22 @@ def _used_on(tensors, streams, device):
                 t.record_stream(so)
 
 
+def _fresh(shape, device, stream, dtype=_uint8):
+    """A new tensor that work enqueued on `stream` writes. Its memory is `stream`'s own: memory of the
+    caller's stream may just have been freed there, in that stream's order, by work that still uses it and
+    that nothing makes `stream` wait for. The caller's stream may use the tensor too once it is ordered
+    after `stream`."""
+    if stream is None:
+        return _torch.empty(shape, dtype=dtype, device=device)
+    cur, so = _torch.cuda.current_stream(device), _stream_obj(stream, device)
+    if so.cuda_stream == cur.cuda_stream:
+        return _torch.empty(shape, dtype=dtype, device=device)
+    with _torch.cuda.stream(so):
+        t = _torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(cur)
+    return t
+
+
 def num_chains(length, chain_bytes):
     return int(lib().fastrack_num_chains(length, chain_bytes))
 

@@ -4,14 +4,15 @@ link, quantised, multiplied and differentiated by the library's HIP kernels. Arg
 The format, the rounding and the sums are documented in include/fastrack.h. A float operand is a CUDA tensor
 in bfloat16, float16 or float32 whose last axis is dense; the axes before it are taken together as its rows, which
 may be any equal distance apart (a slice of a wider tensor, or one row expanded). Work is enqueued on the current
-stream or on `stream`; results that the call allocates may be used on either. A float tensor's NaN and infinity
+stream or on `stream`, which waits for nothing on the current one: order it after what it reads, and whoever reads the
+results after it. New results may be used on either. A float tensor's NaN and infinity
 go where the formulas put them; in a quantised block they make the whole block NaN.
 """
 import ctypes as _ct
 
 import torch as _torch
 
-from . import EINVAL, _call, _check, _raw_stream, _used_on, lib
+from . import EINVAL, _call, _check, _fresh, _raw_stream, lib
 
 _Tensor, _uint8, _int8 = _torch.Tensor, _torch.uint8, _torch.int8
 _TYPES = {_torch.bfloat16: 0, _torch.float16: 1, _torch.float32: 2}
@@ -93,12 +94,12 @@ class _MX:
         return cls.view(_torch.empty(cls.nbytes(rows, cols), dtype=_uint8, device=device), rows, cols)
 
     @classmethod
-    def _new(cls, rows, cols, device):
+    def _new(cls, rows, cols, device, stream):
         """What a call returns: codes and scales of their own (a call's shapes need no check, and two allocations cost
         a third of cutting one buffer into views: 2.3 and 6.4 us)."""
         q, blocks = object.__new__(cls), -(-cols // 32)
-        q.codes = _torch.empty((rows, blocks * cls.block_bytes), dtype=cls.code_type, device=device)
-        q.scales = _torch.empty((rows, blocks), dtype=_uint8, device=device)
+        q.codes = _fresh((rows, blocks * cls.block_bytes), device, stream, cls.code_type)
+        q.scales = _fresh((rows, blocks), device, stream)
         q.rows, q.cols = rows, cols
         return q
 
@@ -155,17 +156,17 @@ def _float(t, what, idx=None):
     return t.data_ptr(), (ld if rows > 1 else cols), rows, cols, code
 
 
-def _out(t, what, shape, dtype, device, idx):
-    """The caller's output, checked, or a new one; (tensor, address, row stride, whether it is new)."""
+def _out(t, what, shape, dtype, device, idx, stream):
+    """The caller's output, checked, or a new one; (tensor, address, row stride)."""
     if t is None:
-        t = _torch.empty(shape, dtype=dtype, device=device)
-        return t, t.data_ptr(), shape[-1], True
+        t = _fresh(shape, device, stream, dtype)
+        return t, t.data_ptr(), shape[-1]
     p, ld, _, _, _ = _float(t, what, idx)
     if t.shape != _torch.Size(shape):
         raise ValueError("%s must have shape %s, got %s" % (what, tuple(shape), tuple(t.shape)))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (what, dtype, t.dtype))
-    return t, p, ld, False
+    return t, p, ld
 
 
 def _mx(q, what, cls, idx=None, rows=None, cols=None):
@@ -197,26 +198,18 @@ def _act(act):
     return _ACTS[act]
 
 
-def _keep(new, stream, device):
-    if stream is not None and new:
-        _used_on([t for x in new for t in ((x.codes, x.scales) if isinstance(x, _MX) else (x,))], [stream], device)
-
-
-def _new_mx(q, what, cls, rows, cols, device, idx, new):
+def _new_mx(q, what, cls, rows, cols, device, idx, stream):
     if q is None:
-        q = cls._new(rows, cols, device)
-        new.append(q)
-        return q
+        return cls._new(rows, cols, device, stream)
     return _mx(q, what, cls, idx, rows, cols)
 
 
 def _quantize(cls, x, out, stream):
     p, ld, rows, cols, code = _float(x, "x")
-    idx, new = x.get_device(), []
-    out = _new_mx(out, "out", cls, rows, cols, x.device, idx, new)
+    idx = x.get_device()
+    out = _new_mx(out, "out", cls, rows, cols, x.device, idx, stream)
     _call(lib().fastrack_mx_quantize, idx, cls.format, code, p, ld, rows, cols, out.codes.data_ptr(), out.scales.data_ptr(),
           _raw_stream(stream, idx))
-    _keep(new, stream, x.device)
     return out
 
 
@@ -224,10 +217,9 @@ def _dequantize(cls, q, dtype, out, stream):
     _mx(q, "q", cls)
     device, idx = q.codes.device, q.codes.get_device()
     dtype = _dtype(dtype, _torch.bfloat16 if out is None else out.dtype)
-    out, p, ld, fresh = _out(out, "out", (q.rows, q.cols), dtype, device, idx)
+    out, p, ld = _out(out, "out", (q.rows, q.cols), dtype, device, idx, stream)
     _call(lib().fastrack_mx_dequantize, idx, cls.format, q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.cols, _TYPES[dtype],
           p, ld, _raw_stream(stream, idx))
-    _keep([out] if fresh else [], stream, device)
     return out
 
 
@@ -252,7 +244,7 @@ def mx8_dequantize(q, dtype=None, out=None, stream=None):
     return _dequantize(MX8, q, dtype, out, stream)
 
 
-def _product(fn, op, a, work, device, idx, new, stream, head, tail):
+def _product(fn, op, a, work, device, idx, stream, head, tail):
     """Run a product's C entry: its arguments are head, the sizes and tail, the workspace and the stream. a is (type, address,
     stride, m, n, k) of what its workspace depends on. Most small products need none, so the call is made without one
     first; where it is refused for that, nothing was enqueued, and it is made again with one."""
@@ -264,13 +256,12 @@ def _product(fn, op, a, work, device, idx, new, stream, head, tail):
         return
     if _torch._C._cuda_getDevice() != idx:
         with _torch.cuda.device(idx):
-            return _product(fn, op, a, work, device, idx, new, raw, head, tail)
+            return _product(fn, op, a, work, device, idx, stream, head, tail)
     rc = fn(*head, *a[3:], *tail, None, 0, raw)
     if rc == EINVAL:
         need = lib().fastrack_mx_work_bytes(op, *a)
         if need:
-            work = _torch.empty(need, dtype=_uint8, device=device)
-            new.append(work)
+            work = _fresh(need, device, stream)
             rc = fn(*head, *a[3:], *tail, work.data_ptr(), need, raw)
     if rc:
         _check(rc)
@@ -281,13 +272,12 @@ def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
     unless `dtype` says otherwise. x may be an MX4 (tokens, inputs) too; y is then bfloat16 by default.
     `work` is a uint8 buffer to use as workspace; without it the call allocates what it needs."""
     w = _mx(w, "w", MX4)
-    new = []
     if isinstance(x, _MX):
         _mx(x, "x", MX4, w.codes.get_device(), cols=w.cols)
         device, idx, m = w.codes.device, w.codes.get_device(), x.rows
         dtype = _dtype(dtype, _torch.bfloat16 if out is None else out.dtype)
-        out, p, ld, fresh = _out(out, "out", (m, w.rows), dtype, device, idx)
-        _product(lib().fastrack_mx_linear_mx, _LINEAR_MX, (0, None, 0, m, w.rows, w.cols), work, device, idx, new, stream,
+        out, p, ld = _out(out, "out", (m, w.rows), dtype, device, idx, stream)
+        _product(lib().fastrack_mx_linear_mx, _LINEAR_MX, (0, None, 0, m, w.rows, w.cols), work, device, idx, stream,
                  (x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
     else:
         device, idx = w.codes.device, w.codes.get_device()
@@ -295,12 +285,9 @@ def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
         if k != w.cols:
             raise ValueError("x has %d columns, the weights %d" % (k, w.cols))
         dtype = _dtype(dtype, x.dtype if out is None else out.dtype)
-        out, p, ld, fresh = _out(out, "out", x.shape[:-1] + (w.rows,), dtype, device, idx)
-        _product(lib().fastrack_mx_linear, _LINEAR, (code, xp, xld, m, w.rows, k), work, device, idx, new, stream,
+        out, p, ld = _out(out, "out", x.shape[:-1] + (w.rows,), dtype, device, idx, stream)
+        _product(lib().fastrack_mx_linear, _LINEAR, (code, xp, xld, m, w.rows, k), work, device, idx, stream,
                  (code, xp, xld, w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
-    if fresh:
-        new.append(out)
-    _keep(new, stream, device)
     return out
 
 
@@ -308,17 +295,14 @@ def mx4_linear_grad_input(dy, w, dtype=None, out=None, work=None, stream=None):
     """dx = dy W, the gradient of mx4_linear with respect to x: dy (..., outputs) -> (..., inputs), in dy's type
     unless `dtype` says otherwise."""
     w = _mx(w, "w", MX4)
-    device, idx, new = w.codes.device, w.codes.get_device(), []
+    device, idx = w.codes.device, w.codes.get_device()
     yp, yld, m, n, code = _float(dy, "dy", idx)
     if n != w.rows:
         raise ValueError("dy has %d columns, the weights %d rows" % (n, w.rows))
     dtype = _dtype(dtype, dy.dtype if out is None else out.dtype)
-    out, p, ld, fresh = _out(out, "out", dy.shape[:-1] + (w.cols,), dtype, device, idx)
-    _product(lib().fastrack_mx_linear_grad_input, _GRAD_INPUT, (code, yp, yld, m, n, w.cols), work, device, idx, new, stream,
+    out, p, ld = _out(out, "out", dy.shape[:-1] + (w.cols,), dtype, device, idx, stream)
+    _product(lib().fastrack_mx_linear_grad_input, _GRAD_INPUT, (code, yp, yld, m, n, w.cols), work, device, idx, stream,
              (code, yp, yld, w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
-    if fresh:
-        new.append(out)
-    _keep(new, stream, device)
     return out
 
 
@@ -326,20 +310,17 @@ def mx8_weight_grad(dy, saved, dtype=None, out=None, accumulate=False, work=None
     """dW = dy^T x^ for a linear layer's kept input `saved`, an MX8 of (tokens, inputs): dy (..., outputs) ->
     (outputs, inputs), float32 unless `dtype` says otherwise. accumulate=True adds to `out` (float32)."""
     saved = _mx(saved, "saved", MX8)
-    device, idx, new = saved.codes.device, saved.codes.get_device(), []
+    device, idx = saved.codes.device, saved.codes.get_device()
     yp, yld, m, n, code = _float(dy, "dy", idx)
     if m != saved.rows:
         raise ValueError("dy has %d rows, the kept input %d" % (m, saved.rows))
     dtype = _dtype(dtype, _torch.float32 if out is None else out.dtype)
     if accumulate and (out is None or dtype != _torch.float32):
         raise ValueError("accumulate=True needs a float32 out to add to")
-    out, p, ld, fresh = _out(out, "out", (n, saved.cols), dtype, device, idx)
-    _product(lib().fastrack_mx_weight_grad, _WEIGHT_GRAD, (code, yp, yld, m, n, saved.cols), work, device, idx, new, stream,
+    out, p, ld = _out(out, "out", (n, saved.cols), dtype, device, idx, stream)
+    _product(lib().fastrack_mx_weight_grad, _WEIGHT_GRAD, (code, yp, yld, m, n, saved.cols), work, device, idx, stream,
              (code, yp, yld, saved.codes.data_ptr(), saved.scales.data_ptr()),
              (_TYPES[dtype], p, ld, 1 if accumulate else 0))
-    if fresh:
-        new.append(out)
-    _keep(new, stream, device)
     return out
 
 
@@ -348,7 +329,7 @@ def mx8_act(x, gate=None, act="silu", out=None, saved=None, saved_gate=None, str
     act is "silu" or "gelu" (with the error function). x and gate may be halves of one wider tensor."""
     a = _act(act)
     p, ld, rows, cols, code = _float(x, "x")
-    device, idx, new = x.device, x.get_device(), []
+    device, idx = x.device, x.get_device()
     gp, gld = None, 0
     if gate is not None:
         gp, gld, _, _, gcode = _float(gate, "gate", idx)
@@ -357,17 +338,14 @@ def mx8_act(x, gate=None, act="silu", out=None, saved=None, saved_gate=None, str
                              % (tuple(x.shape), x.dtype, tuple(gate.shape), gate.dtype))
     elif saved_gate is not None:
         raise ValueError("saved_gate without a gate")
-    out, yp, yld, fresh = _out(out, "out", x.shape, x.dtype, device, idx)
-    if fresh:
-        new.append(out)
-    saved = _new_mx(saved, "saved", MX8, rows, cols, device, idx, new)
+    out, yp, yld = _out(out, "out", x.shape, x.dtype, device, idx, stream)
+    saved = _new_mx(saved, "saved", MX8, rows, cols, device, idx, stream)
     if gate is not None:
-        saved_gate = _new_mx(saved_gate, "saved_gate", MX8, rows, cols, device, idx, new)
+        saved_gate = _new_mx(saved_gate, "saved_gate", MX8, rows, cols, device, idx, stream)
     if rows and cols:
         _call(lib().fastrack_mx_act, idx, a, code, p, ld, gp, gld, rows, cols, yp, yld, saved.codes.data_ptr(),
               saved.scales.data_ptr(), None if gate is None else saved_gate.codes.data_ptr(),
               None if gate is None else saved_gate.scales.data_ptr(), _raw_stream(stream, idx))
-    _keep(new, stream, device)
     return out, saved, saved_gate
 
 
@@ -375,25 +353,20 @@ def mx8_act_grad(dy, saved, saved_gate=None, act="silu", out=None, out_gate=None
     """(dx, dgate) of mx8_act from what it kept; dgate is None where there was no gate. Both in dy's type."""
     a = _act(act)
     saved = _mx(saved, "saved", MX8)
-    device, idx, new = saved.codes.device, saved.codes.get_device(), []
+    device, idx = saved.codes.device, saved.codes.get_device()
     p, ld, rows, cols, code = _float(dy, "dy", idx)
     if rows != saved.rows or cols != saved.cols:
         raise ValueError("dy is %d x %d, the kept x %d x %d" % (rows, cols, saved.rows, saved.cols))
-    out, xp, xld, fresh = _out(out, "out", dy.shape, dy.dtype, device, idx)
-    if fresh:
-        new.append(out)
+    out, xp, xld = _out(out, "out", dy.shape, dy.dtype, device, idx, stream)
     qg = gp = None
     gld = 0
     if saved_gate is not None:
         qg = _mx(saved_gate, "saved_gate", MX8, idx, rows, cols)
-        out_gate, gp, gld, fresh = _out(out_gate, "out_gate", dy.shape, dy.dtype, device, idx)
-        if fresh:
-            new.append(out_gate)
+        out_gate, gp, gld = _out(out_gate, "out_gate", dy.shape, dy.dtype, device, idx, stream)
     elif out_gate is not None:
         raise ValueError("out_gate without a saved gate")
     if rows and cols:
         _call(lib().fastrack_mx_act_grad, idx, a, code, p, ld, saved.codes.data_ptr(), saved.scales.data_ptr(),
               None if qg is None else qg.codes.data_ptr(), None if qg is None else qg.scales.data_ptr(), rows, cols, xp, xld,
               gp, gld, _raw_stream(stream, idx))
-    _keep(new, stream, device)
     return out, out_gate
