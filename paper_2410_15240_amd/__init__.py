@@ -227,34 +227,22 @@ def _stream_obj(s, device):
     return _torch.cuda.ExternalStream(_stream(s), device=device)
 
 
-def _used_on(tensors, streams, device):
-    """The binding allocated `tensors` on the current stream, and the library's work
-    on `streams` still reads or writes them after the call returns: tell the caching
-    allocator, so that freeing one does not hand its memory to a new allocation
-    while that work is in flight."""
-    cur = _torch.cuda.current_stream(device)
-    for s in streams:
-        so = _stream_obj(s, device)
-        if so.cuda_stream == cur.cuda_stream:
-            continue
-        for t in tensors:
-            if t is not None:
-                t.record_stream(so)
-
-
-def _fresh(shape, device, stream, dtype=_uint8):
-    """A new tensor that work enqueued on `stream` writes. Its memory is `stream`'s own: memory of the
-    caller's stream may just have been freed there, in that stream's order, by work that still uses it and
-    that nothing makes `stream` wait for. The caller's stream may use the tensor too once it is ordered
-    after `stream`."""
-    if stream is None:
+def _fresh(shape, device, stream, dtype=_uint8, later=()):
+    """A new tensor that work enqueued on `stream` uses first, and work on the streams `later` once it is ordered
+    after that. Its memory is `stream`'s own: memory of the caller's stream may just have been freed there, in
+    that stream's order, by work that still uses it and that nothing makes `stream` wait for. The caller's
+    stream may use the tensor too once it is ordered after `stream`."""
+    if stream is None and not later:
         return _torch.empty(shape, dtype=dtype, device=device)
     cur, so = _torch.cuda.current_stream(device), _stream_obj(stream, device)
     if so.cuda_stream == cur.cuda_stream:
-        return _torch.empty(shape, dtype=dtype, device=device)
-    with _torch.cuda.stream(so):
         t = _torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(cur)
+    else:
+        with _torch.cuda.stream(so):
+            t = _torch.empty(shape, dtype=dtype, device=device)
+    for s in (cur,) + tuple(_stream_obj(x, device) for x in later):
+        if s.cuda_stream != so.cuda_stream:
+            t.record_stream(s)
     return t
 
 
@@ -274,18 +262,13 @@ def decrypt_verify(key, base_iv, chain_bytes, ct, tags, aad=None, out=None, ok=N
     n = _chains(size, chain_bytes)
     tags_p = _dev_ptr(tags, "tags", 16 * n, idx, dev)
     aad_p, aad_bytes = _dev_aad(aad, n, idx, dev)
-    new = []
     if out is None:
-        out = _torch.empty_like(ct)
-        new.append(out)
+        out = _fresh(ct.shape, dev, stream)
     if ok is None:
-        ok = _torch.empty(n, dtype=_uint8, device=dev)
-        new.append(ok)
+        ok = _fresh(n, dev, stream)
     out_p, ok_p = _dev_ptr(out, "out", size, idx, dev), _dev_ptr(ok, "ok", n, idx, dev)
     _call(lib().fastrack_gcm_decrypt_verify, idx, _host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"),
           chain_bytes, ct.data_ptr(), size, tags_p, aad_p, aad_bytes, out_p, ok_p, flags, _raw_stream(stream, idx))
-    if new and stream is not None:
-        _used_on(new, [stream], dev)
     return out, ok
 
 
@@ -311,18 +294,13 @@ def encrypt_tag(key, base_iv, chain_bytes, pt, aad=None, out=None, tags=None, fl
     dev, idx, size = pt.device, pt.get_device(), pt.numel()
     n = _chains(size, chain_bytes)
     aad_p, aad_bytes = _dev_aad(aad, n, idx, dev)
-    new = []
     if out is None:
-        out = _torch.empty_like(pt)
-        new.append(out)
+        out = _fresh(pt.shape, dev, stream)
     if tags is None:
-        tags = _torch.empty((n, 16), dtype=_uint8, device=dev)
-        new.append(tags)
+        tags = _fresh((n, 16), dev, stream)
     out_p, tags_p = _dev_ptr(out, "out", size, idx, dev), _dev_ptr(tags, "tags", 16 * n, idx, dev)
     _call(lib().fastrack_gcm_encrypt_tag, idx, _host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"),
           chain_bytes, pt.data_ptr(), size, aad_p, aad_bytes, out_p, tags_p, flags, _raw_stream(stream, idx))
-    if new and stream is not None:
-        _used_on(new, [stream], dev)
     return out, tags
 
 
@@ -359,20 +337,16 @@ def decrypt_eager(key, base_iv, chain_bytes, ct, tags, aad=None, out=None, ok=No
     n = _chains(size, chain_bytes)
     tags_p = _dev_ptr(tags, "tags", 16 * n, idx, dev)
     aad_p, aad_bytes = _dev_aad(aad, n, idx, dev)
-    new = []
-    if out is None:
-        out = _torch.empty_like(ct)
-        new.append(out)
-    if ok is None:
-        ok = _torch.empty(n, dtype=_uint8, device=dev)
-        new.append(ok)
-    out_p, ok_p = _dev_ptr(out, "out", size, idx, dev), _dev_ptr(ok, "ok", n, idx, dev)
     vs = verify_stream if verify_stream is not None else decrypt_stream
+    later = () if vs is None else (vs,)   # (it starts after what the decrypt stream has queued)
+    if out is None:
+        out = _fresh(ct.shape, dev, decrypt_stream, later=later)
+    if ok is None:
+        ok = _fresh(n, dev, decrypt_stream, later=later)
+    out_p, ok_p = _dev_ptr(out, "out", size, idx, dev), _dev_ptr(ok, "ok", n, idx, dev)
     _call(lib().fastrack_gcm_decrypt_eager, idx, _host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"),
           chain_bytes, ct.data_ptr(), size, tags_p, aad_p, aad_bytes, out_p, ok_p, _raw_stream(decrypt_stream, idx),
           _raw_stream(vs, idx))
-    if new and vs is not None:
-        _used_on(new, [decrypt_stream, vs], dev)
     with _torch.cuda.device(dev):
         ev = _torch.cuda.Event()
         ev.record(_stream_obj(vs, dev))
@@ -382,18 +356,14 @@ def decrypt_eager(key, base_iv, chain_bytes, ct, tags, aad=None, out=None, ok=No
 def keystream(key, base_iv, chain_bytes, length, chain_base=0, out=None, stream=None, device=None, bitsliced=False):
     """The CTR keystream of chains chain_base.. covering `length` bytes (a uint8 CUDA tensor).
     bitsliced=True computes it with the bitsliced AES kernel instead of the T-table one."""
-    new = []
     if out is None:
         device = _torch.device("cuda", _torch.cuda.current_device()) if device is None else _torch.device(device)
-        out = _torch.empty(length, dtype=_uint8, device=device)
-        new.append(out)
+        out = _fresh(length, device, stream)
     _u8(out, "out", min_numel=length)
     idx = out.get_device()
     fn = lib().fastrack_gcm_keystream_bitsliced if bitsliced else lib().fastrack_gcm_keystream
     _call(fn, idx, _host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"), chain_bytes, chain_base, length,
           out.data_ptr(), _raw_stream(stream, idx))
-    if new and stream is not None:
-        _used_on(new, [stream], out.device)
     return out
 
 
@@ -412,20 +382,15 @@ def apply_verify(key, base_iv, chain_bytes, ct, ks, tags, aad=None, aad_bytes=No
     if chain_base + n > total:
         raise ValueError("tags hold %d chains, need %d" % (total, chain_base + n))
     aad_bytes = _aad_bytes(aad, total, aad_bytes=aad_bytes, device=dev)
-    new = []
     if out is None:
-        out = _torch.empty_like(ct)
-        new.append(out)
+        out = _fresh(ct.shape, dev, stream)
     if ok is None:
-        ok = _torch.empty(total, dtype=_uint8, device=dev)
-        new.append(ok)
+        ok = _fresh(total, dev, stream)
     out_p = _dev_ptr(out, "out", size, idx, dev)
     _u8(ok, "ok", min_numel=chain_base + n, device=dev)
     _call(lib().fastrack_gcm_apply_verify, idx, _host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"),
           chain_bytes, chain_base, ct.data_ptr(), size, ks.data_ptr(), tags.data_ptr(), _dptr(aad), aad_bytes, out_p,
           ok.data_ptr(), _raw_stream(stream, idx))
-    if new and stream is not None:
-        _used_on(new, [stream], dev)
     return out, ok
 
 
@@ -444,27 +409,23 @@ def pipeline_h2d(key, base_iv, chain_bytes, h_ct, h_tags, h_aad=None, chunk_byte
     _u8(h_tags, "h_tags", numel=16 * n, cuda=False)
     aad_bytes = _aad_bytes(h_aad, n, "h_aad", cuda=False)
     need = stage_bytes(length, chain_bytes, aad_bytes, chunk_bytes, depth)
-    new = []
+    vstream = verify_stream if verify_stream is not None else compute_stream
+    later = (compute_stream, vstream)   # (both start after the copy stream's first upload)
     if stage is None:
-        stage = _torch.empty(max(need, 1), dtype=_torch.uint8, device=device)
-        new.append(stage)
+        stage = _fresh(max(need, 1), device, copy_stream, later=later)
     if out is None:
-        out = _torch.empty(length, dtype=_torch.uint8, device=device)
-        new.append(out)
+        out = _fresh(length, device, copy_stream, later=later)
     if ok is None:
-        ok = _torch.empty(n, dtype=_torch.uint8, device=device)
-        new.append(ok)
+        ok = _fresh(n, device, copy_stream, later=later)
     _u8(stage, "stage", min_numel=need, device=device)
     _u8(out, "out", numel=length, device=device)
     _u8(ok, "ok", numel=n, device=device)
     with _torch.cuda.device(device):
-        vstream = verify_stream if verify_stream is not None else compute_stream
         _check(lib().fastrack_pipeline_h2d_mode(_host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"),
                                                 chain_bytes, h_ct.data_ptr(), length, h_tags.data_ptr(), _dptr(h_aad),
                                                 aad_bytes, chunk_bytes, depth, mode, _dptr(stage), stage.numel(),
                                                 _dptr(out), _dptr(ok), _stream(copy_stream), _stream(compute_stream),
                                                 _stream(vstream)))
-        _used_on(new, [copy_stream, compute_stream, vstream], device)
     return out, ok
 
 
@@ -478,13 +439,10 @@ def pipeline_d2h(key, base_iv, chain_bytes, pt, aad=None, chunk_bytes=8 << 20, o
     dev = pt.device
     n = num_chains(pt.numel(), chain_bytes)
     aad_bytes = _aad_bytes(aad, n, device=dev)
-    new = []
     if out is None and mode != PIPE_DIRECT:
-        out = _torch.empty_like(pt)
-        new.append(out)
+        out = _fresh(pt.shape, dev, compute_stream, later=(copy_stream,))
     if tags is None:
-        tags = _torch.empty((n, 16), dtype=_torch.uint8, device=dev)
-        new.append(tags)
+        tags = _fresh((n, 16), dev, compute_stream, later=(copy_stream,))
     if h_ct is None:
         h_ct = _torch.empty(pt.numel(), dtype=_torch.uint8, pin_memory=True)
     if h_tags is None:
@@ -500,7 +458,6 @@ def pipeline_d2h(key, base_iv, chain_bytes, pt, aad=None, chunk_bytes=8 << 20, o
                                                 chunk_bytes, _dptr(out), _dptr(tags), h_ct.data_ptr(),
                                                 h_tags.data_ptr(), _stream(copy_stream), _stream(compute_stream),
                                                 mode))
-        _used_on(new, [copy_stream, compute_stream], dev)
     return h_ct, h_tags
 
 
@@ -544,19 +501,14 @@ def decrypt_verify_ragged(key, base_iv, chain_off, chain_len, ct, tags, aad=None
     n = off.size
     tags_p = _dev_ptr(tags, "tags", 16 * n, idx, dev)
     aad_p, aad_bytes = _dev_aad(aad, n, idx, dev)
-    new = []
     if out is None:
-        out = _torch.empty_like(ct)
-        new.append(out)
+        out = _fresh(ct.shape, dev, stream)
     if ok is None:
-        ok = _torch.empty(n, dtype=_uint8, device=dev)
-        new.append(ok)
+        ok = _fresh(n, dev, stream)
     out_p, ok_p = _dev_ptr(out, "out", size, idx, dev), _dev_ptr(ok, "ok", n, idx, dev)
     _call(lib().fastrack_gcm_decrypt_verify_ragged, idx, _host_bytes(key, 32, "key"),
           _host_bytes(base_iv, 12, "base_iv"), off.ctypes.data, ln.ctypes.data, n, ct.data_ptr(), tags_p, aad_p,
           aad_bytes, out_p, ok_p, _raw_stream(stream, idx))
-    if new and stream is not None:
-        _used_on(new, [stream], dev)
     return out, ok
 
 
@@ -568,18 +520,13 @@ def encrypt_tag_ragged(key, base_iv, chain_off, chain_len, pt, aad=None, out=Non
     off, ln = _ragged_layout(chain_off, chain_len, size, "pt")
     n = off.size
     aad_p, aad_bytes = _dev_aad(aad, n, idx, dev)
-    new = []
     if out is None:
-        out = _torch.empty_like(pt)
-        new.append(out)
+        out = _fresh(pt.shape, dev, stream)
     if tags is None:
-        tags = _torch.empty((n, 16), dtype=_uint8, device=dev)
-        new.append(tags)
+        tags = _fresh((n, 16), dev, stream)
     out_p, tags_p = _dev_ptr(out, "out", size, idx, dev), _dev_ptr(tags, "tags", 16 * n, idx, dev)
     _call(lib().fastrack_gcm_encrypt_tag_ragged, idx, _host_bytes(key, 32, "key"), _host_bytes(base_iv, 12, "base_iv"),
           off.ctypes.data, ln.ctypes.data, n, pt.data_ptr(), aad_p, aad_bytes, out_p, tags_p, _raw_stream(stream, idx))
-    if new and stream is not None:
-        _used_on(new, [stream], dev)
     return out, tags
 
 
@@ -588,7 +535,7 @@ def clock_probe(window_us, n_probes=8, stream=None, device=None):
     for window_us of real time). Returns a uint64 tensor (n_probes, 2) of (shader
     cycles, 100 MHz ticks); read it once the stream is done (see clock_ghz)."""
     dev = _torch.device("cuda", _torch.cuda.current_device()) if device is None else _torch.device(device)
-    out = _torch.zeros((n_probes, 2), dtype=_torch.int64, device=dev)
+    out = _fresh((n_probes, 2), dev, stream, dtype=_torch.int64)   # (every probe writes both its words)
     with _torch.cuda.device(dev):
         _check(lib().fastrack_clock_probe(int(window_us), int(n_probes), out.data_ptr(), _stream(stream)))
     return out
