@@ -545,7 +545,9 @@ Plan plan_of(const MxProduct &p, int num_cu)
     // 6000 167 and 124.) A stage of a tile of 128 alone on its CU takes 0.4 us, 0.65 where the
     // operands are transposed, and the sum of each is cut where that pays.
     const uint64_t large = (m + 255) / 256 * ((n + 255) / 256);
-    const uint32_t tile = large > cu / 2 && stages >= 4 ? 256 : 128;
+    // (And where more tiles of 128 would be 2^32 threads, which no launch has.)
+    const uint64_t tiles128 = (m + 127) / 128 * ((n + 127) / 128);
+    const uint32_t tile = (large > cu / 2 && stages >= 4) || tiles128 * kThreads >= 1ull << 32 ? 256 : 128;
     const uint64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), sum = stages * (in_place ? 1 : terms);
     const double whole_us = (ta ? 0.65 : 0.4) * (double)sum;
     const uint64_t splits = tile == 256 ? 1 : cuts_of(whole_us, tiles, sum, m * n, cu);
@@ -573,6 +575,8 @@ Plan plan_of(const MxProduct &p, int num_cu)
     const uint64_t tiles64 = (m + 63) / 64 * ((n + 63) / 64), tiles32 = (m + 31) / 32 * ((n + 31) / 32);
     const bool by64 = tiles64 >= cu / 2 && p.type != kFp32;
     const uint64_t count = by64 ? tiles64 : tiles32, at_once = by64 ? cu : 2 * cu;
+    if (count * kSmallThreads >= 1ull << 32)   // as many threads as no launch has
+        return as_tiles;
     const double across = p.op == kWeightGrad ? 2.6 : mx_blocks(p.k) < 128 ? 1.5 : 2.6;
     const double slice = (p.op == kLinear ? (by64 ? 1.8 : 0.7) : by64 ? (p.op == kGradInput ? 2.2 : 3.0) : count <= 64 ? 1.0 : across) *
                          (p.type == kBf16 ? 1.0 : p.type == kFp16 ? 1.4 : p.op == kLinear ? 4.0 : 2.5);

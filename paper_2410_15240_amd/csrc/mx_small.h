@@ -23,6 +23,8 @@ struct SmallProduct {
     float *parts;            // [cuts][m][n] where cuts > 1
 };
 
+constexpr int kSmallThreads = 512;   // of a workgroup of launch_mx_small
+
 // linear alone, m up to 2 and k from 8.
 hipError_t launch_mx_dot(const SmallProduct &g, uint32_t type, hipStream_t s);
 // Tiles of side 32, or of 64 where a is not fp32 (its terms of 64 rows do not fit the registers);

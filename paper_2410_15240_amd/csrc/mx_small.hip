@@ -17,7 +17,7 @@
 namespace fastrack {
 namespace mx {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kThreads = kSmallThreads, kWaves = kThreads / 64;
 
 // Eight elements of a float operand as they lie in memory, and taken apart into bf16 terms.
 template <uint32_t T> struct Unit8 {
@@ -434,21 +434,24 @@ using namespace mx;
     } while (0)
 
 template <uint32_t T, int M>
-static void dot(const SmallProduct &g, hipStream_t s)
+static hipError_t dot(SmallProduct g, hipStream_t s)
 {
-    constexpr uint32_t R = dot_rows<T, M>();
-    hipLaunchKernelGGL((dot_kernel<T, M>), dim3((g.n + R - 1) / R), dim3(64 * kDotWaves), 0, s, g);
+    constexpr uint32_t R = dot_rows<T, M>(), kMost = R << 23;   // rows of w: a launch has fewer than 2^32 threads
+    for (uint32_t left = g.n;; left -= kMost) {
+        g.n = left < kMost ? left : kMost;
+        hipLaunchKernelGGL((dot_kernel<T, M>), dim3((g.n + R - 1) / R), dim3(64 * kDotWaves), 0, s, g);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || left <= kMost)
+            return e;
+        g.q.codes += (uint64_t)kMost * g.nb * 16;
+        g.q.scales += (uint64_t)kMost * g.nb;
+        g.out.p = reinterpret_cast<uint8_t *>(g.out.p) + (uint64_t)kMost * mx_type_size(g.out.type);
+    }
 }
 
 hipError_t launch_mx_dot(const SmallProduct &g, uint32_t type, hipStream_t s)
 {
-    MX_TYPE(type, {
-        if (g.m == 1)
-            dot<T, 1>(g, s);
-        else
-            dot<T, 2>(g, s);
-    });
-    return hipGetLastError();
+    MX_TYPE(type, return g.m == 1 ? dot<T, 1>(g, s) : dot<T, 2>(g, s));
 }
 
 template <uint32_t FMT, bool TA, bool TB>
