@@ -436,9 +436,11 @@ int fastrack_mx_act_grad(uint32_t act, uint32_t type, const void *d_dy, uint64_t
  *   weight_grad        dw[n][k] = sum over m of dy[m][n] x^[m][k], added to what d_dw
  *                      holds where accumulate is 1 (32-bit d_dw only)
  *   linear_mx          linear with x in MX4 as well
- * Every MX value is exact in bf16, and the products of the float operand's bf16
- * terms (1 for bf16, 2 for fp16, 3 for fp32) with it are exact: what is rounded is
- * the 32-bit sum.
+ * Every MX value is exact in bf16, the float operand is taken as bf16 terms (1 for
+ * bf16, 2 for fp16, 3 for fp32), and their products are exact: what is rounded is
+ * the 32-bit sum. The terms add up to the value, but bf16 ends at 2^-133: bits of a
+ * 32-bit value below that may be dropped, which values from 2^-110 up do not have.
+ * (linear of one or two tokens and 512 inputs or more keeps them.)
  * d_work: fastrack_mx_work_bytes(...) bytes, 16-byte aligned (NULL if that is 0);
  * it depends on the float operand's address and stride (an operand that is not
  * bf16 in whole 16-byte pieces is laid out there first) and on the device.

@@ -194,7 +194,8 @@ __device__ __forceinline__ u32x2 encode8(const float (&v)[8], uint32_t e)
 }
 
 // The upper halves of eight floats: bf16 values cut, not rounded, so that what is left of each
-// (left: v becomes it) has 8 significant bits less and the terms add up exactly.
+// (left: v becomes it) has 8 significant bits less and the terms add up to the value, down to
+// bf16's smallest, 2^-133.
 __device__ __forceinline__ u32x4 upper_halves(const float (&v)[8])
 {
     u32x4 h;

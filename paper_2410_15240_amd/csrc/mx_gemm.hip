@@ -4,6 +4,9 @@
 // a bf16 matrix with an MX one is a bf16 product with 32-bit sums and no rounding of its own.
 // A 16-bit float with more significant bits, or a 32-bit one, is the exact sum of 2 or 3 bf16
 // terms: its product is the sum of the terms' products, which the kernels run as a longer sum.
+// (But for bits of a 32-bit float below bf16's smallest value, 2^-133, which are cut: floats
+// below 2^-110 have them. Terms scaled up into range cost a sixth of the time, for bits that only
+// MX scales near the top of theirs would show.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -418,7 +421,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float *parts, uint
 
 // The bf16 terms of a float matrix, rows padded with zeros to ld (a multiple of 8): each term
 // is what is left cut to its upper 16 bits, so that 3 terms of 8 significant bits (2 for
-// 11 bits) add up to the value exactly.
+// 11 bits) add up to the value, down to its bit of 2^-133.
 struct Terms {
     MxRows a;
     uint64_t row0;
