@@ -442,8 +442,11 @@ int fastrack_mx_act_grad(uint32_t act, uint32_t type, const void *d_dy, uint64_t
  * 32-bit value below that may be dropped, which values from 2^-110 up do not have.
  * (linear of one or two tokens and 512 inputs or more keeps them.)
  * d_work: fastrack_mx_work_bytes(...) bytes, 16-byte aligned (NULL if that is 0);
- * it depends on the float operand's address and stride (an operand that is not
- * bf16 in whole 16-byte pieces is laid out there first) and on the device.
+ * it depends on the float operand's address and stride and on the device. With many
+ * outputs bf16 is read in place at any multiple of 4 bytes with an even row stride
+ * (weight_grad: of rows of whole 8 values); any other operand is laid out there
+ * first. With few, every operand is read in place. Parts of long sums lie there too,
+ * and weight_grad's input decoded where many tiles would decode it again.
  * EINVAL as for quantize; a workspace too small; more than 2^24 output tiles of
  * 128 x 128.
  */
