@@ -379,7 +379,10 @@ int fastrack_clock_probe(uint64_t window_us, uint32_t n_probes, uint64_t *d_out,
  *   FASTRACK_MX8  32 bytes a block: int8 q, worth q / 64
  * Codes are [rows][blocks][16 or 32] bytes, 16-byte aligned; scales are
  * [rows][blocks] bytes of any alignment. The codes of a row past `cols` are zero
- * (the quantizer writes them so; other sources of codes must too).
+ * (the quantizer writes them so; other sources of codes must too). MX4 values of
+ * 2^128 and more, which only scale bytes 253 and 254 can say and the quantizer never
+ * writes, decode to infinities, and sums with them are infinite or NaN; linear_mx
+ * alone multiplies with them as they are.
  *
  * Float matrices are given as an address, an element type and a row stride `ld`
  * in elements, with neighbouring elements of a row side by side; any alignment of
@@ -408,8 +411,8 @@ uint64_t fastrack_mx_scale_bytes(uint64_t rows, uint64_t cols);
 int fastrack_mx_quantize(uint32_t format, uint32_t type, const void *d_x, uint64_t ldx, uint64_t rows, uint64_t cols,
                          uint8_t *d_codes, uint8_t *d_scales, void *stream);
 
-/* The values that the codes stand for (exact in bf16 and fp32; in fp16 rounded,
- * past its range infinite). EINVAL as for quantize. */
+/* The values that the codes stand for (exact in bf16 and fp32, but see above; in
+ * fp16 rounded, past its range infinite). EINVAL as for quantize. */
 int fastrack_mx_dequantize(uint32_t format, const uint8_t *d_codes, const uint8_t *d_scales, uint64_t rows,
                            uint64_t cols, uint32_t type, void *d_out, uint64_t ld_out, void *stream);
 
@@ -436,7 +439,7 @@ int fastrack_mx_act_grad(uint32_t act, uint32_t type, const void *d_dy, uint64_t
  *   weight_grad        dw[n][k] = sum over m of dy[m][n] x^[m][k], added to what d_dw
  *                      holds where accumulate is 1 (32-bit d_dw only)
  *   linear_mx          linear with x in MX4 as well
- * Every MX value is exact in bf16, the float operand is taken as bf16 terms (1 for
+ * Every finite MX value is exact in bf16, the float operand is taken as bf16 terms (1 for
  * bf16, 2 for fp16, 3 for fp32), and their products are exact: what is rounded is
  * the 32-bit sum. The terms add up to the value, but bf16 ends at 2^-133: bits of a
  * 32-bit value below that may be dropped, which values from 2^-110 up do not have.

@@ -74,3 +74,26 @@ def test_the_largest_beside_the_smallest(m, n, k):
     q = F.MX4(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), k)
     got = F.mx4_linear(torch.from_numpy(a.astype(np.float32)).cuda(), q).cpu().double().numpy()
     assert (got[0] == big).all() and (m == 1 or (got[1] == np.inf).all())
+
+
+@pytest.mark.parametrize("e", [252, 253, 254])
+@pytest.mark.parametrize("m", [1, 3, 200])
+def test_weights_at_the_top_of_the_scales(m, e):
+    """Every code at the largest scales, against inputs of 2^-60 everywhere: values of 2^128 and more are infinite, but
+    in the product of two MX4 matrices."""
+    n, k = 16, 512
+    codes = np.arange(n, dtype=np.uint8)[:, None] * np.full((1, k // 2), 17, np.uint8)
+    scales = np.full((n, k // 32), e, np.uint8)
+    v = O.values(codes, scales, k)
+    w = F.MX4(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), k)
+    x = torch.full((m, k), 2.0 ** -60, device="cuda")
+    want, past = (v * 2.0 ** -60).sum(axis=1), np.abs(v[:, 0]) >= 2.0 ** 128
+    assert past.any() == (e > 252)
+    for row in F.mx4_linear(F.mx4_quantize(x), w, dtype=torch.float32).cpu().double().numpy():
+        assert np.array_equal(row, want)
+    for dt in (torch.bfloat16, torch.float16, torch.float32):
+        x = torch.full((m, k), 2.0 ** -24, device="cuda", dtype=dt)
+        for row in F.mx4_linear(x, w, dtype=torch.float32).cpu().double().numpy():
+            assert np.array_equal(row[~past], want[~past] * 2.0 ** 36) and not np.isfinite(row[past]).any()
+    got = F.mx4_dequantize(w, dtype=torch.float32).cpu().double().numpy()
+    assert np.array_equal(got[~past], v[~past]) and np.array_equal(got[past], np.copysign(np.inf, v[past]))
