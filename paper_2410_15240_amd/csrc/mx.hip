@@ -92,6 +92,27 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(Shape sh, MxMatrix
     store8<T>(out.p, u.row * out.ld, u.c, sh.cols, v);
 }
 
+// The normal distribution above a >= 0, over e^(-a^2 / 2): a polynomial in t = 1 / (1 + c a) without a
+// constant term, fitted for the least relative error over [0, 14.6] (2^-20.6 with 7 coefficients, 2^-28.5
+// with 10). P of a negative x is that product and keeps its digits, where 1 + erf of it has none left
+// from x = -5.5 down. (4096 x 16384 of bf16 with a gate: 97 us forwards and 101 backwards, with the
+// library's erff 110 and 107, with its erfcf 133 and 137.)
+template <bool FAST>
+__device__ __forceinline__ float normal_tail(float a)
+{
+    constexpr int N = FAST ? 7 : 10;
+    constexpr float c[10] = {FAST ? 0.105599828f : 0.0937371254f,   FAST ? 0.107836783f : 0.0940763354f,
+                             FAST ? 0.0829465464f : 0.0853466466f,  FAST ? 0.142493442f : 0.0966654718f,
+                             FAST ? -0.0663630813f : -0.00348356646f, FAST ? 0.195273235f : 0.207300872f,
+                             FAST ? -0.0677870661f : -0.227627978f, 0.273647487f, -0.147487491f, 0.0278251003f};
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, FAST ? 0.265f : 0.235f, 1.0f));
+    float p = c[N - 1];
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i)
+        p = __builtin_fmaf(p, t, c[i]);
+    return p * t;
+}
+
 // f and f' of the activation. FAST (16-bit types, whose own rounding is 2^-9 or 2^-12): the
 // hardware's exponential and reciprocal, a few 2^-23 each.
 template <uint32_t ACT, bool FAST>
@@ -103,10 +124,18 @@ __device__ __forceinline__ void act_of(float x, float &f, float &df)
         f = x * s;
         df = s * (1.0f + x * (1.0f - s));
     } else {              // x P(x), P + x p(x); P the normal distribution, p its density
-        const float P = 0.5f * (1.0f + erff(x * 0.70710678f));
-        const float t = -0.5f * x * x;
+        const float a = fminf(__builtin_fabsf(x), 20.0f);   // (past which e is 0; a NaN goes on in x)
+        float e;
+        if (FAST) {
+            e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
+        } else {   // what the square's rounding leaves counts as much as its size
+            const float sq = a * a;
+            e = expf(-0.5f * sq);
+            e = __builtin_fmaf(-0.5f * e, __builtin_fmaf(a, a, -sq), e);
+        }
+        const float q = e * normal_tail<FAST>(a), P = x < 0.0f ? q : 1.0f - q;
         f = x * P;
-        df = P + x * ((FAST ? __expf(t) : expf(t)) * 0.39894228f);
+        df = P + x * (e * 0.39894228f);
     }
 }
 
