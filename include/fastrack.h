@@ -420,6 +420,9 @@ int fastrack_mx_dequantize(uint32_t format, const uint8_t *d_codes, const uint8_
  * An activation that keeps what its gradient needs in 8 bits, in one pass:
  *   y = f(x), or f(x) * gate where d_gate is not NULL; x (and gate) quantized to MX8
  * with f(x) = x / (1 + e^-x) (SILU) or x P(x), P the normal distribution (GELU).
+ * Both are right relative to the value, in 32 bits to 2^-20 of it, in 16-bit types
+ * before their rounding to 2^-15; SILU is 0 from where 1 + e^-x passes 2^126 down
+ * (x about -87.3, |f| below 2^-119; in 32 bits 2^128, x about -88.7).
  * The gradients are taken at the kept values x^ and gate^:
  *   dx = dy * gate^ * f'(x^),  dgate = dy * f(x^)    (no gate: d_gcodes NULL, dx = dy * f'(x^))
  * EINVAL as for quantize, and an unknown activation.

@@ -3,7 +3,10 @@
 Bounds. GELU in 32 bits: the fit of the tail (2^-28), its evaluation (3 roundings of t, 10 of the polynomial, whose terms
 are at most 14 times their sum: its leading ones, where t is small, about the sum itself), the exponential and three
 products, together below 16 units of 2^-24. In 16-bit types the exponential's argument, x^2 / 2, is rounded twice (its
-constant is off by a quarter of a unit, for which 2^-18 leaves room), and the fit is 2^-20.
+constant is off by a quarter of a unit, for which 2^-18 leaves room), and the fit is 2^-20. SiLU in 16-bit types: the
+argument is -x, times a rounded constant: 2 units of |x|, and the exponential's and the reciprocal's own unit or two.
+In 32 bits: an exponential, a sum, a division and a product, 1 unit each or 2; and where s is small the gradient's
+rest, 1 - s, is right to a unit of 1, times x.
 """
 import numpy as np
 import pytest
@@ -30,10 +33,12 @@ def check_between(got, want, bound):
 
 
 def relative(kind, name, x):
-    return 2.0 ** -20 if name == "fp32" else 2.0 ** -18 + x * x * 2.0 ** -24
+    if name == "fp32":
+        return np.full(x.shape, 2.0 ** -20)
+    return 2.0 ** -18 + (x * x * 2.0 ** -24 if kind == "gelu" else np.abs(x) * 2.0 ** -23)
 
 
-@pytest.mark.parametrize("kind,low", [("gelu", -13.0)])
+@pytest.mark.parametrize("kind,low", [("gelu", -13.0), ("silu", -87.0)])
 @pytest.mark.parametrize("name", list(TYPES))
 @pytest.mark.parametrize("gated", [False, True])
 def test_the_negative_end_is_right_relative_to_itself(kind, low, name, gated):
@@ -51,7 +56,7 @@ def test_the_negative_end_is_right_relative_to_itself(kind, low, name, gated):
     f, df = O.act(kept, kind)
     # f' has a zero here: its two terms are s or P and the rest
     first = f / kept
-    size = np.abs(first) + np.abs(df - first)
+    size = np.abs(first) * (1 + np.abs(kept)) if kind == "silu" else np.abs(first) + np.abs(df - first)
     check_between(dx, df * by, size * by * 2 * relative(kind, name, kept))
     if gated:
         check_between(dg, f, np.abs(f) * relative(kind, name, kept))
