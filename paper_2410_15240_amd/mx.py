@@ -5,8 +5,12 @@ The format, the rounding and the sums are documented in include/fastrack.h. A fl
 in bfloat16, float16 or float32 whose last axis is dense; the axes before it are taken together as its rows, which
 may be any equal distance apart (a slice of a wider tensor, or one row expanded). Work is enqueued on the current
 stream or on `stream`, which waits for nothing on the current one: order it after what it reads, and whoever reads the
-results after it. New results may be used on either. A float tensor's NaN and infinity
-go where the formulas put them; in a quantised block they make the whole block NaN.
+results after it. New results may be used on either. A float tensor's NaN and infinity go where the formulas put
+them; in a quantised block they make the whole block NaN.
+
+Nothing here is recorded by autograd: a result needs no gradient, whatever its operands do, and a `backward()` ends at it.
+Training calls the gradients by name (mx4_linear_grad_input, mx8_weight_grad, mx8_act_grad), in the backward of a
+torch.autograd.Function of its own or, as examples/offloaded_layer.py does, in order.
 """
 import ctypes as _ct
 
