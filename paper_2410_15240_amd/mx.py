@@ -189,8 +189,10 @@ def _mx(q, what, cls, idx=None, rows=None, cols=None):
     return q
 
 
-def _dtype(dtype, default):
-    dtype = default if dtype is None else dtype
+def _dtype(dtype, out, default):
+    """The type that a call's result is to have: asked for, or that of the output given, or the call's own."""
+    if dtype is None:
+        dtype = out.dtype if isinstance(out, _Tensor) else default
     if dtype not in _TYPES:
         raise ValueError("dtype must be bfloat16, float16 or float32, got %s" % dtype)
     return dtype
@@ -220,7 +222,7 @@ def _quantize(cls, x, out, stream):
 def _dequantize(cls, q, dtype, out, stream):
     _mx(q, "q", cls)
     device, idx = q.codes.device, q.codes.get_device()
-    dtype = _dtype(dtype, _torch.bfloat16 if out is None else out.dtype)
+    dtype = _dtype(dtype, out, _torch.bfloat16)
     out, p, ld = _out(out, "out", (q.rows, q.cols), dtype, device, idx, stream)
     _call(lib().fastrack_mx_dequantize, idx, cls.format, q.codes.data_ptr(), q.scales.data_ptr(), q.rows, q.cols, _TYPES[dtype],
           p, ld, _raw_stream(stream, idx))
@@ -279,7 +281,7 @@ def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
     if isinstance(x, _MX):
         _mx(x, "x", MX4, w.codes.get_device(), cols=w.cols)
         device, idx, m = w.codes.device, w.codes.get_device(), x.rows
-        dtype = _dtype(dtype, _torch.bfloat16 if out is None else out.dtype)
+        dtype = _dtype(dtype, out, _torch.bfloat16)
         out, p, ld = _out(out, "out", (m, w.rows), dtype, device, idx, stream)
         _product(lib().fastrack_mx_linear_mx, _LINEAR_MX, (0, None, 0, m, w.rows, w.cols), work, device, idx, stream,
                  (x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
@@ -288,7 +290,7 @@ def mx4_linear(x, w, dtype=None, out=None, work=None, stream=None):
         xp, xld, m, k, code = _float(x, "x", idx)
         if k != w.cols:
             raise ValueError("x has %d columns, the weights %d" % (k, w.cols))
-        dtype = _dtype(dtype, x.dtype if out is None else out.dtype)
+        dtype = _dtype(dtype, out, x.dtype)
         out, p, ld = _out(out, "out", x.shape[:-1] + (w.rows,), dtype, device, idx, stream)
         _product(lib().fastrack_mx_linear, _LINEAR, (code, xp, xld, m, w.rows, k), work, device, idx, stream,
                  (code, xp, xld, w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
@@ -303,7 +305,7 @@ def mx4_linear_grad_input(dy, w, dtype=None, out=None, work=None, stream=None):
     yp, yld, m, n, code = _float(dy, "dy", idx)
     if n != w.rows:
         raise ValueError("dy has %d columns, the weights %d rows" % (n, w.rows))
-    dtype = _dtype(dtype, dy.dtype if out is None else out.dtype)
+    dtype = _dtype(dtype, out, dy.dtype)
     out, p, ld = _out(out, "out", dy.shape[:-1] + (w.cols,), dtype, device, idx, stream)
     _product(lib().fastrack_mx_linear_grad_input, _GRAD_INPUT, (code, yp, yld, m, n, w.cols), work, device, idx, stream,
              (code, yp, yld, w.codes.data_ptr(), w.scales.data_ptr()), (_TYPES[dtype], p, ld))
@@ -318,7 +320,7 @@ def mx8_weight_grad(dy, saved, dtype=None, out=None, accumulate=False, work=None
     yp, yld, m, n, code = _float(dy, "dy", idx)
     if m != saved.rows:
         raise ValueError("dy has %d rows, the kept input %d" % (m, saved.rows))
-    dtype = _dtype(dtype, _torch.float32 if out is None else out.dtype)
+    dtype = _dtype(dtype, out, _torch.float32)
     if accumulate and (out is None or dtype != _torch.float32):
         raise ValueError("accumulate=True needs a float32 out to add to")
     out, p, ld = _out(out, "out", (n, saved.cols), dtype, device, idx, stream)

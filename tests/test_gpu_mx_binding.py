@@ -38,3 +38,14 @@ def test_a_function_of_the_callers_joins_them():
     Linear.apply(x, w).backward(dy)
     q, k = F.mx4_quantize(w), F.mx8_quantize(x)
     assert torch.equal(x.grad, F.mx4_linear_grad_input(dy, q)) and torch.equal(w.grad, F.mx8_weight_grad(dy, k))
+
+
+@pytest.mark.parametrize("out", [[1.0], "out", 3])
+def test_an_output_that_is_no_tensor_is_refused(out):
+    x, dy = torch.zeros(4, 64, device="cuda"), torch.zeros(4, 10, device="cuda")
+    w, k = F.mx4_quantize(torch.zeros(10, 64, device="cuda")), F.mx8_quantize(x)
+    for call in (lambda: F.mx4_dequantize(w, out=out), lambda: F.mx8_dequantize(k, out=out), lambda: F.mx4_linear(x, w, out=out),
+                 lambda: F.mx4_linear(F.mx4_quantize(x), w, out=out), lambda: F.mx4_linear_grad_input(dy, w, out=out),
+                 lambda: F.mx8_weight_grad(dy, k, out=out), lambda: F.mx8_act(x, out=out), lambda: F.mx8_act_grad(x, k, out=out)):
+        with pytest.raises(ValueError, match="out must be a torch tensor"):
+            call()
