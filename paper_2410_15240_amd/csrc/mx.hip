@@ -209,13 +209,7 @@ hipError_t over_rows(uint64_t rows, uint64_t cols, F launch)
 
 using namespace mx;
 
-// Run-time choices as template arguments.
-#define MX_TYPE(t, ...)                                                                            \
-    do {                                                                                           \
-        if ((t) == kBf16) { constexpr uint32_t T = kBf16; __VA_ARGS__; }                           \
-        else if ((t) == kFp16) { constexpr uint32_t T = kFp16; __VA_ARGS__; }                      \
-        else { constexpr uint32_t T = kFp32; __VA_ARGS__; }                                        \
-    } while (0)
+// A run-time choice as a template argument.
 #define MX_BOOL(name, v, ...)                                                                      \
     do {                                                                                           \
         if (v) { constexpr bool name = true; __VA_ARGS__; }                                        \

@@ -25,6 +25,14 @@ template <> struct Elem<kBf16> { typedef __bf16 type; };
 template <> struct Elem<kFp16> { typedef _Float16 type; };
 template <> struct Elem<kFp32> { typedef float type; };
 
+// A run-time MxType as the constant T of what follows.
+#define MX_TYPE(t, ...)                                                                            \
+    do {                                                                                           \
+        if ((t) == kBf16) { constexpr uint32_t T = kBf16; __VA_ARGS__; }                           \
+        else if ((t) == kFp16) { constexpr uint32_t T = kFp16; __VA_ARGS__; }                      \
+        else { constexpr uint32_t T = kFp32; __VA_ARGS__; }                                        \
+    } while (0)
+
 // Elements [c, c + 8) of a row as floats, zero past `cols`. A whole unit is loaded 16 bytes at a
 // time wherever it starts: the hardware takes any alignment.
 template <uint32_t T>

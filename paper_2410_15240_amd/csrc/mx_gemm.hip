@@ -58,34 +58,34 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
     n = j / rows;
 }
 
-// A workgroup's results, 2 x 2 waves of MI x NJ squares of 32: lane l of a wave holds column
+// A workgroup's results, 2 x 2 waves of N x N squares of 32: lane l of a wave holds column
 // l % 32 of rows 8 (r / 4) + 4 (l / 32) + r % 4 of each. They pass through LDS, 64 rows at a
 // time, so that c is written in whole rows of the tile. Rows whose bit 2 is set are turned by
 // 32 columns: the two halves of a wave then write to different banks.
-template <int WN, int MI, int NJ>
-__device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds, uint32_t m0, uint32_t n0, uint32_t m,
+template <int N>
+__device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t m,
                                          uint32_t n, const Out &o)
 {
-    constexpr uint32_t BN = 32 * WN * NJ, TH = 128 * WN;
+    constexpr uint32_t B = 64 * N;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
+    for (int i = 0; i < N; ++i) {
         if (i)
             __syncthreads();
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const uint32_t y = wave / WN * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-                const uint32_t x = wave % WN * 32 * NJ + j * 32 + (lane & 31);
-                lds[y * BN + (x ^ ((y & 4) << 3))] = acc[i][j][r];
+                const uint32_t y = wave / 2 * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
+                const uint32_t x = wave % 2 * 32 * N + j * 32 + (lane & 31);
+                lds[y * B + (x ^ ((y & 4) << 3))] = acc[i][j][r];
             }
         __syncthreads();
 #pragma unroll 2
-        for (uint32_t u = t; u < 64 * BN / 8; u += TH) {
-            const uint32_t y = u / (BN / 8), x = u % (BN / 8) * 8;
-            const uint32_t row = m0 + (y >> 5) * 32 * MI + i * 32 + (y & 31), col = n0 + x;
-            const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * BN + (x ^ ((y & 4) << 3)));
+        for (uint32_t u = t; u < 64 * B / 8; u += kThreads) {
+            const uint32_t y = u / (B / 8), x = u % (B / 8) * 8;
+            const uint32_t row = m0 + (y >> 5) * 32 * N + i * 32 + (y & 31), col = n0 + x;
+            const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
             const f32x4 lo = p[0], hi = p[1];
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if (row < m && col < n)
@@ -94,7 +94,7 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds
     }
 }
 
-// One tile of c, or of one part of it, by 2 x WN waves of 32 MI x 32 NJ outputs each. TA: a is
+// One tile of c, or of one part of it, by 2 x 2 waves of 32 N x 32 N outputs each. TA: a is
 // summed over its rows (a[k][m]) instead of along them (a[m][k]); TB: the same of the MX
 // matrix. While a stage of 64 summed values is multiplied out of one half of the LDS, the next
 // one is decoded from registers to bf16 in the other half, and the one after is on its way
@@ -115,56 +115,56 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[MI][NJ], float *lds
 // A whole stage is read without a check: rows and columns past the matrices' ends read the
 // last ones again, for results that are not stored. (Rows so long that a tile spans 2^32
 // bytes have no such stages; all of theirs are checked.)
-template <uint32_t FMT, bool TA, bool TB, int WN, int MI, int NJ>
-__global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gemm g)
+template <uint32_t FMT, bool TA, bool TB, int N>
+__global__ __launch_bounds__(kThreads, N > 2 ? 1 : 2) void gemm_kernel(Gemm g)
 {
-    constexpr int BM = 64 * MI, BN = 32 * WN * NJ, TH = 128 * WN, UA = BM * 8 / TH, UB = BN * 8 / TH;
+    constexpr int B = 64 * N, U = B * 8 / kThreads;   // outputs a side; units of 8 values that a thread copies of each operand
     constexpr uint32_t CB = FMT == kMx4 ? 4 : FMT == kMx8 ? 8 : 16;   // bytes of 8 codes, or bf16 values
     typedef uint32_t Codes __attribute__((ext_vector_type(FMT == kDecoded ? 4 : 2)));
     // Two stages: both tiles of a, then both of the MX matrix, so that a lane's offsets within
     // either are a register and a constant of 16 bits.
-    constexpr uint32_t kA = BM * kBK * 2, kB = BN * kBK * 2;
-    __shared__ __align__(16) uint8_t lds[2 * (kA + kB)];
+    constexpr uint32_t kTile = B * kBK * 2;
+    __shared__ __align__(16) uint8_t lds[4 * kTile];
     const uint32_t t = threadIdx.x;
     const uint32_t lane = t & 63, wave = t >> 6;
     const uint32_t tiles = g.tm * g.tn, part = blockIdx.x / tiles;
     uint32_t tile_m, tile_n;
     tile_of(blockIdx.x - part * tiles, g.tm, g.tn, tile_m, tile_n);
-    const uint32_t m0 = tile_m * BM, n0 = tile_n * BN;
-    const uint32_t wm = wave / WN * 32 * MI, wn = wave % WN * 32 * NJ;
+    const uint32_t m0 = tile_m * B, n0 = tile_n * B;
+    const uint32_t wm = wave / 2 * 32 * N, wn = wave % 2 * 32 * N;
     const uint32_t s_begin = part * g.per, s_end = min(g.stages, s_begin + g.per);
     const uint32_t full = g.whole, nfull = full * g.planes;   // whole stages of a term, of all
 
-    f32x16 acc[MI][NJ] = {};
-    u32x4 ra[UA];
-    Codes rb[UB];
-    uint8_t re[UB];
+    f32x16 acc[N][N] = {};
+    u32x4 ra[U];
+    Codes rb[U];
+    uint8_t re[U];
 
     // Offsets in the LDS: of the reads (see frag_k_at, frag_t_at), and of this thread's writes.
     uint32_t fa_at[4], fb_at[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        fa_at[i] = TA ? frag_t_at<BM>(wm + i % MI * 32, lane) : frag_k_at(wm, i, lane);
-        fb_at[i] = 2 * kA + (TB ? frag_t_at<BN>(wn + i % NJ * 32, lane) : frag_k_at(wn, i, lane));
+        fa_at[i] = TA ? frag_t_at<B>(wm + i % N * 32, lane) : frag_k_at(wm, i, lane);
+        fb_at[i] = 2 * kTile + (TB ? frag_t_at<B>(wn + i % N * 32, lane) : frag_k_at(wn, i, lane));
     }
-    const uint32_t wa_at = TA ? at_t<BM>(t / (BM / 8), t % (BM / 8) * 8) : at_k(t / 8, t % 8);
-    const uint32_t wb_at = 2 * kA + (TB ? at_t<BN>(t / (BN / 8), t % (BN / 8) * 8) : at_k(t / 8, t % 8));
+    const uint32_t wa_at = TA ? at_t<B>(t / (B / 8), t % (B / 8) * 8) : at_k(t / 8, t % 8);
+    const uint32_t wb_at = 2 * kTile + (TB ? at_t<B>(t / (B / 8), t % (B / 8) * 8) : at_k(t / 8, t % 8));
 
     // A whole stage: one address for the workgroup and 32-bit offsets of the lanes, in bytes.
-    uint32_t oa[UA], ob[UB], oe[UB];
+    uint32_t oa[U], ob[U], oe[U];
 #pragma unroll
-    for (int i = 0; i < UA; ++i) {
-        const uint32_t u = i * TH + t;
+    for (int i = 0; i < U; ++i) {
+        const uint32_t u = i * kThreads + t;
         if (TA)
-            oa[i] = u / (BM / 8) * (uint32_t)g.lda * 2 + min(u % (BM / 8) * 8, (g.m - 1 - m0) & ~7u) * 2;
+            oa[i] = u / (B / 8) * (uint32_t)g.lda * 2 + min(u % (B / 8) * 8, (g.m - 1 - m0) & ~7u) * 2;
         else
             oa[i] = min(u / 8, g.m - 1 - m0) * (uint32_t)g.lda * 2 + u % 8 * 16;
     }
 #pragma unroll
-    for (int i = 0; i < UB; ++i) {
-        const uint32_t u = i * TH + t;
-        const uint32_t row = TB ? u / (BN / 8) : min(u / 8, g.n - 1 - n0);
-        const uint32_t unit = TB ? min(u % (BN / 8), (g.nb - n0 / 32) * 4 - 1) : u % 8;
+    for (int i = 0; i < U; ++i) {
+        const uint32_t u = i * kThreads + t;
+        const uint32_t row = TB ? u / (B / 8) : min(u / 8, g.n - 1 - n0);
+        const uint32_t unit = TB ? min(u % (B / 8), (g.nb - n0 / 32) * 4 - 1) : u % 8;
         ob[i] = row * g.nb * (4 * CB) + unit * CB;
         oe[i] = row * g.nb + unit / 4;
     }
@@ -205,16 +205,15 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
         re[i] = __builtin_amdgcn_raw_buffer_load_b8(buffer_at(ps), oe[i], 0, 0);
     };
     // The next stage's way from registers to the LDS, in small items, and its registers' next
-    // load: per group one or two units of the MX matrix (the scale, then the codes in pairs or
-    // all of E2M1's, then the write) and as many of a.
-    constexpr int kPieces = FMT == kDecoded ? 1 : FMT == kMx4 ? 2 : 6, kGroup = UB / (UB < UA ? UB : UA) * kPieces + 1, kItems = kGroup * UA;
-    static_assert(UA == UB, "groups of one unit each");
+    // load: per group a unit of the MX matrix (the scale, then the codes in pairs or all of
+    // E2M1's, then the write) and one of a.
+    constexpr int kPieces = FMT == kDecoded ? 1 : FMT == kMx4 ? 2 : 6, kGroup = kPieces + 1, kItems = kGroup * U;
     float scale;
     u32x4 dec;
     auto item = [&](uint32_t half, int y, bool again) {
         const int i = y / kGroup, p = y % kGroup;
         if (p == kGroup - 1) {
-            *reinterpret_cast<u32x4 *>(lds + wa_at + half * kA + i * TH * 16) = ra[i];
+            *reinterpret_cast<u32x4 *>(lds + wa_at + half * kTile + i * kThreads * 16) = ra[i];
             if (again)
                 load_a(i);
             return;
@@ -228,7 +227,7 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
                 dec = rb[i];
             if (FMT == kMx4)
                 dec = decode4_bf16(rb[i][0], scale);
-            *reinterpret_cast<u32x4 *>(lds + wb_at + half * kB + i * TH * 16) = dec;
+            *reinterpret_cast<u32x4 *>(lds + wb_at + half * kTile + i * kThreads * 16) = dec;
             if (again)
                 load_b(i);
         }
@@ -236,7 +235,7 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
     auto load_whole = [&](uint32_t s) {   // in the order of the main loop
         go_to(s);
 #pragma unroll
-        for (int i = 0; i < UA; ++i) {
+        for (int i = 0; i < U; ++i) {
             load_b(i);
             __builtin_amdgcn_sched_barrier(0);
             load_a(i);
@@ -248,16 +247,16 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
         const uint32_t per = (g.k + kBK - 1) / kBK - full, plane = i / per, k0 = (full + i - plane * per) * kBK;
         const uint16_t *a = g.a + plane * g.a_plane;
 #pragma unroll
-        for (int i = 0; i < UA; ++i) {
-            const uint32_t u = i * TH + t;
-            const uint32_t row = TA ? k0 + u / (BM / 8) : m0 + u / 8, col = TA ? m0 + u % (BM / 8) * 8 : k0 + u % 8 * 8;
+        for (int i = 0; i < U; ++i) {
+            const uint32_t u = i * kThreads + t;
+            const uint32_t row = TA ? k0 + u / (B / 8) : m0 + u / 8, col = TA ? m0 + u % (B / 8) * 8 : k0 + u % 8 * 8;
             ra[i] = row < (TA ? g.k : g.m) ? chunk_at(a + row * g.lda, col, g.a_cols) : u32x4{0, 0, 0, 0};
         }
 #pragma unroll
-        for (int i = 0; i < UB; ++i) {
-            const uint32_t u = i * TH + t;
-            const uint32_t row = TB ? k0 + u / (BN / 8) : n0 + u / 8;
-            const uint32_t unit = TB ? n0 / 8 + u % (BN / 8) : k0 / 8 + u % 8;   // 8 codes, 4 to a block
+        for (int i = 0; i < U; ++i) {
+            const uint32_t u = i * kThreads + t;
+            const uint32_t row = TB ? k0 + u / (B / 8) : n0 + u / 8;
+            const uint32_t unit = TB ? n0 / 8 + u % (B / 8) : k0 / 8 + u % 8;   // 8 codes, 4 to a block
             rb[i] = Codes(0);
             re[i] = 0;
             if (row < (TB ? g.k : g.n) && unit / 4 < g.nb) {
@@ -278,23 +277,23 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
             load_short(s - nfull);
         }
     };
-    bf16x8 fa[2][MI], fb[2][NJ];
+    bf16x8 fa[2][N], fb[2][N];
     auto read = [&](uint32_t half, int ks, int to, int r) {   // operand r of a step
-        if (r < MI)
-            fa[to][r] = TA ? read_t<BM>(lds + fa_at[r] + half * kA + ks * 16 * BM * 2) : read_k(lds + fa_at[ks] + half * kA + r * 4096);
+        if (r < N)
+            fa[to][r] = TA ? read_t<B>(lds + fa_at[r] + half * kTile + ks * 16 * B * 2) : read_k(lds + fa_at[ks] + half * kTile + r * 4096);
         else
-            fb[to][r - MI] = TB ? read_t<BN>(lds + fb_at[r - MI] + half * kB + ks * 16 * BN * 2)
-                                : read_k(lds + fb_at[ks] + half * kB + (r - MI) * 4096);
+            fb[to][r - N] = TB ? read_t<B>(lds + fb_at[r - N] + half * kTile + ks * 16 * B * 2)
+                                : read_k(lds + fb_at[ks] + half * kTile + (r - N) * 4096);
     };
     // A step multiplies 16 values of the sum out of registers. `beside(x)` is what is issued
     // after product x: the matrix unit is busy 32 cycles with each, so the rest of the wave's work
     // is dealt out between them, in this order.
-    constexpr int P = MI * NJ, R = MI + NJ;
+    constexpr int P = N * N, R = 2 * N;
     auto step = [&](int regs, auto beside) {
 #pragma unroll
         for (int x = 0; x < P; ++x) {
-            acc[x / NJ][x % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[regs][x / NJ], fb[regs][x % NJ],
-                                                                          acc[x / NJ][x % NJ], 0, 0, 0);
+            acc[x / N][x % N] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[regs][x / N], fb[regs][x % N],
+                                                                          acc[x / N][x % N], 0, 0, 0);
             beside(x);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -385,7 +384,7 @@ __global__ __launch_bounds__(128 * WN, MI * NJ > 8 ? 1 : 2) void gemm_kernel(Gem
     Out o = {g.c, g.ldc, g.ctype, g.accumulate};
     if (g.splits > 1)
         o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
-    put_tile<WN, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
+    put_tile<N>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
 // c = the sum of the parts, always in their order; four values of a row to a thread, or fewer at
@@ -620,33 +619,32 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // stage in LDS took 538), the matrix unit busy 57% of the cycles: a stage brings 68 KB to a
 // workgroup in the time in which gemm_kernel brings 40 to 48, and its waits are what is left.
 // (The checked last stages spill a few registers; the main loop does not.)
-template <int MI, int NJ>
-__global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Gemm4 g)
+template <int N>
+__global__ __launch_bounds__(kThreads, N > 2 ? 1 : 2) void gemm4_kernel(Gemm4 g)
 {
-    constexpr int BM = 64 * MI, BN = 64 * NJ, U = BM * 8 / kThreads, R = MI + NJ, P = MI * NJ;
-    static_assert(BM == BN, "one count of copies");
-    constexpr uint32_t kA = BM * 128, kB = BN * 128, kS = (BM + BN) * 8;
-    __shared__ __align__(16) uint8_t lds[2 * (kA + kB + kS)];   // two stages: codes of x, of w, scales
+    constexpr int B = 64 * N, U = B * 8 / kThreads, R = 2 * N, P = N * N;
+    constexpr uint32_t kTile = B * 128, kS = 2 * B * 8;
+    __shared__ __align__(16) uint8_t lds[2 * (2 * kTile + kS)];   // two stages: codes of x, of w, scales
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const uint32_t tiles = g.tm * g.tn, part = blockIdx.x / tiles;
     uint32_t tile_m, tile_n;
     tile_of(blockIdx.x - part * tiles, g.tm, g.tn, tile_m, tile_n);
-    const uint32_t m0 = tile_m * BM, n0 = tile_n * BN;
-    const uint32_t wm = (wave >> 1) * 32 * MI, wn = (wave & 1) * 32 * NJ;
+    const uint32_t m0 = tile_m * B, n0 = tile_n * B;
+    const uint32_t wm = (wave >> 1) * 32 * N, wn = (wave & 1) * 32 * N;
     const uint32_t s_begin = part * g.per, s_end = min(g.stages, s_begin + g.per);
 
-    f32x16 acc[MI][NJ] = {};
+    f32x16 acc[N][N] = {};
     u32x4 rc[2][U];            // codes on their way: of x, of w
-    constexpr int S = (BM + BN) / kThreads;   // rows of scales that a thread copies
+    constexpr int S = 2 * B / kThreads;   // rows of scales that a thread copies
     u32x2 rsc[S];
 
     uint32_t frag_at[2][4], code_at[2][U], scale_at[S];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         frag_at[0][i] = frag_k_at(wm, i, lane);
-        frag_at[1][i] = 2 * kA + frag_k_at(wn, i, lane);
+        frag_at[1][i] = 2 * kTile + frag_k_at(wn, i, lane);
     }
-    const uint32_t write_at = at_k(t / 8, t % 8), write_w = 2 * kA + write_at;
+    const uint32_t write_at = at_k(t / 8, t % 8), write_w = 2 * kTile + write_at;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         code_at[0][i] = min(i * 32 + t / 8, g.m - 1 - m0) * g.nb * 16 + t % 8 * 16;
@@ -657,7 +655,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
 #pragma unroll
     for (int i = 0; i < S; ++i) {
         const uint32_t r = row_of(i);
-        scale_at[i] = r < BM ? min(r, g.m - 1 - m0) * g.nb : min(r - BM, g.n - 1 - n0) * g.nb;
+        scale_at[i] = r < B ? min(r, g.m - 1 - m0) * g.nb : min(r - B, g.n - 1 - n0) * g.nb;
     }
     const uint8_t *px = nullptr, *pw = nullptr, *sx = nullptr, *sw = nullptr;   // the next whole stage
     auto go_to = [&](uint32_t s) {
@@ -669,15 +667,15 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
         rc[o][i] = __builtin_amdgcn_raw_buffer_load_b128(buffer_at(o ? pw : px), code_at[o][i], 0, 0);
     };
     auto load_scale = [&](int i) {   // 8 bytes of any alignment
-        const uint8_t *base = (BM % kThreads == 0 ? i * kThreads < BM : t < BM) ? sx : sw;
+        const uint8_t *base = (B % kThreads == 0 ? i * kThreads < B : t < B) ? sx : sw;
         __builtin_memcpy(&rsc[i], base + scale_at[i], 8);
     };
     constexpr int kItems = 2 * U + S;
     auto write = [&](uint32_t half, int y) {
         if (y < 2 * U)
-            *reinterpret_cast<u32x4 *>(lds + (y & 1 ? write_w + half * kB : write_at + half * kA) + (y >> 1) * 4096) = rc[y & 1][y >> 1];
+            *reinterpret_cast<u32x4 *>(lds + (y & 1 ? write_w + half * kTile : write_at + half * kTile) + (y >> 1) * 4096) = rc[y & 1][y >> 1];
         else
-            *reinterpret_cast<u32x2 *>(lds + 2 * (kA + kB) + half * kS + row_of(y - 2 * U) * 8) = rsc[y - 2 * U];
+            *reinterpret_cast<u32x2 *>(lds + 4 * kTile + half * kS + row_of(y - 2 * U) * 8) = rsc[y - 2 * U];
     };
     auto load_item = [&](int y) {
         if (y < 2 * U)
@@ -707,8 +705,8 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
             }
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-            const bool w = row_of(i) >= BM;
-            const uint32_t row = w ? n0 + row_of(i) - BM : m0 + row_of(i);
+            const bool w = row_of(i) >= B;
+            const uint32_t row = w ? n0 + row_of(i) - B : m0 + row_of(i);
             const uint8_t *p = (w ? g.w.scales : g.x.scales) + (uint64_t)row * g.nb + b0;
             uint64_t v = 0;   // a block of codes 0 is 0 at any scale but a NaN
             if (row < (w ? g.n : g.m))
@@ -729,11 +727,11 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
     u32x2 next_scale[R];
     uint32_t scale[R][2];
     auto read = [&](uint32_t half, int ks, int to, int r) {
-        fc[to][r] = *reinterpret_cast<const u32x4 *>(lds + (r < MI ? frag_at[0][ks] + half * kA + r * 4096 : frag_at[1][ks] + half * kB + (r - MI) * 4096));
+        fc[to][r] = *reinterpret_cast<const u32x4 *>(lds + (r < N ? frag_at[0][ks] + half * kTile + r * 4096 : frag_at[1][ks] + half * kTile + (r - N) * 4096));
     };
     auto read_scale = [&](uint32_t half, int r) {
-        const uint32_t row = r < MI ? wm + r * 32 : BM + wn + (r - MI) * 32;
-        next_scale[r] = *reinterpret_cast<const u32x2 *>(lds + 2 * (kA + kB) + half * kS + (row + (lane & 31)) * 8);
+        const uint32_t row = r < N ? wm + r * 32 : B + wn + (r - N) * 32;
+        next_scale[r] = *reinterpret_cast<const u32x2 *>(lds + 4 * kTile + half * kS + (row + (lane & 31)) * 8);
     };
     const uint32_t shift = (lane >> 5) * 8;
     auto take_scale = [&](int r) {
@@ -747,10 +745,10 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
         constexpr int ks = decltype(ks_)::value;
 #pragma unroll
         for (int x = 0; x < P; ++x) {
-            const int i = x / NJ, j = x % NJ;
+            const int i = x / N, j = x % N;
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                wide(fc[ks & 1][i]), wide(fc[ks & 1][MI + j]), acc[i][j], 4, 4, ks % 2 * 2, (int)scale[i][ks / 2],
-                ks % 2 * 2, (int)scale[MI + j][ks / 2]);
+                wide(fc[ks & 1][i]), wide(fc[ks & 1][N + j]), acc[i][j], 4, 4, ks % 2 * 2, (int)scale[i][ks / 2],
+                ks % 2 * 2, (int)scale[N + j][ks / 2]);
             beside(x);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -850,7 +848,7 @@ __global__ __launch_bounds__(kThreads, MI * NJ > 4 ? 1 : 2) void gemm4_kernel(Ge
     Out o = {g.c, g.ldc, g.ctype, 0};
     if (g.splits > 1)
         o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
-    put_tile<2, MI, NJ>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
+    put_tile<N>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
 Gemm4 plan4_of(const Mx4Product &p, int num_cu)
@@ -948,12 +946,12 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
     g.accumulate = p.accumulate;
     g.parts = parts;
     const dim3 grid(r.tm * r.tn * r.splits);
-#define MX_GEMM(...)                                                                                 \
-    do {                                                                                             \
-        if (r.tile == 256)                                                                           \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 4, 4>), grid, dim3(kThreads), 0, s, g);  \
-        else                                                                                         \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, 2, 2>), grid, dim3(kThreads), 0, s, g);  \
+#define MX_GEMM(...)                                                                              \
+    do {                                                                                          \
+        if (r.tile == 256)                                                                        \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 4>), grid, dim3(kThreads), 0, s, g);     \
+        else                                                                                      \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2>), grid, dim3(kThreads), 0, s, g);     \
     } while (0)
     if (p.op == kLinear)
         MX_GEMM(kMx4, false, false);
@@ -962,7 +960,7 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
     else if (!r.decoded)
         MX_GEMM(kMx8, true, true);
     else
-        hipLaunchKernelGGL((gemm_kernel<kDecoded, true, true, 2, 4, 4>), grid, dim3(kThreads), 0, s, g);
+        hipLaunchKernelGGL((gemm_kernel<kDecoded, true, true, 4>), grid, dim3(kThreads), 0, s, g);
 #undef MX_GEMM
     return hipGetLastError();
 }
@@ -1033,9 +1031,9 @@ hipError_t launch_mx4_product(const Mx4Product &p, int num_cu, hipStream_t s)
     g.parts = reinterpret_cast<float *>(p.work);
     const dim3 grid(g.tm * g.tn * g.splits);
     if (g.tile == 256)
-        hipLaunchKernelGGL((gemm4_kernel<4, 4>), grid, dim3(kThreads), 0, s, g);
+        hipLaunchKernelGGL((gemm4_kernel<4>), grid, dim3(kThreads), 0, s, g);
     else
-        hipLaunchKernelGGL((gemm4_kernel<2, 2>), grid, dim3(kThreads), 0, s, g);
+        hipLaunchKernelGGL((gemm4_kernel<2>), grid, dim3(kThreads), 0, s, g);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess && g.splits > 1 ? join(g.parts, g.splits, p.m, p.n, {p.c.p, p.c.ld, p.ctype, 0}, s) : e;
 }

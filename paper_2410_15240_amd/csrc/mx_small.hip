@@ -19,7 +19,7 @@ namespace mx {
 
 constexpr int kThreads = kSmallThreads, kWaves = kThreads / 64;
 
-// Eight elements of a float operand as they lie in memory, and taken apart into bf16 terms.
+// Eight elements of a float operand as they lie in memory.
 template <uint32_t T> struct Unit8 {
     static constexpr int kTerms = T == kBf16 ? 1 : T == kFp16 ? 2 : 3;
     static constexpr int kWords = T == kFp32 ? 8 : 4, kSize = T == kFp32 ? 4 : 2;
@@ -83,23 +83,6 @@ template <uint32_t T> struct Unit8 {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 v[i] = (float)h[i];
-        }
-    }
-    // All terms at once.
-    __device__ __forceinline__ void terms(u32x4 (&t)[kTerms]) const
-    {
-        if (T == kBf16) {
-            t[0] = bf16();
-            return;
-        }
-        float v[8];
-        floats(v);
-        t[0] = first_term(v);
-        if (kTerms >= 2)
-            t[kTerms >= 2 ? 1 : 0] = upper_halves(v);
-        if (kTerms == 3) {
-            leave_lower(v);
-            t[kTerms - 1] = upper_halves(v);
         }
     }
 };
@@ -425,13 +408,6 @@ __global__ __launch_bounds__(kThreads, S == 2 ? 2 : 4) void small_kernel(SmallPr
 }  // namespace mx
 
 using namespace mx;
-
-#define MX_TYPE(t, ...)                                                                            \
-    do {                                                                                           \
-        if ((t) == kBf16) { constexpr uint32_t T = kBf16; __VA_ARGS__; }                           \
-        else if ((t) == kFp16) { constexpr uint32_t T = kFp16; __VA_ARGS__; }                      \
-        else { constexpr uint32_t T = kFp32; __VA_ARGS__; }                                        \
-    } while (0)
 
 template <uint32_t T, int M>
 static hipError_t dot(SmallProduct g, hipStream_t s)
