@@ -105,7 +105,13 @@ __device__ __forceinline__ float normal_tail(float a)
                              FAST ? 0.0829465464f : 0.0853466466f,  FAST ? 0.142493442f : 0.0966654718f,
                              FAST ? -0.0663630813f : -0.00348356646f, FAST ? 0.195273235f : 0.207300872f,
                              FAST ? -0.0677870661f : -0.227627978f, 0.273647487f, -0.147487491f, 0.0278251003f};
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, FAST ? 0.265f : 0.235f, 1.0f));
+    constexpr float k = FAST ? 0.265f : 0.235f;
+    const float d = __builtin_fmaf(a, k, 1.0f);
+    float t = __builtin_amdgcn_rcpf(d);
+    if (!FAST) {   // the reciprocal's and d's own rounding, which count three times in the result
+        const float low = __builtin_fmaf(a, k, 1.0f - d);
+        t = __builtin_fmaf(t, __builtin_fmaf(-low, t, __builtin_fmaf(-d, t, 1.0f)), t);
+    }
     float p = c[N - 1];
 #pragma unroll
     for (int i = N - 2; i >= 0; --i)
@@ -125,13 +131,12 @@ __device__ __forceinline__ void act_of(float x, float &f, float &df)
         df = s * (1.0f + x * (1.0f - s));
     } else {              // x P(x), P + x p(x); P the normal distribution, p its density
         const float a = fminf(__builtin_fabsf(x), 20.0f);   // (past which e is 0; a NaN goes on in x)
-        float e;
-        if (FAST) {
-            e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
-        } else {   // what the square's rounding leaves counts as much as its size
-            const float sq = a * a;
-            e = expf(-0.5f * sq);
-            e = __builtin_fmaf(-0.5f * e, __builtin_fmaf(a, a, -sq), e);
+        constexpr float c = -0.7213475f, c_low = -9.629815e-9f;   // -log2(e) / 2
+        const float sq = a * a, h = sq * c;
+        float e = __builtin_amdgcn_exp2f(h);
+        if (!FAST) {   // what the argument's roundings leave: a unit of it is worth as many as it is large
+            const float low = __builtin_fmaf(sq, c_low, __builtin_fmaf(__builtin_fmaf(a, a, -sq), c, __builtin_fmaf(sq, c, -h)));
+            e = __builtin_fmaf(e, low * 0.6931472f, e);
         }
         const float q = e * normal_tail<FAST>(a), P = x < 0.0f ? q : 1.0f - q;
         f = x * P;
