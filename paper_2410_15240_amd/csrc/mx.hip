@@ -5,8 +5,8 @@
 // Work is cut into units of 8 values; four neighbouring lanes hold a block of 32 and share
 // its largest magnitude by two lane exchanges, so no value is read twice and nothing goes
 // through LDS. What bounds it is HBM: 1 GiB of bf16 to MX4 in 223-258 us, back in 233-246 (5.3-6
-// TB/s; a device copy of 1 GiB runs at 5.1); gated SiLU of 4096 x 16384 bf16 forwards 93-95 us and
-// backwards 92-95 (5.8 TB/s).
+// TB/s; a device copy of 1 GiB runs at 5.1); gated SiLU of 4096 x 16384 bf16 forwards 91-97 us and
+// backwards 92-100 (5.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -106,9 +106,9 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
 // 8192 x 8192 weights of bf16; eight waves of 128 x 64, 414 too, and 572 instead of 490 where
 // both operands are read across their rows). A wave alone on its SIMD has only its own work to
 // put beside its products, so that is dealt out by hand, a few instructions after each
-// (compiled in its own order: 514). Measured for that layer: linear 405-415 us (1.33-1.36
-// PFLOP/s), input gradient 380-390 (1.41-1.45), weight gradient 439 with its decoding; the
-// library's bf16 product of these sizes 421. The matrix unit is busy 70-76% of the cycles; what
+// (compiled in its own order: 514). Measured for that layer, on cards of different clocks:
+// linear 403-443 us (1.24-1.36 PFLOP/s), input gradient 380-424 (1.30-1.45), weight gradient
+// 439-487 with its decoding; the library's bf16 product of these sizes 398-421. The matrix unit is busy 70-76% of the cycles; what
 // bounds them is power, which holds the clock near 1.7 GHz under this load.
 //
 // Stages of 64 whole values come first, of every term of a, then the terms' last, short ones.
@@ -569,7 +569,11 @@ Plan plan_of(const MxProduct &p, int num_cu)
 
     // Small tiles or gemm_kernel's of 128, by estimates of their times in us. A workgroup of small
     // tiles takes 3 and an eighth of what its slices were measured to take a wave; those of 32
-    // run two to a CU. Slower where a tile reads a few bytes each of long rows of the MX matrix.
+    // run two to a CU. Where the MX matrix is read across its rows, 16 or 32 bytes of each, a slice
+    // takes longer the more tiles read at once and the farther its rows lie apart (gradient of
+    // 32 tokens, 4096 outputs of bf16, tiles of 32: 0.7 us in 16 and 32 tiles, 1.7 in 64 to 125; 2.1 in 128 with rows
+    // of 128 blocks, 2.8 in 256, with gemm_kernel on the other side 15.7 and 16.0 us for 16.7 of 125 tiles
+    // and 25.6 of 256): so the step at 64 tiles, and the one at rows of 128 blocks.
     // gemm_kernel takes 8, 4 more to lay out a's terms, and its sum's time as above, a quarter more
     // for every round of several. (Both sides: linear, 1000 x 2000 x 1000 of bf16: 12 and 26; 128 tokens, 8192 x
     // 8192 of fp32: 125 and 71; gradient of 32 tokens, 8192 x 8192 of bf16: 48 and 25; weight
@@ -615,7 +619,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // read like one of 64 bf16 values above (16 bytes are a block here), and its 8 scales of each
 // row beside it. A lane reads its row's 8 scales at once, and the instruction picks the byte:
 // blocks 2 ks of the lower lanes, 2 ks + 1 of the upper ones, whose words are shifted down by
-// one byte. 143-148 us for 4096 tokens and 8192 x 8192 weights (3.7 PFLOP/s; tiles of 128 and one
+// one byte. 141-155 us for 4096 tokens and 8192 x 8192 weights (3.7 PFLOP/s; tiles of 128 and one
 // stage in LDS took 538), the matrix unit busy 57% of the cycles: a stage brings 68 KB to a
 // workgroup in the time in which gemm_kernel brings 40 to 48, and its waits are what is left.
 // (The checked last stages spill a few registers; the main loop does not.)

@@ -93,8 +93,9 @@ template <uint32_t T> struct Unit8 {
 // blocks of a row at once, one to a lane (1 KB of codes that follow one another), of R rows
 // before it uses the first, and multiplies them with the x of those places, which it keeps in
 // registers for all R. bf16 by the pairwise product, 16 and 32-bit floats in 32 bits. The
-// lanes' sums meet in LDS. What bounds it is the reading of w, K / 2 + K / 32 bytes a row: 7.1
-// us for 8192 x 8192, 5 TB/s (6.6 alone). (Lanes that read 64 bytes each of 16 rows, as the matrix
+// lanes' sums meet in LDS. What bounds it is the reading of w, K / 2 + K / 32 bytes a row: 7.0
+// us for 8192 x 8192, 5.1 TB/s, out of the last-level cache, and 9.4, 3.8 TB/s, out of memory
+// (32 such layers in turn). (Lanes that read 64 bytes each of 16 rows, as the matrix
 // instruction takes them, took twice that: rows a power of two apart are one memory channel's
 // work at a time.)
 constexpr int kDotWaves = 4;
