@@ -473,6 +473,103 @@ int fastrack_mx_linear_mx(const uint8_t *d_xcodes, const uint8_t *d_xscales, con
                           const uint8_t *d_scales, uint64_t m, uint64_t n, uint64_t k, uint32_t out_type, void *d_y,
                           uint64_t ldy, void *d_work, uint64_t work_bytes, void *stream);
 
+/*
+ * What stands around a model's layers: the lookup of its first activations, the norm
+ * between two blocks, the loss at its end. Operands, sizes, strides, rounding and EINVAL
+ * as above; ids are int32 or int64 (FASTRACK_I32, FASTRACK_I64), one after the other.
+ */
+enum fastrack_index { FASTRACK_I32 = 0, FASTRACK_I64 = 1 };
+
+/*
+ * Embedding: y[t][k] = scale * table[id_t][k] for a table [rows][cols] in MX4. A negative
+ * id is padding: its row is 0, and it counts for nothing in the gradient. An id of `rows`
+ * or more is a mistake that the device alone can see: its row is NaN.
+ *   embedding_grad  dw[i][k] = scale * sum of dy[t][k] over the t with id_t = i, added in
+ *                   the order of t (so that it is the same every time) within runs of 32
+ *                   sorted tokens, and these in their order; added to what d_dw holds
+ *                   where accumulate is 1 (32-bit d_dw only). Ids of `rows` or more
+ *                   count for nothing.
+ * d_work: fastrack_mx_embedding_grad_work_bytes(...) bytes, 16-byte aligned.
+ * EINVAL too: more than 2^24 - 1 pieces of 32 tokens and 2048 columns (of the gradient).
+ */
+int fastrack_mx_embedding(uint32_t index_type, const void *d_ids, uint64_t m, const uint8_t *d_codes, const uint8_t *d_scales,
+                          uint64_t rows, uint64_t cols, float scale, uint32_t type, void *d_y, uint64_t ldy, void *stream);
+uint64_t fastrack_mx_embedding_grad_work_bytes(uint64_t m, uint64_t rows, uint64_t cols);
+int fastrack_mx_embedding_grad(uint32_t index_type, const void *d_ids, uint32_t type, const void *d_dy, uint64_t ld_dy,
+                               uint64_t m, uint64_t rows, uint64_t cols, float scale, uint32_t out_type, void *d_dw,
+                               uint64_t ld_dw, uint32_t accumulate, void *d_work, uint64_t work_bytes, void *stream);
+
+/*
+ * The norm between two blocks, with the first block's own norm, gate, residual and its
+ * scale, in one pass:
+ *   b = x / rms(x) * post_weight   (d_post_weight NULL: b = x)
+ *   h = residual + scale * gate * b   (d_residual, d_gate NULL: without)
+ *   y = h / rms(h) * weight
+ * with rms(v) = sqrt(mean of v^2 + eps) over a row. All is in 32 bits; y comes from h as it
+ * is before its rounding to d_hidden (NULL: not written). Kept for the gradient: h / rms(h)
+ * in MX8 (d_ucodes, d_uscales) and 1 / rms(h) in d_inverse [rows]; with a post_weight
+ * x / rms(x) in MX8 (d_vcodes, d_vscales) and 1 / rms(x) in d_post_inverse [rows]; with a
+ * gate and no post_weight x itself in MX8 (d_vcodes, d_vscales); with a gate, that in MX8.
+ * Weights are [cols], of the rows' type or 32-bit floats.
+ *
+ * norm_grad, at the kept values u, v (or x^) and gate^:
+ *   t = dy * weight,  dh = inverse * (t - u * mean(t u)) + dhidden   (d_dhidden NULL: without)
+ *   dweight = sum over rows of dy u,  dresidual = dh   (NULL: not written)
+ *   db = scale * gate^ * dh,  dgate = scale * dh * (v * post_weight, or x^)
+ *   dpost_weight = sum over rows of db v
+ *   dx = post_inverse * (t1 - v * mean(t1 v)), t1 = db * post_weight; without one dx = db
+ * dweight and dpost_weight are 32-bit floats [cols], added in an order that is the same
+ * every time. d_work: fastrack_mx_norm_grad_work_bytes(rows, cols, has post_weight) bytes,
+ * 16-byte aligned. EINVAL too: eps negative or not finite, a scale that is no number.
+ */
+int fastrack_mx_norm(uint32_t type, const void *d_x, uint64_t ldx, const void *d_residual, uint64_t ld_residual,
+                     const void *d_gate, uint64_t ld_gate, uint64_t rows, uint64_t cols, uint32_t weight_type,
+                     const void *d_weight, const void *d_post_weight, float scale, float eps, void *d_y, uint64_t ldy,
+                     void *d_hidden, uint64_t ld_hidden, uint8_t *d_ucodes, uint8_t *d_uscales, float *d_inverse,
+                     uint8_t *d_vcodes, uint8_t *d_vscales, float *d_post_inverse, uint8_t *d_gcodes, uint8_t *d_gscales,
+                     void *stream);
+uint64_t fastrack_mx_norm_grad_work_bytes(uint64_t rows, uint64_t cols, uint32_t post);
+int fastrack_mx_norm_grad(uint32_t type, const void *d_dy, uint64_t ld_dy, const void *d_dhidden, uint64_t ld_dhidden,
+                          uint64_t rows, uint64_t cols, uint32_t weight_type, const void *d_weight, const void *d_post_weight,
+                          float scale, const uint8_t *d_ucodes, const uint8_t *d_uscales, const float *d_inverse,
+                          const uint8_t *d_vcodes, const uint8_t *d_vscales, const float *d_post_inverse,
+                          const uint8_t *d_gcodes, const uint8_t *d_gscales, void *d_dx, uint64_t ld_dx, void *d_dresidual,
+                          uint64_t ld_dresidual, void *d_dgate, uint64_t ld_dgate, float *d_dweight, float *d_dpost_weight,
+                          void *d_work, uint64_t work_bytes, void *stream);
+
+/*
+ * Softmax cross entropy over n classes whose head w [n][k] is in MX4, without keeping the
+ * logits z[t][v] = scale * sum over k of x[t][k] w[v][k] (products as in mx_linear):
+ *   lse[t] = log sum over v of e^z[t][v],  loss[t] = lse[t] - z[t][id_t]
+ * A negative id leaves its token out: loss 0, no gradient (its lse is written). An id of n
+ * or more is a mistake that the device alone can see: its loss and lse are NaN, and all
+ * gradients that it counts for.
+ *   loss_grad  dz[t][v] = scale * dloss[t] * (e^(z[t][v] - lse[t]) - [v = id_t])
+ *              dx[t][k] = sum over v of dz[t][v] w[v][k]   (d_dx NULL: not computed)
+ *              dw[v][k] = sum over t of dz[t][v] x^[t][k], x kept in MX8 (d_dw NULL: not
+ *              computed); added to what d_dw holds where accumulate is 1 (32-bit only)
+ * from the same x, w, ids and scale and the lse that they gave. The logits are computed
+ * again, a piece of the vocabulary at a time. dz is rounded once to bf16 for a gradient in
+ * bf16 and taken as two or three bf16 terms for one in fp16 or fp32; sums are in 32 bits.
+ * d_loss, d_lse, d_dloss: 32-bit floats [m], d_dloss `dloss_step` elements apart (0: one for
+ * all). d_work: fastrack_mx_loss_work_bytes(...) or fastrack_mx_loss_grad_work_bytes(...)
+ * bytes, 16-byte aligned; they depend on x's address and stride and on the device; dx and
+ * dw say which gradients are wanted.
+ * EINVAL too: n = 0 with m > 0; more than 2^24 - 1 tokens; more than 2^24 output tiles of
+ * 128 x 128 in a gradient.
+ */
+uint64_t fastrack_mx_loss_work_bytes(uint32_t type, const void *d_x, uint64_t ldx, uint64_t m, uint64_t n, uint64_t k);
+int fastrack_mx_loss(uint32_t type, const void *d_x, uint64_t ldx, const uint8_t *d_codes, const uint8_t *d_scales,
+                     uint32_t index_type, const void *d_ids, uint64_t m, uint64_t n, uint64_t k, float scale, float *d_loss,
+                     float *d_lse, void *d_work, uint64_t work_bytes, void *stream);
+uint64_t fastrack_mx_loss_grad_work_bytes(uint32_t type, const void *d_x, uint64_t ldx, uint64_t m, uint64_t n, uint64_t k,
+                                          uint32_t dx, uint32_t dx_type, uint32_t dw, uint32_t dw_type);
+int fastrack_mx_loss_grad(uint32_t type, const void *d_x, uint64_t ldx, const uint8_t *d_codes, const uint8_t *d_scales,
+                          const uint8_t *d_xcodes, const uint8_t *d_xscales, uint32_t index_type, const void *d_ids,
+                          const float *d_dloss, uint64_t dloss_step, const float *d_lse, uint64_t m, uint64_t n, uint64_t k,
+                          float scale, uint32_t dx_type, void *d_dx, uint64_t ld_dx, uint32_t dw_type, void *d_dw,
+                          uint64_t ld_dw, uint32_t accumulate, void *d_work, uint64_t work_bytes, void *stream);
+
 /* Message of the last failure on this thread ("" if none). */
 const char *fastrack_last_error(void);
 

@@ -13,7 +13,8 @@ OUT_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUT_DIR, "libfastrack.so")
 # Each source with the LLVM scheduling flags it is built with (see below).
 SOURCES = [("kernels.hip", True), ("api.hip", True), ("bitslice.hip", False), ("mx.hip", False), ("mx_gemm.hip", False),
-           ("mx_small.hip", False), ("mx_api.hip", False)]
+           ("mx_small.hip", False), ("mx_api.hip", False), ("mx_norm.hip", False), ("mx_embed.hip", False),
+           ("mx_loss.hip", False), ("mx_model_api.hip", False)]
 ARCH = "gfx950"
 
 

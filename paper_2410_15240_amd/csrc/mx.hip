@@ -19,14 +19,6 @@ namespace mx {
 
 constexpr int kThreads = 256;
 
-// Where a thread's unit lies: units are numbered along the rows, 4 to a block.
-struct Unit {
-    uint64_t row;
-    uint32_t c;      // first column
-    uint64_t block;  // index of its block in the whole matrix
-    uint32_t lane;   // which quarter of it
-};
-
 struct Shape {
     uint64_t row0;        // first row of this launch
     uint32_t units;       // of this launch, below 2^32
@@ -46,28 +38,6 @@ __device__ __forceinline__ bool unit_of(const Shape &sh, Unit &u)
     u.block = u.row * (sh.per_row / 4) + j / 4;
     u.lane = j & 3;
     return true;
-}
-
-template <uint32_t FMT>
-__device__ __forceinline__ void put(const MxMatrix &q, const Unit &u, const float (&v)[8])
-{
-    const uint32_t e = block_scale<FMT>(block_top(v));
-    if (FMT == kMx4)
-        reinterpret_cast<uint32_t *>(q.codes)[u.block * 4 + u.lane] = encode4(v, e);
-    else
-        reinterpret_cast<u32x2 *>(q.codes)[u.block * 4 + u.lane] = encode8(v, e);
-    if (u.lane == 0)
-        q.scales[u.block] = (uint8_t)e;
-}
-
-template <uint32_t FMT>
-__device__ __forceinline__ void get(const MxMatrix &q, const Unit &u, float (&v)[8])
-{
-    const uint32_t e = q.scales[u.block];
-    if (FMT == kMx4)
-        decode4_f32(reinterpret_cast<const uint32_t *>(q.codes)[u.block * 4 + u.lane], scale4_f32(e), v);
-    else
-        decode8_f32(reinterpret_cast<const u32x2 *>(q.codes)[u.block * 4 + u.lane], scale8_f32(e), v);
 }
 
 template <uint32_t FMT, uint32_t T>

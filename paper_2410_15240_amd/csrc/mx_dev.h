@@ -201,6 +201,36 @@ __device__ __forceinline__ u32x2 encode8(const float (&v)[8], uint32_t e)
     return u32x2{b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24};
 }
 
+// Where a thread's unit lies: units are numbered along the rows, 4 to a block.
+struct Unit {
+    uint64_t row;
+    uint32_t c;      // first column
+    uint64_t block;  // index of its block in the whole matrix
+    uint32_t lane;   // which quarter of it
+};
+
+template <uint32_t FMT>
+__device__ __forceinline__ void put(const MxMatrix &q, const Unit &u, const float (&v)[8])
+{
+    const uint32_t e = block_scale<FMT>(block_top(v));
+    if (FMT == kMx4)
+        reinterpret_cast<uint32_t *>(q.codes)[u.block * 4 + u.lane] = encode4(v, e);
+    else
+        reinterpret_cast<u32x2 *>(q.codes)[u.block * 4 + u.lane] = encode8(v, e);
+    if (u.lane == 0)
+        q.scales[u.block] = (uint8_t)e;
+}
+
+template <uint32_t FMT>
+__device__ __forceinline__ void get(const MxMatrix &q, const Unit &u, float (&v)[8])
+{
+    const uint32_t e = q.scales[u.block];
+    if (FMT == kMx4)
+        decode4_f32(reinterpret_cast<const uint32_t *>(q.codes)[u.block * 4 + u.lane], scale4_f32(e), v);
+    else
+        decode8_f32(reinterpret_cast<const u32x2 *>(q.codes)[u.block * 4 + u.lane], scale8_f32(e), v);
+}
+
 // The upper halves of eight floats: bf16 values cut, not rounded, so that what is left of each
 // (left: v becomes it) has 8 significant bits less and the terms add up to the value, down to
 // bf16's smallest, 2^-133.

@@ -1,0 +1,437 @@
+// The norm between two blocks of a model, with what stands around it: the block's own norm, its
+// gate, the residual and its scale. Forwards in one pass, with what the gradient needs kept in 8
+// bits; backwards in one pass over that.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "launch.h"
+#include "mx_dev.h"
+#include "mx_model.h"
+
+namespace fastrack {
+namespace mx {
+
+// A row is shared by G threads: unit j of 8 columns belongs to thread j % G, U of them to a thread,
+// which stay in its registers from the row's sum to its end. U = 0: rows of any length, read again
+// after each sum.
+template <int G> constexpr int threads_of() { return G < 256 ? 256 : G; }
+
+// The sum over the G threads of a row, to all of them. `slot` takes turns between 0 and 1: what one
+// sum leaves in LDS is read until the next one's barrier.
+template <int G>
+__device__ __forceinline__ float row_sum(float v, float (*lds)[16], int slot)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+        v += __shfl_xor(v, d, 64);
+    if (G > 64) {
+        if (threadIdx.x % 64 == 0)
+            lds[slot][threadIdx.x / 64] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < G / 64; ++w)
+            v += lds[slot][w];
+    }
+    return v;
+}
+
+// Eight of a weight vector, in the rows' type or in 32 bits.
+template <uint32_t T>
+__device__ __forceinline__ void weights8(const void *w, uint32_t wtype, uint32_t c, uint32_t cols, float (&v)[8])
+{
+    if (T != kFp32 && wtype == kFp32)
+        load8<kFp32>(w, 0, c, cols, v);
+    else
+        load8<T>(w, 0, c, cols, v);
+}
+
+__device__ __forceinline__ Unit unit_at(uint64_t row, uint32_t j, uint32_t units)
+{
+    return {row, j * 8, row * (units / 4) + j / 4, j & 3};
+}
+
+__device__ __forceinline__ float square_sum(const float (&v)[8])
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        s = __builtin_fmaf(v[i], v[i], s);
+    return s;
+}
+
+__device__ __forceinline__ float inverse_rms(float squares, uint32_t cols, float eps)
+{
+    return 1.0f / sqrtf(squares / (float)cols + eps);
+}
+
+template <uint32_t T, int G, int U>
+__global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t row0)
+{
+    constexpr int N = U ? U : 1, R = threads_of<G>() / G;
+    __shared__ float lds[2][16];
+    const uint32_t t = threadIdx.x % G, cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols));
+    const uint64_t row = row0 + (uint64_t)blockIdx.x * R + threadIdx.x / G;
+    if (row >= n.rows)   // (a whole wave, or a whole workgroup)
+        return;
+    auto each = [&](auto f) {
+        if (U) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (t + i * G < units)
+                    f(i, t + i * G);
+        } else {
+            for (uint32_t j = t; j < units; j += G)
+                f(0, j);
+        }
+    };
+    float h[N][8];
+    float inv1 = 1.0f;
+    if (n.w1) {
+        float s = 0.0f;
+        each([&](int i, uint32_t j) {
+            load8<T>(n.x.p, row * n.x.ld, j * 8, cols, h[i]);
+            s += square_sum(h[i]);
+        });
+        inv1 = inverse_rms(row_sum<G>(s, lds, 0), cols, n.eps);
+        if (t == 0)
+            n.inv1[row] = inv1;
+    }
+    // h of a unit, and on the way (`keep`) what is kept of x and g.
+    auto hidden = [&](int i, uint32_t j, bool keep) {
+        const Unit u = unit_at(row, j, units);
+        float f[8];
+        if (!U || !n.w1)
+            load8<T>(n.x.p, row * n.x.ld, u.c, cols, h[i]);
+        if (n.w1)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                h[i][e] *= inv1;
+        if (keep && n.v.codes)
+            put<kMx8>(n.v, u, h[i]);
+        if (n.w1) {
+            weights8<T>(n.w1, n.wtype, u.c, cols, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                h[i][e] *= f[e];
+        }
+        if (n.g.p) {
+            load8<T>(n.g.p, row * n.g.ld, u.c, cols, f);
+            if (keep)
+                put<kMx8>(n.gq, u, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                h[i][e] *= f[e];
+        }
+        if (n.r.p) {
+            load8<T>(n.r.p, row * n.r.ld, u.c, cols, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                h[i][e] = __builtin_fmaf(h[i][e], n.scale, f[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                h[i][e] *= n.scale;
+        }
+    };
+    float s = 0.0f;
+    each([&](int i, uint32_t j) {
+        hidden(i, j, true);
+        s += square_sum(h[i]);
+        if (n.h.p)
+            store8<T>(n.h.p, row * n.h.ld, j * 8, cols, h[i]);
+    });
+    const float inv2 = inverse_rms(row_sum<G>(s, lds, 1), cols, n.eps);
+    if (t == 0)
+        n.inv2[row] = inv2;
+    each([&](int i, uint32_t j) {
+        if (!U)
+            hidden(i, j, false);
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            h[i][e] *= inv2;
+        put<kMx8>(n.u, unit_at(row, j, units), h[i]);
+        weights8<T>(n.w2, n.wtype, j * 8, cols, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            w[e] *= h[i][e];
+        store8<T>(n.y.p, row * n.y.ld, j * 8, cols, w);
+    });
+}
+
+// How rows of a length are shared out. (Measured choices stand at the launches.)
+enum Way : int { kWave, k256x1, k256x2, k256x4, k1024x1, k1024x2, k1024x4, kLoop };
+
+// ---- backwards -----------------------------------------------------------------------------------
+//
+//   t = dy w2,  dh' = inv2 (t - u mean(t u)) + dh,  dw2 += dy u,  dr = dh'
+//   db = scale dh',  dg = db (v w1),  db *= g,  dw1 += db v
+//   dx = inv1 (db w1 - v mean(db w1 v))
+// A group takes every P-th row and adds up its rows' parts of dw2 and dw1, in registers; the groups'
+// sums are added in their order by columns_kernel.
+template <uint32_t T, int G, int U>
+__global__ __launch_bounds__(threads_of<G>()) void norm_grad_kernel(NormGrad n, uint32_t groups)
+{
+    constexpr int N = U ? U : 1, R = threads_of<G>() / G;
+    __shared__ float lds[2][16];
+    const uint32_t t = threadIdx.x % G, cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols));
+    const uint32_t group = blockIdx.x * R + threadIdx.x / G;
+    if (group >= groups)
+        return;
+    auto each = [&](auto f) {
+        if (U) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (t + i * G < units)
+                    f(i, t + i * G);
+        } else {
+            for (uint32_t j = t; j < units; j += G)
+                f(0, j);
+        }
+    };
+    float *const part2 = n.work + (uint64_t)group * cols, *const part1 = part2 + (uint64_t)groups * cols;
+    float sum2[N][8] = {}, sum1[N][8] = {};
+    auto flush = [&](uint32_t j, float *part, float (&s)[8], bool add) {
+        if (add) {
+            float old[8];
+            load8<kFp32>(part, 0, j * 8, cols, old);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s[e] += old[e];
+        }
+        store8<kFp32>(part, 0, j * 8, cols, s);
+    };
+    bool first = true;
+    for (uint64_t row = group; row < n.rows; row += groups, first = false) {
+        float d[N][8], a[N][8];   // dy w2 and then what goes on; u and then v
+        const float inv2 = n.inv2[row];
+        float s = 0.0f;
+        auto begin = [&](int i, uint32_t j, bool sums) {
+            const Unit u = unit_at(row, j, units);
+            float w[8];
+            load8<T>(n.dy.p, row * n.dy.ld, u.c, cols, d[i]);
+            get<kMx8>(n.u, u, a[i]);
+            weights8<T>(n.w2, n.wtype, u.c, cols, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (sums)
+                    sum2[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum2[i][e]);
+                d[i][e] *= w[e];
+            }
+        };
+        each([&](int i, uint32_t j) {
+            if (!U)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum2[i][e] = 0.0f;
+            begin(i, j, true);
+            if (!U)
+                flush(j, part2, sum2[i], !first);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s = __builtin_fmaf(d[i][e], a[i][e], s);
+        });
+        const float along2 = row_sum<G>(s, lds, 0) / (float)cols;
+        s = 0.0f;
+        // The gradient of b, and of what comes before it.
+        auto middle = [&](int i, uint32_t j, bool put_out) {
+            const Unit u = unit_at(row, j, units);
+            float f[8];
+            if (!U)
+                begin(i, j, false);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                d[i][e] = inv2 * __builtin_fmaf(-along2, a[i][e], d[i][e]);
+            if (n.dh.p) {
+                load8<T>(n.dh.p, row * n.dh.ld, u.c, cols, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[i][e] += f[e];
+            }
+            if (put_out && n.dr.p)
+                store8<T>(n.dr.p, row * n.dr.ld, u.c, cols, d[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                d[i][e] *= n.scale;
+            float w[8];
+            if (n.v.codes)
+                get<kMx8>(n.v, u, a[i]);
+            if (n.w1)
+                weights8<T>(n.w1, n.wtype, u.c, cols, w);
+            if (n.gq.codes) {
+                float g[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    f[e] = d[i][e] * (n.w1 ? a[i][e] * w[e] : a[i][e]);
+                if (put_out)
+                    store8<T>(n.dg.p, row * n.dg.ld, u.c, cols, f);
+                get<kMx8>(n.gq, u, g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[i][e] *= g[e];
+            }
+            if (n.w1)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (put_out)
+                        sum1[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum1[i][e]);
+                    d[i][e] *= w[e];
+                }
+        };
+        each([&](int i, uint32_t j) {
+            if (!U)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum1[i][e] = 0.0f;
+            middle(i, j, true);
+            if (!n.w1) {
+                store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d[i]);
+                return;
+            }
+            if (!U)
+                flush(j, part1, sum1[i], !first);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s = __builtin_fmaf(d[i][e], a[i][e], s);
+        });
+        if (!n.w1) {
+            if (G > 64)
+                __syncthreads();   // (the next row's sum goes to the same place of the LDS)
+            continue;
+        }
+        const float along1 = row_sum<G>(s, lds, 1) / (float)cols, inv1 = n.inv1[row];
+        each([&](int i, uint32_t j) {
+            if (!U)
+                middle(i, j, false);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                d[i][e] = inv1 * __builtin_fmaf(-along1, a[i][e], d[i][e]);
+            store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d[i]);
+        });
+    }
+    if (U)
+        each([&](int i, uint32_t j) {
+            flush(j, part2, sum2[i], false);
+            if (n.w1)
+                flush(j, part1, sum1[i], false);
+        });
+}
+
+// Sums of 64 columns of `parts` rows, always in the same order: a wave takes every 16th row, the
+// waves' sums are added in theirs.
+__global__ __launch_bounds__(1024) void columns_kernel(const float *work, uint32_t parts, uint32_t cols, float *out0, float *out1)
+{
+    __shared__ float lds[16][64];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    const float *p = work + (uint64_t)blockIdx.y * parts * cols;
+    float s = 0.0f;
+    if (c < cols)
+#pragma unroll 8
+        for (uint32_t r = wave; r < parts; r += 16)
+            s += p[(uint64_t)r * cols + c];
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w)
+            s += lds[w][lane];
+        (blockIdx.y ? out1 : out0)[c] = s;
+    }
+}
+
+}  // namespace mx
+
+using namespace mx;
+
+static Way forward_way(uint64_t rows, uint64_t cols, int num_cu)
+{
+    const uint64_t units = 4 * mx_blocks(cols);
+    if (units > 4096)
+        return kLoop;
+    if (units > 1024)
+        return k1024x4;
+    if (units <= 128)
+        return kWave;
+    if (rows < (uint64_t)num_cu)
+        return k1024x1;
+    return units <= 256 ? k256x1 : units <= 512 ? k256x2 : k256x4;
+}
+
+hipError_t launch_mx_norm(const Norm &n, int num_cu, hipStream_t s)
+{
+    if (n.rows == 0 || n.cols == 0)
+        return hipSuccess;
+    const Way way = forward_way(n.rows, n.cols, num_cu);
+    const uint64_t most = 1ull << 21;   // rows of a launch: fewer than 2^32 threads
+    for (uint64_t row0 = 0; row0 < n.rows; row0 += most) {
+        Norm p = n;
+        p.rows = n.rows - row0 < most ? n.rows : row0 + most;
+        const uint64_t rows = p.rows - row0;
+#define NORM(G, U)                                                                                                   \
+    MX_TYPE(n.type, hipLaunchKernelGGL((norm_kernel<T, G, U>), dim3((uint32_t)((rows * G + threads_of<G>() - 1) / threads_of<G>())), \
+                                       dim3(threads_of<G>()), 0, s, p, row0))
+        switch (way) {
+        case kWave: NORM(64, 2); break;
+        case k256x1: NORM(256, 1); break;
+        case k256x2: NORM(256, 2); break;
+        case k256x4: NORM(256, 4); break;
+        case k1024x1: NORM(1024, 1); break;
+        case k1024x4: NORM(1024, 4); break;
+        default: NORM(1024, 0); break;
+        }
+#undef NORM
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}
+
+static Way backward_way(uint64_t cols)
+{
+    const uint64_t units = 4 * mx_blocks(cols);
+    return units <= 128 ? kWave : units <= 256 ? k256x1 : units <= 512 ? k256x2 : units <= 1024 ? k1024x1 : units <= 2048 ? k1024x2 : kLoop;
+}
+
+// Groups that take the rows in turn: as many as run at once.
+static uint32_t groups_of(uint64_t rows, uint64_t cols, int num_cu)
+{
+    const Way way = backward_way(cols);
+    const uint64_t most = (uint64_t)num_cu * (way == kWave ? 16 : way == k256x1 || way == k256x2 ? 4 : 1);
+    return (uint32_t)(rows < most ? rows : most);
+}
+
+uint64_t mx_norm_grad_work(uint64_t rows, uint64_t cols, bool w1, int num_cu)
+{
+    return (uint64_t)groups_of(rows, cols, num_cu) * cols * (w1 ? 2 : 1);
+}
+
+hipError_t launch_mx_norm_grad(const NormGrad &n, int num_cu, hipStream_t s)
+{
+    if (n.cols == 0)
+        return hipSuccess;
+    const uint32_t groups = groups_of(n.rows, n.cols, num_cu);
+    if (groups) {
+#define NORM(G, U)                                                                                                        \
+    MX_TYPE(n.type, hipLaunchKernelGGL((norm_grad_kernel<T, G, U>), dim3((groups * G + threads_of<G>() - 1) / threads_of<G>()), \
+                                       dim3(threads_of<G>()), 0, s, n, groups))
+        switch (backward_way(n.cols)) {
+        case kWave: NORM(64, 2); break;
+        case k256x1: NORM(256, 1); break;
+        case k256x2: NORM(256, 2); break;
+        case k1024x1: NORM(1024, 1); break;
+        case k1024x2: NORM(1024, 2); break;
+        default: NORM(1024, 0); break;
+        }
+#undef NORM
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    hipLaunchKernelGGL(columns_kernel, dim3((uint32_t)((n.cols + 63) / 64), n.w1 ? 2 : 1), dim3(1024), 0, s, n.work, groups,
+                       (uint32_t)n.cols, n.dw2, n.dw1);
+    return hipGetLastError();
+}
+
+}  // namespace fastrack
