@@ -485,12 +485,12 @@ enum fastrack_index { FASTRACK_I32 = 0, FASTRACK_I64 = 1 };
  * id is padding: its row is 0, and it counts for nothing in the gradient. An id of `rows`
  * or more is a mistake that the device alone can see: its row is NaN.
  *   embedding_grad  dw[i][k] = scale * sum of dy[t][k] over the t with id_t = i, added in
- *                   the order of t (so that it is the same every time) within runs of 32
+ *                   the order of t (so that it is the same every time) within runs of 16
  *                   sorted tokens, and these in their order; added to what d_dw holds
  *                   where accumulate is 1 (32-bit d_dw only). Ids of `rows` or more
  *                   count for nothing.
  * d_work: fastrack_mx_embedding_grad_work_bytes(...) bytes, 16-byte aligned.
- * EINVAL too: more than 2^24 - 1 pieces of 32 tokens and 2048 columns (of the gradient).
+ * EINVAL too: 2^26 pieces of 16 tokens and 512 columns, or more (of the gradient).
  */
 int fastrack_mx_embedding(uint32_t index_type, const void *d_ids, uint64_t m, const uint8_t *d_codes, const uint8_t *d_scales,
                           uint64_t rows, uint64_t cols, float scale, uint32_t type, void *d_y, uint64_t ldy, void *stream);

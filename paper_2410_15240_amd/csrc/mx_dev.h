@@ -16,6 +16,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// A constant as an argument of a lambda.
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
+
 __device__ __forceinline__ float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
 
@@ -32,6 +38,15 @@ template <> struct Elem<kFp32> { typedef float type; };
         else if ((t) == kFp16) { constexpr uint32_t T = kFp16; __VA_ARGS__; }                      \
         else { constexpr uint32_t T = kFp32; __VA_ARGS__; }                                        \
     } while (0)
+
+// This wave's LDS accesses before it come before those after it. (The LDS takes a wave's accesses
+// in order; what is held back is the compiler.)
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
 
 // Elements [c, c + 8) of a row as floats, zero past `cols`. A whole unit is loaded 16 bytes at a
 // time wherever it starts: the hardware takes any alignment.
@@ -52,6 +67,25 @@ __device__ __forceinline__ void load8(const void *base, uint64_t row_off, uint32
             v[i] = c + i < cols ? (float)p[i] : 0.0f;
     }
 }
+
+// Eight elements of a row as they lie in memory.
+template <uint32_t T>
+struct Raw8 {
+    typedef typename Elem<T>::type E;
+    typedef E Ex8 __attribute__((ext_vector_type(8)));
+    Ex8 v;
+    __device__ __forceinline__ void load(const void *base, uint64_t row_off, uint32_t c, uint32_t cols)
+    {
+        const E *p = reinterpret_cast<const E *>(base) + row_off + c;
+        if (c + 8 <= cols) {
+            __builtin_memcpy(&v, p, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                v[i] = c + i < cols ? p[i] : (E)0.0f;
+        }
+    }
+};
 
 // Rounded to the output's type once, to nearest even (what the conversion does).
 template <uint32_t T>

@@ -19,40 +19,60 @@ __device__ __forceinline__ int64_t id_of(const MxIds &ids, uint64_t i)
 
 // ---- lookup ---------------------------------------------------------------------------------
 //
-// A unit of 8 values to a thread, as in mx.hip. What bounds it is the writing of y.
+// A lane loads a block, 16 bytes of codes: with 4 bytes to a lane there is too little on its way to
+// cover the way to memory. (16384 rows of 4096 out of 143 MB, 170 MB in all: 32 us, 5.3 TB/s; with 4 bytes 44.) Four
+// neighbouring lanes hold blocks 16 apart and exchange their words, so that a wave writes 1 KB that
+// lies together at a time, 8 values to a lane.
 constexpr int kThreads = 256;
 
 struct Lookup {
     MxIds ids;
     MxMatrix table;
-    uint32_t rows, cols, per_row, recip, units;
-    uint64_t t0;   // first token of this launch
+    uint32_t rows, cols, nb, recip, blocks;   // blocks of a row; of this launch
+    uint64_t t0;                              // first token of this launch
     float scale;
     MxRows y;
 };
 
+// The value of lane I of each four.
+template <int I>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, I * 0x55, 0xF, 0xF, true);
+}
+
 template <uint32_t T>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(Lookup g)
 {
-    const uint32_t i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= g.units)
+    const uint32_t lane = threadIdx.x & 63, j = lane & 3, first = blockIdx.x * kThreads + threadIdx.x - lane;
+    if (first >= g.blocks)   // a whole wave
         return;
-    const uint32_t r = div_recip(i, g.per_row, g.recip), j = i - r * g.per_row;
-    const uint64_t t = g.t0 + r;
-    const int64_t id = id_of(g.ids, t);
-    float v[8];
+    // (Past the last block it is read again.)
+    const uint32_t at = min(first + j * 16 + lane / 4, g.blocks - 1), r = div_recip(at, g.nb, g.recip);
+    const int64_t id = id_of(g.ids, g.t0 + r);
+    u32x4 codes = {0, 0, 0, 0};
+    uint32_t e = id < 0 ? 127 : 255;   // padding: zeros; no row of the table: NaN
     if (id >= 0 && id < (int64_t)g.rows) {
-        const uint64_t block = (uint64_t)id * ((g.per_row + 3) / 4) + j / 4;
-        decode4_f32(reinterpret_cast<const uint32_t *>(g.table.codes)[block * 4 + j % 4], scale4_f32(g.table.scales[block]), v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] *= g.scale;
-    } else {   // padding; no row of the table
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = id < 0 ? 0.0f : __builtin_nanf("");
+        const uint64_t block = (uint64_t)id * g.nb + (at - r * g.nb);
+        codes = reinterpret_cast<const u32x4 *>(g.table.codes)[block];
+        e = g.table.scales[block];
     }
-    store8<T>(g.y.p, t * g.y.ld, j * 8, g.cols, v);
+    auto put_unit = [&](auto i_) {
+        constexpr int I = decltype(i_)::value;
+        const uint32_t w0 = from_lane<I>(codes[0]), w1 = from_lane<I>(codes[1]), w2 = from_lane<I>(codes[2]), w3 = from_lane<I>(codes[3]);
+        const uint32_t to = first + I * 16 + lane / 4, row = div_recip(to, g.nb, g.recip), c = (to - row * g.nb) * 32 + j * 8;
+        float v[8];
+        decode4_f32(j & 2 ? (j & 1 ? w3 : w2) : (j & 1 ? w1 : w0), scale4_f32(from_lane<I>(e)), v);
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+            v[x] *= g.scale;
+        if (to < g.blocks && c < g.cols)
+            store8<T>(g.y.p, (g.t0 + row) * g.y.ld, c, g.cols, v);
+    };
+    put_unit(Const<0>());
+    put_unit(Const<1>());
+    put_unit(Const<2>());
+    put_unit(Const<3>());
 }
 
 // ---- sorting ids -------------------------------------------------------------------------------
@@ -62,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(Lookup g)
 // wave ranks its 64 keys among equal digits by one vote per bit, and adds what came before
 // them: in its own earlier keys, in the waves before it, and in the blocks before.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr uint32_t kDigits = 256;
+constexpr uint32_t kDigitBits = 9, kDigits = 1u << kDigitBits;
 
 struct Sort {
     MxIds ids;                    // of the first pass; later ones read keys and places
@@ -73,8 +93,8 @@ struct Sort {
     bool first;
 };
 
-constexpr int kItems = 16;        // keys of a thread
-constexpr uint32_t kSortBlock = kSortThreads * kItems;
+constexpr int kMostItems = 16;    // keys of a thread
+constexpr uint32_t kSortBlock = kSortThreads * kMostItems;
 
 __device__ __forceinline__ uint32_t key_of(const MxIds &ids, uint32_t i, uint32_t rows)
 {
@@ -82,41 +102,41 @@ __device__ __forceinline__ uint32_t key_of(const MxIds &ids, uint32_t i, uint32_
     return id >= 0 && id < (int64_t)rows ? (uint32_t)id : rows;
 }
 
-// A wave's keys are 64 * kItems that follow one another, 64 at a time. `counts[digit]` of the wave
-// grows; rank[] is a key's number among the wave's equal digits.
-__device__ __forceinline__ void rank_keys(const uint32_t (&key)[kItems], uint32_t (&rank)[kItems], uint32_t valid, uint32_t shift,
+// A wave's keys are 64 K that follow one another, 64 at a time. `counts[digit]` of the wave grows;
+// rank[] is a key's number among the wave's equal digits.
+template <int K>
+__device__ __forceinline__ void rank_keys(const uint32_t (&key)[K], uint32_t (&rank)[K], uint32_t valid, uint32_t shift,
                                           uint32_t bits, uint32_t *counts)
 {
     const uint32_t lane = threadIdx.x & 63, mask = (1u << bits) - 1;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < K; ++i) {
         if (i * 64u >= valid)   // the whole wave
             break;
         const bool in = i * 64u + lane < valid;
-        const uint32_t d = key[i] >> shift & mask;
-        uint64_t same = __ballot(in);
+        const uint32_t d = key[i] >> shift & mask, so_far = counts[d];
+        const uint64_t all = __ballot(in);
+        uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);   // lanes with the same digit
         for (uint32_t b = 0; b < bits; ++b) {
-            const uint64_t v = __ballot(d >> b & 1);
-            same &= d >> b & 1 ? v : ~v;
+            const int32_t s = (int32_t)(d << (31 - b)) >> 31;
+            const uint64_t v = __ballot(s != 0);
+            lo &= ~((uint32_t)v ^ (uint32_t)s);
+            hi &= ~((uint32_t)(v >> 32) ^ (uint32_t)s);
         }
-        if (in) {
-            rank[i] = counts[d] + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-            if (lane == (uint32_t)(63 - __clzll((long long)same)))   // the last of them
-                counts[d] = rank[i] + 1;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+        rank[i] = so_far + __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+        if (in && lane == (hi ? 63u - (uint32_t)__builtin_clz(hi) : 31u - (uint32_t)__builtin_clz(lo | 1)))   // the last of them
+            counts[d] = rank[i] + 1;
+        wave_fence();
     }
 }
 
 // counts[wave][digit] of a workgroup to where each wave's first key of a digit goes among the
 // workgroup's; total[digit] of thread `digit` is returned. Threads past the digits bring 0.
-__device__ __forceinline__ uint32_t digits_before(uint32_t (*counts)[kDigits], uint32_t *sums, uint32_t &before)
+__device__ __forceinline__ uint32_t digits_before(uint32_t (*counts)[kDigits], uint32_t *sums, uint32_t mask, uint32_t &before)
 {
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     uint32_t total = 0;
-    if (t < kDigits) {
+    if (t <= mask) {
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
             const uint32_t c = counts[w][t];
@@ -139,6 +159,39 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t (*counts)[kDigits], u
     return total;
 }
 
+// Zeros into rows of `width` bytes, by `parts` workgroups: 16 KB each of all bytes as they follow one
+// another (16 bytes to a thread and no loop: 1 GiB in 171 us, 156 in workgroups of 256, 190-250 in
+// loops of as many workgroups as run at once), or a row to a wave, where gaps stay as they are.
+struct Zero {
+    uint8_t *p;
+    uint64_t stride, width, rows;
+    uint32_t parts;
+};
+constexpr uint64_t kZeroPart = kSortThreads * 16;
+
+// The 16-byte pieces first, first + step, ... of p[0, n), and the 16-bit values before and behind the
+// aligned ones.
+__device__ __forceinline__ void zero_bytes(uint8_t *p, uint64_t n, uint64_t first, uint64_t step)
+{
+    const u32x4 zero = {0, 0, 0, 0};
+    const uint64_t align = (16 - reinterpret_cast<uintptr_t>(p) % 16) % 16, head = align < n ? align : n;
+    const uint64_t whole = (n - head) / 16, tail = head + whole * 16, ends = head + (n - tail);
+    for (uint64_t i = first; i < whole; i += step)
+        reinterpret_cast<u32x4 *>(p + head)[i] = zero;
+    for (uint64_t b = first * 2; b < ends; b += step * 2)
+        *reinterpret_cast<uint16_t *>(p + (b < head ? b : tail + (b - head))) = 0;
+}
+
+__device__ __forceinline__ void zero_part(const Zero &z, uint32_t part)
+{
+    if (z.rows == 1) {
+        zero_bytes(z.p, z.width, (uint64_t)part * kSortThreads + threadIdx.x, (uint64_t)z.parts * kSortThreads);
+        return;
+    }
+    for (uint64_t r = part * kSortWaves + threadIdx.x / 64; r < z.rows; r += (uint64_t)z.parts * kSortWaves)
+        zero_bytes(z.p + r * z.stride, z.width, threadIdx.x % 64, 64);
+}
+
 // All passes by one workgroup, up to kSortBlock ids. Keys and places go from pass to pass through
 // LDS.
 struct SortSmall {
@@ -147,69 +200,91 @@ struct SortSmall {
     uint32_t n, rows, bits, passes;   // bits of a digit
 };
 
-struct SortLds {
-    uint32_t key[kSortBlock];
-    uint16_t place[kSortBlock];
-    uint32_t counts[kSortWaves][kDigits];
-    uint32_t base[kDigits];
-    uint32_t sums[kDigits / 64];
+// (64 KB at most: two workgroups to a CU, so that those that write zeros fill the GPU.)
+template <int K>
+union SortLds {
+    uint32_t swap[kSortThreads * K];
+    struct {
+        uint32_t counts[kSortWaves][kDigits];
+        uint32_t base[kDigits];
+        uint32_t sums[kDigits / 64];
+    };
 };
 
-__device__ __forceinline__ void sort_small(const SortSmall &g, SortLds &l)
+template <int K>
+__device__ __forceinline__ void sort_small(const SortSmall &g, SortLds<K> &l)
 {
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const uint32_t per = (g.n + kSortThreads - 1) / kSortThreads * 64, w0 = wave * per;   // keys of a wave
     const uint32_t valid = w0 < g.n ? min(per, g.n - w0) : 0;
-    uint32_t key[kItems], place[kItems], rank[kItems];
+    uint32_t key[K], place[K], to[K];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < K; ++i) {
         const uint32_t at = i * 64 + lane;
         place[i] = w0 + at;
         key[i] = at < valid ? key_of(g.ids, w0 + at, g.rows) : 0;
     }
+    auto swap = [&](uint32_t (&v)[K]) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i * 64 + lane < valid)
+                l.swap[to[i]] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            if (i * 64 + lane < valid)
+                v[i] = l.swap[w0 + i * 64 + lane];
+    };
     for (uint32_t p = 0; p < g.passes; ++p) {
         const uint32_t shift = p * g.bits, mask = (1u << g.bits) - 1;
-        for (uint32_t i = t; i < kSortWaves * kDigits; i += kSortThreads)
-            (&l.counts[0][0])[i] = 0;
         __syncthreads();
-        rank_keys(key, rank, valid, shift, g.bits, l.counts[wave]);
+        for (uint32_t i = t; i < kSortWaves << g.bits; i += kSortThreads)
+            l.counts[i >> g.bits][i & mask] = 0;
+        __syncthreads();
+        rank_keys(key, to, valid, shift, g.bits, l.counts[wave]);
         __syncthreads();
         uint32_t before;
-        digits_before(l.counts, l.sums, before);
+        digits_before(l.counts, l.sums, mask, before);
         if (t < kDigits)
             l.base[t] = before;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kItems; ++i)
-            if (i * 64 + lane < valid) {
-                const uint32_t d = key[i] >> shift & mask, to = l.base[d] + l.counts[wave][d] + rank[i];
-                if (p + 1 < g.passes) {
-                    l.key[to] = key[i];
-                    l.place[to] = (uint16_t)place[i];
-                } else {
-                    g.keys_out[to] = key[i];
-                    g.places_out[to] = place[i];
-                }
-            }
-        __syncthreads();
+        for (int i = 0; i < K; ++i) {
+            const uint32_t d = key[i] >> shift & mask;
+            to[i] += l.base[d] + l.counts[wave][d];
+        }
         if (p + 1 < g.passes) {
-#pragma unroll
-            for (int i = 0; i < kItems; ++i)
-                if (i * 64 + lane < valid) {
-                    key[i] = l.key[w0 + i * 64 + lane];
-                    place[i] = l.place[w0 + i * 64 + lane];
-                }
+            swap(key);
+            swap(place);
         }
     }
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (i * 64 + lane < valid) {
+            g.keys_out[to[i]] = key[i];
+            g.places_out[to[i]] = place[i];
+        }
+}
+
+// Workgroup 0 sorts; the others write zeros meanwhile.
+template <int K>
+__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SortSmall g, Zero z)
+{
+    __shared__ SortLds<K> l;
+    if (blockIdx.x)
+        zero_part(z, blockIdx.x - 1);
+    else
+        sort_small(g, l);
 }
 
 // A pass of many workgroups: the digits of each block counted, the counts added up (digit by
 // digit, block by block), the keys put where they go.
-__device__ __forceinline__ void load_keys(const Sort &g, uint32_t w0, uint32_t valid, uint32_t (&key)[kItems])
+__device__ __forceinline__ void load_keys(const Sort &g, uint32_t w0, uint32_t valid, uint32_t (&key)[kMostItems])
 {
     const uint32_t lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < kMostItems; ++i) {
         const uint32_t at = i * 64 + lane;
         key[i] = at >= valid ? 0 : g.first ? key_of(g.ids, w0 + at, g.rows) : g.keys[w0 + at];
     }
@@ -221,9 +296,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(Sort g)
     __shared__ uint32_t counts[kSortWaves][kDigits];
     __shared__ uint32_t sums[kDigits / 64];
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, mask = (1u << g.bits) - 1;
-    const uint64_t first = (uint64_t)blockIdx.x * kSortBlock + wave * (64 * kItems);
-    const uint32_t w0 = (uint32_t)first, valid = first < g.n ? min(64u * kItems, g.n - w0) : 0;
-    uint32_t key[kItems], rank[kItems];
+    const uint64_t first = (uint64_t)blockIdx.x * kSortBlock + wave * (64 * kMostItems);
+    const uint32_t w0 = (uint32_t)first, valid = first < g.n ? min(64u * kMostItems, g.n - w0) : 0;
+    uint32_t key[kMostItems], rank[kMostItems];
     load_keys(g, w0, valid, key);
     for (uint32_t i = t; i < kSortWaves * kDigits; i += kSortThreads)
         (&counts[0][0])[i] = 0;
@@ -231,7 +306,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(Sort g)
     rank_keys(key, rank, valid, g.shift, g.bits, counts[wave]);
     __syncthreads();
     uint32_t before;
-    const uint32_t total = digits_before(counts, sums, before);
+    const uint32_t total = digits_before(counts, sums, mask, before);
     if (!PUT) {
         if (t <= mask)
             g.counts[(uint64_t)t * g.blocks + blockIdx.x] = total;
@@ -239,7 +314,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(Sort g)
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
+    for (int i = 0; i < kMostItems; ++i)
         if (i * 64 + lane < valid) {
             const uint32_t d = key[i] >> g.shift & mask;
             const uint32_t to = g.counts[(uint64_t)d * g.blocks + blockIdx.x] + counts[wave][d] + rank[i];
@@ -248,10 +323,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_pass_kernel(Sort g)
         }
 }
 
-// Each count becomes the sum of those before it; one workgroup.
-__global__ __launch_bounds__(1024) void sums_before_kernel(uint32_t *counts, uint32_t n)
+// Each count becomes the sum of those before it; one workgroup. The others write zeros meanwhile.
+__global__ __launch_bounds__(1024) void sums_before_kernel(uint32_t *counts, uint32_t n, Zero z)
 {
     __shared__ uint32_t sums[16];
+    if (blockIdx.x) {
+        zero_part(z, blockIdx.x - 1);
+        return;
+    }
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     uint32_t carry = 0;
     for (uint32_t i0 = 0; i0 < n; i0 += 4096) {
@@ -294,120 +373,249 @@ struct Sums {
     const uint32_t *keys, *places;   // sorted
     uint32_t n, rows, cols;
     uint32_t chunks, tiles;          // of kChunk sorted tokens; of kTileCols columns
-    uint32_t type;
     MxRows dy;
     float scale;
     Out out;
     float *parts;                    // [chunks][2][cols]
 };
 
-constexpr uint32_t kChunk = 32, kSumThreads = 256, kTileCols = kSumThreads * 8;
+constexpr uint32_t kChunk = 16, kTileCols = 64 * 8;
 
+template <uint32_t OT>
 __device__ __forceinline__ void put_row(const Out &o, uint64_t row, uint32_t c, uint32_t cols, float (&v)[8], float scale)
 {
+    const uint64_t at = row * o.ld;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         v[e] *= scale;
-    const uint64_t at = row * o.ld;
-    if (o.type == kFp32) {
-        if (o.accumulate) {
-            float w[8];
-            load8<kFp32>(o.p, at, c, cols, w);
+    if (OT == kFp32 && o.accumulate) {
+        float w[8];
+        load8<kFp32>(o.p, at, c, cols, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] += w[e];
+        for (int e = 0; e < 8; ++e)
+            v[e] += w[e];
+    }
+    store8<OT>(o.p, at, c, cols, v);
+}
+
+// Few tokens: no sorting. A workgroup has 16 rows of the table, one to a wave, and 512 columns, looks
+// through all ids for them, and writes its rows once, sums and zeros. Its waves look through a part
+// of the ids each; what they find, one list after the other, is in the order of the tokens.
+constexpr uint32_t kOwnWaves = 16, kOwnMost = 2048;
+constexpr uint32_t kOwnAlone = 8;   // tokens of a row that its wave adds up alone
+
+struct Owned {
+    MxIds ids;
+    uint32_t n, rows, cols, tiles;
+    MxRows dy;
+    float scale;
+    Out out;
+};
+
+template <uint32_t T, uint32_t OT>
+__global__ __launch_bounds__(64 * kOwnWaves, 8) void owned_kernel(Owned g)
+{
+    constexpr int B = T == kFp32 ? 4 : 8;   // rows on their way at once
+    __shared__ uint16_t found[kOwnMost];     // a row of this workgroup's << 11 | the token
+    __shared__ uint16_t some[kOwnWaves][kOwnAlone], many[kOwnMost];   // tokens of a wave's row; of one of more
+    __shared__ uint32_t count[kOwnWaves], total[kOwnWaves];
+    __shared__ float part[kOwnWaves - 1][512];
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t own = blockIdx.x / g.tiles, c = (blockIdx.x - own * g.tiles) * 512 + lane * 8, r0 = own * kOwnWaves;
+    const uint32_t rows = min(kOwnWaves, g.rows - r0);
+    auto before = [&](uint64_t lanes) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0)); };
+    // 64 or 128 ids to a wave.
+    const uint32_t halves = g.n > 64 * kOwnWaves ? 2 : 1;
+    uint32_t entry[2];
+    uint64_t in[2];
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) {
+        const uint32_t at = (wave * halves + h) * 64 + lane;
+        const int64_t r = h < halves && at < g.n ? id_of(g.ids, at) - (int64_t)r0 : -1;
+        in[h] = __ballot(r >= 0 && r < (int64_t)rows);
+        entry[h] = (uint32_t)r << 11 | at;
+    }
+    const uint32_t n0 = (uint32_t)__popcll(in[0]);
+    if (lane == 0)
+        count[wave] = n0 + (uint32_t)__popcll(in[1]);
+    __syncthreads();
+    uint32_t at = 0, all = 0;   // what the waves before found, and all of them
+#pragma unroll
+    for (uint32_t w = 0; w < kOwnWaves; ++w) {
+        at += w < wave ? count[w] : 0;
+        all += count[w];
+    }
+    if (in[0] >> lane & 1)
+        found[at + before(in[0])] = (uint16_t)entry[0];
+    if (in[1] >> lane & 1)
+        found[at + n0 + before(in[1])] = (uint16_t)entry[1];
+    __syncthreads();
+    // The first `most` tokens of row r into a list; how many there are.
+    auto gather = [&](uint32_t r, uint16_t *list, uint32_t most) {
+        uint32_t m = 0;
+        for (uint32_t i = 0; i < all; i += 64) {
+            const uint32_t f = i + lane < all ? found[i + lane] : 0;
+            const uint64_t lanes = __ballot(i + lane < all && f >> 11 == r);
+            const uint32_t to = m + before(lanes);
+            if ((lanes >> lane & 1) && to < most)
+                list[to] = (uint16_t)(f & 2047);
+            m += (uint32_t)__popcll(lanes);
         }
-        store8<kFp32>(o.p, at, c, cols, v);
-    } else if (o.type == kBf16) {
-        store8<kBf16>(o.p, at, c, cols, v);
-    } else {
-        store8<kFp16>(o.p, at, c, cols, v);
+        wave_fence();
+        return m;
+    };
+    auto add = [&](const uint16_t *list, uint32_t from, uint32_t to, float (&sum)[8]) {
+        for (uint32_t i = from; i < to; i += B) {
+            Raw8<T> raw[B];
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                if (i + j < to)
+                    raw[j].load(g.dy.p, list[i + j] * g.dy.ld, c, g.cols);
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                if (i + j < to)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sum[e] += (float)raw[j].v[e];
+        }
+    };
+    uint32_t m = 0;
+    if (wave < rows) {
+        m = gather(wave, some[wave], kOwnAlone);
+        if (lane == 0)
+            total[wave] = m;
+        if (c < g.cols && m <= kOwnAlone && (m || !g.out.accumulate)) {
+            float sum[8] = {};
+            add(some[wave], 0, m, sum);
+            put_row<OT>(g.out, r0 + wave, c, g.cols, sum, g.scale);
+        }
+    }
+    if (all <= kOwnAlone)   // (the whole workgroup)
+        return;
+    __syncthreads();
+    for (uint32_t r = 0; r < rows; ++r) {   // rows of many tokens: a part of them to each wave
+        const uint32_t m = total[r], per = (m + kOwnWaves - 1) / kOwnWaves;
+        if (m <= kOwnAlone)
+            continue;
+        if (wave == 0)
+            gather(r, many, kOwnMost);
+        __syncthreads();
+        float sum[8] = {};
+        if (c < g.cols)
+            add(many, min(m, wave * per), min(m, (wave + 1) * per), sum);
+        if (wave)
+            store8<kFp32>(part[wave - 1], 0, lane * 8, 512, sum);
+        __syncthreads();
+        if (wave == 0 && c < g.cols) {
+#pragma unroll
+            for (uint32_t w = 0; w < kOwnWaves - 1; ++w)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    sum[e] += part[w][lane * 8 + e];
+            put_row<OT>(g.out, r0 + r, c, g.cols, sum, g.scale);
+        }
+        __syncthreads();
     }
 }
 
-// The sums of kChunk sorted tokens, 8 columns to a thread. A sum that lies in the chunk whole is
-// put out; one that goes on from the chunk before is left in part 0, one that begins here and
-// goes on in part 1.
-template <uint32_t T>
-__global__ __launch_bounds__(kSumThreads) void sums_kernel(Sums g)
+// The sums of kChunk sorted tokens, 8 columns to a lane, a wave to a workgroup. All of the tokens' rows
+// are on their way before the first is added. A sum that lies in the chunk whole is put out; one
+// that goes on from the chunk before is left in part 0, one that begins here and goes on in part 1.
+template <uint32_t T, uint32_t OT>
+__global__ __launch_bounds__(64) void sums_kernel(Sums g)
 {
-    const uint32_t chunk = blockIdx.x / g.tiles, c = (blockIdx.x - chunk * g.tiles) * kTileCols + threadIdx.x * 8;
-    const uint32_t begin = chunk * kChunk, end = min(g.n, begin + kChunk);
+    const uint32_t chunk = blockIdx.x / g.tiles, lane = threadIdx.x, c = (blockIdx.x - chunk * g.tiles) * kTileCols + lane * 8;
+    const uint32_t begin = chunk * kChunk, count = min(kChunk, g.n - begin);
+    // Lane i + 1 holds the key of the chunk's token i: the one before it and the one after it too.
+    const uint32_t at = begin + lane - 1;
+    const uint32_t key = lane <= kChunk + 1 && begin + lane > 0 && at < g.n ? g.keys[at] : ~0u;
+    const uint32_t place = lane < count ? g.places[begin + lane] : 0;
+    uint32_t keys[kChunk + 2], places[kChunk];   // (read from all lanes, before any of them leaves)
+#pragma unroll
+    for (int i = 0; i < (int)kChunk + 2; ++i)
+        keys[i] = (uint32_t)__builtin_amdgcn_readlane((int)key, i);
+#pragma unroll
+    for (int i = 0; i < (int)kChunk; ++i)
+        places[i] = (uint32_t)__builtin_amdgcn_readlane((int)place, i);
+    auto key_at = [&](int i) { return keys[i + 1]; };
+    Raw8<T> raw[kChunk];
+    if (c < g.cols)
+#pragma unroll
+        for (int i = 0; i < (int)kChunk; ++i)
+            if (i < (int)count && key_at(i) < g.rows)
+                raw[i].load(g.dy.p, places[i] * g.dy.ld, c, g.cols);
     if (c >= g.cols)
         return;
     float sum[8] = {};
-    bool here = begin == 0 || g.keys[begin] != g.keys[begin - 1];   // whether the running sum began in this chunk
-    for (uint32_t i = begin; i < end; ++i) {
-        const uint32_t key = g.keys[i];
-        if (key >= g.rows)   // sorted last: no row's
-            return;
-        float v[8];
-        load8<T>(g.dy.p, g.places[i] * g.dy.ld, c, g.cols, v);
+    bool here = key_at(-1) != key_at(0);   // whether the running sum began in this chunk
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            sum[e] += v[e];
-        const bool last = i + 1 == g.n || g.keys[i + 1] != key;
-        if (last && here)
-            put_row(g.out, key, c, g.cols, sum, g.scale);
-        else if (last || i + 1 == end)
-            store8<kFp32>(g.parts, ((uint64_t)chunk * 2 + here) * g.cols, c, g.cols, sum);
-        if (last) {
-            here = true;
+    for (int i = 0; i < (int)kChunk; ++i) {
+        if (i < (int)count && key_at(i) < g.rows) {   // (ids that name no row are sorted last)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                sum[e] = 0.0f;
-        }
-    }
-}
-
-// The sums that go on from the chunk in which they began: its part 1, and part 0 of those after.
-__global__ __launch_bounds__(kSumThreads) void join_sums_kernel(Sums g)
-{
-    const uint32_t chunk = blockIdx.x / g.tiles, c = (blockIdx.x - chunk * g.tiles) * kTileCols + threadIdx.x * 8;
-    const uint32_t begin = chunk * kChunk, end = begin + kChunk;
-    if (c >= g.cols || end >= g.n)
-        return;
-    const uint32_t key = g.keys[end - 1];
-    if (key >= g.rows || g.keys[end] != key)
-        return;
-    if (g.keys[begin] == key && begin != 0 && g.keys[begin - 1] == key)
-        return;   // it began before
-    float sum[8], v[8];
-    load8<kFp32>(g.parts, ((uint64_t)chunk * 2 + 1) * g.cols, c, g.cols, sum);
-    for (uint32_t k = chunk + 1; k < g.chunks && g.keys[k * kChunk] == key; ++k) {
-        load8<kFp32>(g.parts, (uint64_t)k * 2 * g.cols, c, g.cols, v);
+                sum[e] += (float)raw[i].v[e];
+            const bool last = key_at(i + 1) != key_at(i);
+            if (last && here)
+                put_row<OT>(g.out, key_at(i), c, g.cols, sum, g.scale);
+            else if (last || i + 1 == (int)kChunk)
+                store8<kFp32>(g.parts, ((uint64_t)chunk * 2 + here) * g.cols, c, g.cols, sum);
+            if (last) {
+                here = true;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            sum[e] += v[e];
-    }
-    put_row(g.out, key, c, g.cols, sum, g.scale);
-}
-
-// Zeros, 16 bytes to a thread and a step, in rows of `width` bytes.
-__global__ __launch_bounds__(kThreads) void zero_kernel(uint8_t *p, uint64_t stride, uint64_t width, uint64_t rows)
-{
-    if (stride == width || rows == 1) {
-        width *= rows;
-        rows = 1;
-    }
-    for (uint64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-        uint8_t *row = p + r * stride;
-        for (uint64_t at = (uint64_t)(blockIdx.x * kThreads + threadIdx.x) * 16; at < width; at += (uint64_t)gridDim.x * kThreads * 16) {
-            if (at + 16 <= width) {
-                const u32x4 zero = {0, 0, 0, 0};
-                __builtin_memcpy(row + at, &zero, 16);
-            } else {
-                for (uint64_t b = at; b < width; b += 2)
-                    *reinterpret_cast<uint16_t *>(row + b) = 0;
+                for (int e = 0; e < 8; ++e)
+                    sum[e] = 0.0f;
             }
         }
     }
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SortSmall g)
+// The sums that go on from the chunk in which they began: its part 1, and part 0 of those after.
+template <uint32_t OT>
+__global__ __launch_bounds__(64) void join_sums_kernel(Sums g)
 {
-    __shared__ SortLds l;
-    sort_small(g, l);
+    const uint32_t chunk = blockIdx.x / g.tiles, c = (blockIdx.x - chunk * g.tiles) * kTileCols + threadIdx.x * 8;
+    const uint32_t begin = chunk * kChunk, end = begin + kChunk;
+    if (end >= g.n)
+        return;
+    const uint32_t key = g.keys[end - 1];
+    if (key >= g.rows || g.keys[end] != key)
+        return;
+    if (begin != 0 && g.keys[begin - 1] == key)
+        return;   // it began before
+    // The chunks that it reaches into: 64 looked at at once.
+    uint32_t last = chunk;
+    for (;;) {
+        const uint64_t k = (uint64_t)last + 1 + threadIdx.x;
+        const uint32_t more = (uint32_t)__builtin_ctzll(~__ballot(k < g.chunks && g.keys[k * kChunk] == key) | 1ull << 63);
+        const bool all = more == 63 && last + 64 < g.chunks && g.keys[(uint64_t)(last + 64) * kChunk] == key;
+        last += all ? 64 : more;
+        if (!all)
+            break;
+    }
+    if (c >= g.cols)
+        return;
+    float sum[8];
+    load8<kFp32>(g.parts, ((uint64_t)chunk * 2 + 1) * g.cols, c, g.cols, sum);
+    uint32_t k = chunk + 1;
+    for (; k + 8 <= last + 1; k += 8) {   // 8 on their way at once, added in their order
+        float v[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            load8<kFp32>(g.parts, (uint64_t)(k + i) * 2 * g.cols, c, g.cols, v[i]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                sum[e] += v[i][e];
+    }
+    for (; k <= last; ++k) {
+        float v[8];
+        load8<kFp32>(g.parts, (uint64_t)k * 2 * g.cols, c, g.cols, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sum[e] += v[e];
+    }
+    put_row<OT>(g.out, key, c, g.cols, sum, g.scale);
 }
 
 }  // namespace mx
@@ -423,14 +631,14 @@ hipError_t launch_mx_embedding(const Embedding &e, hipStream_t s)
     g.table = e.table;
     g.rows = (uint32_t)e.rows;
     g.cols = (uint32_t)e.cols;
-    g.per_row = (uint32_t)((e.cols + 7) / 8);
-    g.recip = div_recip_of(g.per_row);
+    g.nb = (uint32_t)mx_blocks(e.cols);
+    g.recip = div_recip_of(g.nb);
     g.scale = e.scale;
     g.y = e.y;
-    const uint64_t most = 0xFFFFFF00u / g.per_row;
+    const uint64_t most = 0xFFFFFF00u / g.nb;
     for (g.t0 = 0; g.t0 < e.m; g.t0 += most) {
-        g.units = (uint32_t)((e.m - g.t0 < most ? e.m - g.t0 : most) * g.per_row);
-        MX_TYPE(e.type, hipLaunchKernelGGL((lookup_kernel<T>), dim3((g.units + kThreads - 1) / kThreads), dim3(kThreads), 0, s, g));
+        g.blocks = (uint32_t)((e.m - g.t0 < most ? e.m - g.t0 : most) * g.nb);
+        MX_TYPE(e.type, hipLaunchKernelGGL((lookup_kernel<T>), dim3((g.blocks + kThreads - 1) / kThreads), dim3(kThreads), 0, s, g));
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess)
             return err;
@@ -439,6 +647,8 @@ hipError_t launch_mx_embedding(const Embedding &e, hipStream_t s)
 }
 
 namespace {
+
+constexpr uint64_t kMostParts = (1u << 22) - 2;   // workgroups of 1024 threads: fewer than 2^32 of these
 
 uint64_t round16(uint64_t v) { return (v + 15) / 16 * 16; }
 
@@ -455,7 +665,7 @@ GradPlan plan_of(uint64_t m, uint64_t rows, uint64_t cols)
     uint32_t bits = 1;
     while (rows >> bits)
         ++bits;
-    p.passes = (bits + 7) / 8;
+    p.passes = (bits + kDigitBits - 1) / kDigitBits;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.small = m <= kSortBlock;
     p.blocks = (uint32_t)((m + kSortBlock - 1) / kSortBlock);
@@ -466,29 +676,58 @@ GradPlan plan_of(uint64_t m, uint64_t rows, uint64_t cols)
     return p;
 }
 
+// Whether few tokens' gradient goes without sorting: where no row has many of them on average, and few
+// workgroups have to look through the ids. (us sorted, owned, bf16: 1001 tokens, 5003 x 1111: 22.6, 13.7; 2048
+// tokens, 5003 x 1111: 28.9, 18.4; 1 token, 32768 x 512, 2048 workgroups: 13.6, 17.4; 1001 tokens, 20000 x 1024, 2500
+// workgroups: 23.0, 23.6; 500 and 2048 tokens, 100 x 4096: 14.1, 11.2 and 17.4, 31.7.)
+bool owned(uint64_t m, uint64_t rows, uint64_t cols)
+{
+    return m && m <= kOwnMost && m <= 8 * rows && (rows + kOwnWaves - 1) / kOwnWaves * ((cols + 511) / 512) <= 1536;
+}
+
 }  // namespace
 
 uint64_t mx_embedding_grad_work(uint64_t m, uint64_t rows, uint64_t cols)
 {
-    return m && rows && cols ? plan_of(m, rows, cols).bytes() : 0;
+    return m && rows && cols && !owned(m, rows, cols) ? plan_of(m, rows, cols).bytes() : 0;
 }
 
-hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, int num_cu, hipStream_t s)
+hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
 {
     if (e.rows == 0 || e.cols == 0)
         return hipSuccess;
     hipError_t err;
-    if (!e.accumulate) {
-        const uint64_t size = mx_type_size(e.otype), width = e.cols * size;
-        const bool whole = e.dw.ld == e.cols || e.rows == 1;
-        const uint64_t units = ((whole ? width * e.rows : width) + 16 * kThreads - 1) / (16 * kThreads);
-        const uint32_t gx = (uint32_t)(units < 16u * num_cu ? units : 16u * num_cu), gy = whole ? 1 : (uint32_t)(e.rows < 8192 ? e.rows : 8192);
-        hipLaunchKernelGGL(zero_kernel, dim3(gx, gy), dim3(kThreads), 0, s, reinterpret_cast<uint8_t *>(e.dw.p), e.dw.ld * size, width, e.rows);
-        if ((err = hipGetLastError()) != hipSuccess)
-            return err;
+    if (owned(e.m, e.rows, e.cols)) {
+        Owned g = {};
+        g.ids = e.ids;
+        g.n = (uint32_t)e.m;
+        g.rows = (uint32_t)e.rows;
+        g.cols = (uint32_t)e.cols;
+        g.tiles = (uint32_t)((e.cols + 511) / 512);
+        g.dy = e.dy;
+        g.scale = e.scale;
+        g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate};
+        const dim3 grid((uint32_t)((e.rows + kOwnWaves - 1) / kOwnWaves) * g.tiles);
+        MX_TYPE(e.type, {
+            constexpr uint32_t D = T;
+            MX_TYPE(e.otype, hipLaunchKernelGGL((owned_kernel<D, T>), grid, dim3(64 * kOwnWaves), 0, s, g));
+        });
+        return hipGetLastError();
     }
-    if (e.m == 0)
-        return hipSuccess;
+    Zero z = {};
+    if (!e.accumulate) {
+        const uint64_t size = mx_type_size(e.otype);
+        const bool whole = e.dw.ld == e.cols || e.rows == 1;
+        z = {reinterpret_cast<uint8_t *>(e.dw.p), e.dw.ld * size, (whole ? e.rows : 1) * e.cols * size, whole ? 1 : e.rows, 0};
+        const uint64_t parts = whole ? (z.width + kZeroPart - 1) / kZeroPart : (z.rows + kSortWaves - 1) / kSortWaves;
+        z.parts = (uint32_t)(parts < kMostParts ? parts : kMostParts);
+    }
+    if (e.m == 0) {
+        if (!z.parts)
+            return hipSuccess;
+        hipLaunchKernelGGL(sums_before_kernel, dim3(1 + z.parts), dim3(1024), 0, s, nullptr, 0, z);
+        return hipGetLastError();
+    }
     const GradPlan p = plan_of(e.m, e.rows, e.cols);
     uint8_t *at = reinterpret_cast<uint8_t *>(e.work);
     uint32_t *keys[2], *places[2];
@@ -500,7 +739,13 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, int num_cu, hipStrea
     int in = 0;
     if (p.small) {
         const SortSmall g = {e.ids, keys[0], places[0], (uint32_t)e.m, (uint32_t)e.rows, p.bits, p.passes};
-        hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSortThreads), 0, s, g);
+        const dim3 grid(1 + z.parts);
+        if (e.m <= kSortThreads)
+            hipLaunchKernelGGL((sort_small_kernel<1>), grid, dim3(kSortThreads), 0, s, g, z);
+        else if (e.m <= 4 * kSortThreads)
+            hipLaunchKernelGGL((sort_small_kernel<4>), grid, dim3(kSortThreads), 0, s, g, z);
+        else
+            hipLaunchKernelGGL((sort_small_kernel<kMostItems>), grid, dim3(kSortThreads), 0, s, g, z);
         if ((err = hipGetLastError()) != hipSuccess)
             return err;
     } else {
@@ -521,7 +766,8 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, int num_cu, hipStrea
             hipLaunchKernelGGL((sort_pass_kernel<false>), dim3(p.blocks), dim3(kSortThreads), 0, s, g);
             if ((err = hipGetLastError()) != hipSuccess)
                 return err;
-            hipLaunchKernelGGL(sums_before_kernel, dim3(1), dim3(1024), 0, s, g.counts, p.blocks << p.bits);
+            const uint32_t zeros = pass == 0 ? z.parts : 0;
+            hipLaunchKernelGGL(sums_before_kernel, dim3(1 + zeros), dim3(1024), 0, s, g.counts, p.blocks << p.bits, z);
             if ((err = hipGetLastError()) != hipSuccess)
                 return err;
             hipLaunchKernelGGL((sort_pass_kernel<true>), dim3(p.blocks), dim3(kSortThreads), 0, s, g);
@@ -543,10 +789,13 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, int num_cu, hipStrea
     g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate};
     g.parts = reinterpret_cast<float *>(at);
     const dim3 grid(g.chunks * g.tiles);
-    MX_TYPE(e.type, hipLaunchKernelGGL((sums_kernel<T>), grid, dim3(kSumThreads), 0, s, g));
+    MX_TYPE(e.type, {
+        constexpr uint32_t D = T;
+        MX_TYPE(e.otype, hipLaunchKernelGGL((sums_kernel<D, T>), grid, dim3(64), 0, s, g));
+    });
     if ((err = hipGetLastError()) != hipSuccess || g.chunks == 1)
         return err;
-    hipLaunchKernelGGL(join_sums_kernel, grid, dim3(kSumThreads), 0, s, g);
+    MX_TYPE(e.otype, hipLaunchKernelGGL((join_sums_kernel<T>), grid, dim3(64), 0, s, g));
     return hipGetLastError();
 }
 

@@ -7,12 +7,6 @@
 namespace fastrack {
 namespace mx {
 
-// A constant as an argument of a lambda.
-template <int V>
-struct Const {
-    static constexpr int value = V;
-};
-
 // 16-byte chunk c of row r of a tile whose rows are 128 bytes: bits 1 to 3 of the row turn the
 // chunk's place, so that one chunk of 16 rows in turn lies in all 64 banks, once in each.
 __device__ __forceinline__ uint32_t at_k(uint32_t r, uint32_t c) { return r * 128 + ((c ^ ((r >> 1) & 7)) << 4); }
@@ -82,15 +76,6 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ __forceinline__ Buffer buffer_at(const void *p)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0xFFFFFFFFu, 0x00027000);
-}
-
-// This wave's LDS accesses before it come before those after it. (The LDS takes a wave's accesses
-// in order; what is held back is the compiler.)
-__device__ __forceinline__ void wave_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
 // All waves' LDS accesses before it are done. (Loads from memory may still be on their way.)

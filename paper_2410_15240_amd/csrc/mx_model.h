@@ -63,7 +63,7 @@ struct EmbeddingGrad {
     void *work;
 };
 uint64_t mx_embedding_grad_work(uint64_t m, uint64_t rows, uint64_t cols);
-hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, int num_cu, hipStream_t s);
+hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s);
 
 // z = scale * x w^T [m, n]; lse = log sum exp z, loss = lse - z[id]; and from dloss the gradients
 // dx [m, k] and dw [n, k] = scale dz^T x8.

@@ -237,15 +237,15 @@ FT_EXPORT int fastrack_mx_embedding_grad(uint32_t index_type, const void *d_ids,
     FT_TRY(check_ids(d_ids, index_type, m));
     FT_TRY(check_rows("d_dy", d_dy, ld_dy, m, cols, type, false));
     FT_TRY(check_rows("d_dw", d_dw, ld_dw, rows, cols, out_type, true));
-    if ((m + 31) / 32 * ((cols + 2047) / 2048) > kMostPieces)
-        return fail(FASTRACK_EINVAL, "more than 2^24 - 1 pieces of 32 tokens and 2048 columns");
+    if ((m + 15) / 16 * ((cols + 511) / 512) >= 1ull << 26)   // waves: fewer than 2^32 threads
+        return fail(FASTRACK_EINVAL, "2^26 pieces of 16 tokens and 512 columns, or more");
     const uint64_t need = mx_embedding_grad_work(m, rows, cols);
     FT_TRY(check_work(d_work, work_bytes, need));
     FT_TRY(check_apart<2, 2>({rows_span("d_dw", d_dw, ld_dw, rows, cols, out_type), work_span(d_work, need)},
                              {ids_span(d_ids, index_type, m), rows_span("d_dy", d_dy, ld_dy, m, cols, type)}));
     const EmbeddingGrad e = {{d_ids, index_type}, type, {mut(d_dy), ld_dy}, m, rows, cols, scale, out_type, {d_dw, ld_dw},
                              accumulate != 0, d_work};
-    return done(launch_mx_embedding_grad(e, num_cu(), as_stream(stream)), "embedding gradient launch");
+    return done(launch_mx_embedding_grad(e, as_stream(stream)), "embedding gradient launch");
 }
 
 namespace {

@@ -14,7 +14,7 @@ namespace mx {
 // A row is shared by G threads: unit j of 8 columns belongs to thread j % G, U of them to a thread,
 // which stay in its registers from the row's sum to its end. U = 0: rows of any length, read again
 // after each sum.
-template <int G> constexpr int threads_of() { return G < 256 ? 256 : G; }
+template <int G> constexpr int threads_of() { return G < 128 ? 256 : G; }
 
 // The sum over the G threads of a row, to all of them. `slot` takes turns between 0 and 1: what one
 // sum leaves in LDS is read until the next one's barrier.
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
 }
 
 // How rows of a length are shared out. (Measured choices stand at the launches.)
-enum Way : int { kWave, k256x1, k256x2, k256x4, k1024x1, k1024x2, k1024x4, kLoop };
+enum Way : int { kWave1, kWave, k128x1, k256x1, k256x2, k256x4, k512x1, k1024x1, k1024x2, k1024x4, kLoop };
 
 // ---- backwards -----------------------------------------------------------------------------------
 //
@@ -169,153 +169,246 @@ enum Way : int { kWave, k256x1, k256x2, k256x4, k1024x1, k1024x2, k1024x4, kLoop
 //   db = scale dh',  dg = db (v w1),  db *= g,  dw1 += db v
 //   dx = inv1 (db w1 - v mean(db w1 v))
 // A group takes every P-th row and adds up its rows' parts of dw2 and dw1, in registers; the groups'
-// sums are added in their order by columns_kernel.
+// sums are added in their order by columns_kernel. The next row is on its way from memory while
+// one is worked on.
+
+// What a thread reads of a row, as it lies in memory.
+template <uint32_t T>
+struct GradRow {
+    Raw8<T> dy, dh;
+    u32x2 u, v, g;
+    uint8_t eu, ev, eg;
+};
+
 template <uint32_t T, int G, int U>
-__global__ __launch_bounds__(threads_of<G>()) void norm_grad_kernel(NormGrad n, uint32_t groups)
+__global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad n, uint32_t groups)
 {
-    constexpr int N = U ? U : 1, R = threads_of<G>() / G;
+    constexpr int R = threads_of<G>() / G;
+    constexpr bool AHEAD = U == 1;   // (two units leave no registers for a second row, nor for the weights)
     __shared__ float lds[2][16];
     const uint32_t t = threadIdx.x % G, cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols));
     const uint32_t group = blockIdx.x * R + threadIdx.x / G;
     if (group >= groups)
         return;
     auto each = [&](auto f) {
-        if (U) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (t + i * G < units)
-                    f(i, t + i * G);
-        } else {
-            for (uint32_t j = t; j < units; j += G)
-                f(0, j);
-        }
+        for (int i = 0; i < U; ++i)
+            if (t + i * G < units)
+                f(i, t + i * G);
     };
-    float *const part2 = n.work + (uint64_t)group * cols, *const part1 = part2 + (uint64_t)groups * cols;
-    float sum2[N][8] = {}, sum1[N][8] = {};
-    auto flush = [&](uint32_t j, float *part, float (&s)[8], bool add) {
-        if (add) {
-            float old[8];
-            load8<kFp32>(part, 0, j * 8, cols, old);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                s[e] += old[e];
-        }
-        store8<kFp32>(part, 0, j * 8, cols, s);
+    float sum2[U][8] = {}, sum1[U][8] = {}, w2[U][8], w1[U][8];
+    auto weights = [&](int i, uint32_t j) {
+        weights8<T>(n.w2, n.wtype, j * 8, cols, w2[i]);
+        if (n.w1)
+            weights8<T>(n.w1, n.wtype, j * 8, cols, w1[i]);
     };
-    bool first = true;
-    for (uint64_t row = group; row < n.rows; row += groups, first = false) {
-        float d[N][8], a[N][8];   // dy w2 and then what goes on; u and then v
-        const float inv2 = n.inv2[row];
-        float s = 0.0f;
-        auto begin = [&](int i, uint32_t j, bool sums) {
+    if (AHEAD)
+        each(weights);
+    auto fetch_first = [&](uint64_t row, GradRow<T> (&r)[U]) {
+        each([&](int i, uint32_t j) {
             const Unit u = unit_at(row, j, units);
-            float w[8];
-            load8<T>(n.dy.p, row * n.dy.ld, u.c, cols, d[i]);
-            get<kMx8>(n.u, u, a[i]);
-            weights8<T>(n.w2, n.wtype, u.c, cols, w);
+            r[i].dy.load(n.dy.p, row * n.dy.ld, u.c, cols);
+            r[i].u = reinterpret_cast<const u32x2 *>(n.u.codes)[u.block * 4 + u.lane];
+            r[i].eu = n.u.scales[u.block];
+        });
+    };
+    auto fetch_others = [&](uint64_t row, GradRow<T> (&r)[U]) {
+        each([&](int i, uint32_t j) {
+            const Unit u = unit_at(row, j, units);
+            if (n.dh.p)
+                r[i].dh.load(n.dh.p, row * n.dh.ld, u.c, cols);
+            if (n.v.codes) {
+                r[i].v = reinterpret_cast<const u32x2 *>(n.v.codes)[u.block * 4 + u.lane];
+                r[i].ev = n.v.scales[u.block];
+            }
+            if (n.gq.codes) {
+                r[i].g = reinterpret_cast<const u32x2 *>(n.gq.codes)[u.block * 4 + u.lane];
+                r[i].eg = n.gq.scales[u.block];
+            }
+        });
+    };
+    GradRow<T> now[U], next[U];
+    if (AHEAD && group < n.rows) {
+        fetch_first(group, now);
+        fetch_others(group, now);
+    }
+    for (uint64_t row = group; row < n.rows; row += groups) {
+        const float inv2 = n.inv2[row], inv1 = n.w1 ? n.inv1[row] : 0.0f;
+        if (!AHEAD) {
+            fetch_first(row, now);
+        } else if (row + groups < n.rows) {
+            fetch_first(row + groups, next);
+            fetch_others(row + groups, next);
+        }
+        float d[U][8], a[U][8];   // dy w2 and then what goes on; u and then v
+        float s = 0.0f;
+        each([&](int i, uint32_t j) {
+            if (!AHEAD)
+                weights8<T>(n.w2, n.wtype, j * 8, cols, w2[i]);
+            decode8_f32(now[i].u, scale8_f32(now[i].eu), a[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (sums)
-                    sum2[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum2[i][e]);
-                d[i][e] *= w[e];
-            }
-        };
-        each([&](int i, uint32_t j) {
-            if (!U)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    sum2[i][e] = 0.0f;
-            begin(i, j, true);
-            if (!U)
-                flush(j, part2, sum2[i], !first);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
+                d[i][e] = (float)now[i].dy.v[e];
+                sum2[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum2[i][e]);
+                d[i][e] *= w2[i][e];
                 s = __builtin_fmaf(d[i][e], a[i][e], s);
+            }
         });
         const float along2 = row_sum<G>(s, lds, 0) / (float)cols;
+        if (!AHEAD)
+            fetch_others(row, now);
         s = 0.0f;
-        // The gradient of b, and of what comes before it.
-        auto middle = [&](int i, uint32_t j, bool put_out) {
-            const Unit u = unit_at(row, j, units);
-            float f[8];
-            if (!U)
-                begin(i, j, false);
+        each([&](int i, uint32_t j) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < 8; ++e) {
                 d[i][e] = inv2 * __builtin_fmaf(-along2, a[i][e], d[i][e]);
-            if (n.dh.p) {
-                load8<T>(n.dh.p, row * n.dh.ld, u.c, cols, f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    d[i][e] += f[e];
+                if (n.dh.p)
+                    d[i][e] += (float)now[i].dh.v[e];
             }
-            if (put_out && n.dr.p)
-                store8<T>(n.dr.p, row * n.dr.ld, u.c, cols, d[i]);
+            if (n.dr.p)
+                store8<T>(n.dr.p, row * n.dr.ld, j * 8, cols, d[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 d[i][e] *= n.scale;
-            float w[8];
             if (n.v.codes)
-                get<kMx8>(n.v, u, a[i]);
-            if (n.w1)
-                weights8<T>(n.w1, n.wtype, u.c, cols, w);
+                decode8_f32(now[i].v, scale8_f32(now[i].ev), a[i]);
+            if (!AHEAD && n.w1)
+                weights8<T>(n.w1, n.wtype, j * 8, cols, w1[i]);
             if (n.gq.codes) {
-                float g[8];
+                float f[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    f[e] = d[i][e] * (n.w1 ? a[i][e] * w[e] : a[i][e]);
-                if (put_out)
-                    store8<T>(n.dg.p, row * n.dg.ld, u.c, cols, f);
-                get<kMx8>(n.gq, u, g);
+                    f[e] = d[i][e] * (n.w1 ? a[i][e] * w1[i][e] : a[i][e]);
+                store8<T>(n.dg.p, row * n.dg.ld, j * 8, cols, f);
+                decode8_f32(now[i].g, scale8_f32(now[i].eg), f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    d[i][e] *= g[e];
+                    d[i][e] *= f[e];
             }
-            if (n.w1)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (put_out)
-                        sum1[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum1[i][e]);
-                    d[i][e] *= w[e];
-                }
-        };
-        each([&](int i, uint32_t j) {
-            if (!U)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    sum1[i][e] = 0.0f;
-            middle(i, j, true);
             if (!n.w1) {
                 store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d[i]);
                 return;
             }
-            if (!U)
-                flush(j, part1, sum1[i], !first);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
+            for (int e = 0; e < 8; ++e) {
+                sum1[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum1[i][e]);
+                d[i][e] *= w1[i][e];
                 s = __builtin_fmaf(d[i][e], a[i][e], s);
+            }
         });
-        if (!n.w1) {
-            if (G > 64)
-                __syncthreads();   // (the next row's sum goes to the same place of the LDS)
-            continue;
+        if (n.w1) {
+            const float along1 = row_sum<G>(s, lds, 1) / (float)cols;
+            each([&](int i, uint32_t j) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[i][e] = inv1 * __builtin_fmaf(-along1, a[i][e], d[i][e]);
+                store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d[i]);
+            });
+        } else if (G > 64) {
+            __syncthreads();   // (the next row's sum goes to the same place of the LDS)
         }
-        const float along1 = row_sum<G>(s, lds, 1) / (float)cols, inv1 = n.inv1[row];
-        each([&](int i, uint32_t j) {
-            if (!U)
-                middle(i, j, false);
+        if (AHEAD)
+            now[0] = next[0];
+    }
+    float *const part2 = n.work + (uint64_t)group * cols, *const part1 = part2 + (uint64_t)groups * cols;
+    each([&](int i, uint32_t j) {
+        store8<kFp32>(part2, 0, j * 8, cols, sum2[i]);
+        if (n.w1)
+            store8<kFp32>(part1, 0, j * 8, cols, sum1[i]);
+    });
+}
+
+// Rows of any length: read again after each sum, and a group's sums of dw2 and dw1 kept in its part of
+// the workspace.
+template <uint32_t T>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGrad n, uint32_t groups)
+{
+    __shared__ float lds[2][16];
+    const uint32_t cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols)), group = blockIdx.x;
+    float *const part2 = n.work + (uint64_t)group * cols, *const part1 = part2 + (uint64_t)groups * cols;
+    auto add = [&](float *part, uint32_t j, const float (&x)[8], const float (&y)[8], bool first) {
+        float s[8] = {};
+        if (!first)
+            load8<kFp32>(part, 0, j * 8, cols, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            s[e] = __builtin_fmaf(x[e], y[e], s[e]);
+        store8<kFp32>(part, 0, j * 8, cols, s);
+    };
+    bool first = true;
+    for (uint64_t row = group; row < n.rows; row += groups, first = false) {
+        const float inv2 = n.inv2[row], inv1 = n.w1 ? n.inv1[row] : 0.0f;
+        float along2 = 0.0f, d[8], a[8], w[8], s = 0.0f;
+        auto begin = [&](uint32_t j, bool sums) {   // d = dy w2, a = u
+            const Unit u = unit_at(row, j, units);
+            load8<T>(n.dy.p, row * n.dy.ld, u.c, cols, d);
+            get<kMx8>(n.u, u, a);
+            weights8<T>(n.w2, n.wtype, u.c, cols, w);
+            if (sums)
+                add(part2, j, d, a, first);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                d[i][e] = inv1 * __builtin_fmaf(-along1, a[i][e], d[i][e]);
-            store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d[i]);
-        });
-    }
-    if (U)
-        each([&](int i, uint32_t j) {
-            flush(j, part2, sum2[i], false);
+                d[e] *= w[e];
+        };
+        auto middle = [&](uint32_t j, bool out) {   // d = db, without w1; a = v; w = w1
+            const Unit u = unit_at(row, j, units);
+            float f[8] = {};
+            begin(j, false);
+            if (n.dh.p)
+                load8<T>(n.dh.p, row * n.dh.ld, u.c, cols, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                d[e] = inv2 * __builtin_fmaf(-along2, a[e], d[e]) + f[e];
+            if (out && n.dr.p)
+                store8<T>(n.dr.p, row * n.dr.ld, u.c, cols, d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                d[e] *= n.scale;
+            if (n.v.codes)
+                get<kMx8>(n.v, u, a);
             if (n.w1)
-                flush(j, part1, sum1[i], false);
-        });
+                weights8<T>(n.w1, n.wtype, u.c, cols, w);
+            if (n.gq.codes) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    f[e] = d[e] * (n.w1 ? a[e] * w[e] : a[e]);
+                if (out)
+                    store8<T>(n.dg.p, row * n.dg.ld, u.c, cols, f);
+                get<kMx8>(n.gq, u, f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[e] *= f[e];
+            }
+        };
+        for (uint32_t j = threadIdx.x; j < units; j += 1024) {
+            begin(j, true);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s = __builtin_fmaf(d[e], a[e], s);
+        }
+        along2 = row_sum<1024>(s, lds, 0) / (float)cols;
+        s = 0.0f;
+        for (uint32_t j = threadIdx.x; j < units; j += 1024) {
+            middle(j, true);
+            if (!n.w1) {
+                store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d);
+                continue;
+            }
+            add(part1, j, d, a, first);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s = __builtin_fmaf(d[e] * w[e], a[e], s);
+        }
+        const float along1 = row_sum<1024>(s, lds, 1) / (float)cols;
+        if (n.w1)
+            for (uint32_t j = threadIdx.x; j < units; j += 1024) {
+                middle(j, false);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[e] = inv1 * __builtin_fmaf(-along1, a[e], d[e] * w[e]);
+                store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d);
+            }
+    }
 }
 
 // Sums of 64 columns of `parts` rows, always in the same order: a wave takes every 16th row, the
@@ -391,14 +484,14 @@ hipError_t launch_mx_norm(const Norm &n, int num_cu, hipStream_t s)
 static Way backward_way(uint64_t cols)
 {
     const uint64_t units = 4 * mx_blocks(cols);
-    return units <= 128 ? kWave : units <= 256 ? k256x1 : units <= 512 ? k256x2 : units <= 1024 ? k1024x1 : units <= 2048 ? k1024x2 : kLoop;
+    return units <= 64 ? kWave1 : units <= 128 ? k128x1 : units <= 256 ? k256x1 : units <= 512 ? k512x1 : units <= 1024 ? k1024x1 : units <= 2048 ? k1024x2 : kLoop;
 }
 
-// Groups that take the rows in turn: as many as run at once.
+// Groups that take the rows in turn: as many as run at once, 16 waves to a CU.
 static uint32_t groups_of(uint64_t rows, uint64_t cols, int num_cu)
 {
     const Way way = backward_way(cols);
-    const uint64_t most = (uint64_t)num_cu * (way == kWave ? 16 : way == k256x1 || way == k256x2 ? 4 : 1);
+    const uint64_t most = (uint64_t)num_cu * (way == kWave1 ? 16 : way == k128x1 ? 8 : way == k256x1 ? 4 : way == k512x1 ? 2 : 1);
     return (uint32_t)(rows < most ? rows : most);
 }
 
@@ -417,12 +510,13 @@ hipError_t launch_mx_norm_grad(const NormGrad &n, int num_cu, hipStream_t s)
     MX_TYPE(n.type, hipLaunchKernelGGL((norm_grad_kernel<T, G, U>), dim3((groups * G + threads_of<G>() - 1) / threads_of<G>()), \
                                        dim3(threads_of<G>()), 0, s, n, groups))
         switch (backward_way(n.cols)) {
-        case kWave: NORM(64, 2); break;
+        case kWave1: NORM(64, 1); break;
+        case k128x1: NORM(128, 1); break;
         case k256x1: NORM(256, 1); break;
-        case k256x2: NORM(256, 2); break;
+        case k512x1: NORM(512, 1); break;
         case k1024x1: NORM(1024, 1); break;
         case k1024x2: NORM(1024, 2); break;
-        default: NORM(1024, 0); break;
+        default: MX_TYPE(n.type, hipLaunchKernelGGL((norm_grad_long_kernel<T>), dim3(groups), dim3(1024), 0, s, n, groups)); break;
         }
 #undef NORM
         const hipError_t e = hipGetLastError();

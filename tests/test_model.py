@@ -67,7 +67,8 @@ def test_workspaces(L):
     assert L.fastrack_mx_norm_grad_work_bytes(0, 100, 1) == 0
     assert L.fastrack_mx_norm_grad_work_bytes(1 << 30, 8192, 1) <= 2 * 4 * 8192 * 8192
     assert L.fastrack_mx_embedding_grad_work_bytes(0, 10, 10) == 0
-    assert L.fastrack_mx_embedding_grad_work_bytes(20, 10, 10) == 160
+    assert L.fastrack_mx_embedding_grad_work_bytes(20, 10, 10) == 0
+    assert L.fastrack_mx_embedding_grad_work_bytes(3000, 10, 10) == 2 * 12000 + 188 * 2 * 40
     assert L.fastrack_mx_embedding_grad_work_bytes(1 << 31, 10, 10) == 0
     assert L.fastrack_mx_loss_work_bytes(BF16, AT[0], 4096, 0, 1000, 4096) == 0
     # The logits of a large batch are never all there.
@@ -130,14 +131,14 @@ def test_embedding_refuses(L, kw):
     assert refused(L, embedding(L, **kw))
 
 
-def embedding_grad(L, itype=1, ids=AT[0], type=BF16, dy=AT[1], ld=64, m=4, rows=10, cols=64, scale=1.0, otype=FP32, dw=AT[2], ldw=64, acc=0,
+def embedding_grad(L, itype=1, ids=AT[0], type=BF16, dy=AT[1], ld=64, m=3000, rows=10, cols=64, scale=1.0, otype=FP32, dw=AT[2], ldw=64, acc=0,
                    work=AT[3], size=1 << 20):
     return L.fastrack_mx_embedding_grad(itype, ids, type, dy, ld, m, rows, cols, scale, otype, dw, ldw, acc, work, size, None)
 
 
 @pytest.mark.parametrize("kw", [dict(itype=2), dict(ids=None), dict(ids=AT[0] + 4), dict(type=3), dict(otype=3), dict(dy=None),
                                 dict(dy=AT[1] + 1), dict(m=1 << 31), dict(rows=1 << 31), dict(dw=None), dict(ldw=63), dict(acc=2),
-                                dict(acc=1, otype=BF16), dict(work=None), dict(work=AT[3] + 8), dict(size=31), dict(dw=AT[1]), dict(dw=AT[0]),
+                                dict(acc=1, otype=BF16), dict(work=None), dict(work=AT[3] + 8), dict(size=12031), dict(dw=AT[1]), dict(dw=AT[0]),
                                 dict(work=AT[2] + 16), dict(m=(1 << 29), cols=2049, ldw=2049, ld=0, size=1 << 62)])
 def test_embedding_grad_refuses(L, kw):
     assert refused(L, embedding_grad(L, **kw))
