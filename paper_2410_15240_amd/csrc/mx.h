@@ -26,6 +26,12 @@ struct MxRows {
     uint64_t ld;
 };
 
+// Ids of rows, 4 or 8 bytes each.
+struct MxIds {
+    const void *p;
+    uint32_t wide;
+};
+
 struct MxMatrix {
     uint8_t *codes;
     uint8_t *scales;
@@ -59,6 +65,10 @@ struct MxProduct {
     bool accumulate;        // c += (fp32 only)
     void *work;
     uint64_t work_bytes;
+    // Where a is bf16 terms already, in rows of ld values (a multiple of 8) that end in zeros: how many,
+    // and the elements between them. type is kBf16.
+    uint32_t terms;
+    uint64_t plane;
 };
 
 // Workspace that a product needs: the parts of a long sum, and a's bf16 terms where a is not

@@ -25,6 +25,11 @@ struct Const {
 __device__ __forceinline__ float bits_f32(uint32_t u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ uint32_t f32_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
 
+__device__ __forceinline__ int64_t id_of(const MxIds &ids, uint64_t i)
+{
+    return ids.wide ? reinterpret_cast<const int64_t *>(ids.p)[i] : reinterpret_cast<const int32_t *>(ids.p)[i];
+}
+
 // The element types as C++ types, by MxType.
 template <uint32_t T> struct Elem;
 template <> struct Elem<kBf16> { typedef __bf16 type; };

@@ -12,11 +12,6 @@
 namespace fastrack {
 namespace mx {
 
-__device__ __forceinline__ int64_t id_of(const MxIds &ids, uint64_t i)
-{
-    return ids.wide ? reinterpret_cast<const int64_t *>(ids.p)[i] : reinterpret_cast<const int32_t *>(ids.p)[i];
-}
-
 // ---- lookup ---------------------------------------------------------------------------------
 //
 // A lane loads a block, 16 bytes of codes: with 4 bytes to a lane there is too little on its way to

@@ -14,6 +14,7 @@
 #include "mx.h"
 #include "mx_dev.h"
 #include "mx_gemm_dev.h"
+#include "mx_loss_dev.h"
 #include "mx_small.h"
 
 namespace fastrack {
@@ -94,6 +95,161 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
     }
 }
 
+// The end of a tile: its results to c, or to their part of a sum.
+struct Store {
+    template <int N>
+    __device__ __forceinline__ void finish(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t part,
+                                           const Gemm &g) const
+    {
+        Out o = {g.c, g.ldc, g.ctype, g.accumulate};
+        if (g.splits > 1)
+            o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
+        put_tile<N>(acc, lds, m0, n0, g.m, g.n, o);
+    }
+};
+
+// 32 of each wave's rows of a tile (its squares i) to LDS, in rows as put_tile has them.
+template <int N>
+__device__ __forceinline__ void spread(const f32x16 (&acc)[N][N], int i, float *lds)
+{
+    constexpr uint32_t B = 64 * N;
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const uint32_t y = wave / 2 * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
+            const uint32_t x = wave % 2 * 32 * N + j * 32 + (lane & 31);
+            lds[y * B + (x ^ ((y & 4) << 3))] = acc[i][j][r];
+        }
+}
+
+// The end of a tile of logits, of which their largest and the sum of their exponentials are left.
+// 64 rows at a time are in LDS, a quarter of a row to a thread, which holds it in registers between
+// the two; threads begin at different places of their quarters, for the banks. What bounds it is
+// v_exp_f32, 16 cycles of the 26 of a value: 6656 of a tile, whose products take 131072 with 4096
+// inputs.
+struct StatEnd {
+    LossTile a;
+
+    template <bool EDGE, uint32_t C>   // EDGE: only the first `left` columns of the quarter are classes
+    __device__ __forceinline__ Stat stat(const f32x4 (&v)[C], const uint32_t (&x)[C], uint32_t left) const
+    {
+        const float inf = __builtin_inff();
+        // The largest value (a NaN shows in the sum). A negative scale turns the order.
+        const bool turned = a.scale < 0.0f;
+        float top = turned ? inf : -inf;
+#pragma unroll
+        for (uint32_t k = 0; k < C; ++k)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const float u = EDGE && x[k] + e >= left ? top : v[k][e];
+                top = turned ? fminf(top, u) : fmaxf(top, u);
+            }
+        float other = quad_xor1(top);
+        top = turned ? fminf(top, other) : fmaxf(top, other);
+        other = quad_xor2(top);
+        top = turned ? fminf(top, other) : fmaxf(top, other);
+        const float scale2 = a.scale * kLog2e, base = __builtin_fabsf(top) == inf ? 0.0f : top * scale2;
+        float sum = 0.0f;
+#pragma unroll
+        for (uint32_t k = 0; k < C; ++k)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k][e], scale2, -base));
+                sum += EDGE && x[k] + e >= left ? 0.0f : p;
+            }
+        sum += quad_xor1(sum);
+        sum += quad_xor2(sum);
+        // (Of infinite logits the scale's sign is kept; of none, or of NaN, any will do.)
+        return {__builtin_fabsf(top) == inf ? (turned ? -top : top) : top * a.scale, sum};
+    }
+
+    template <int N>
+    __device__ __forceinline__ void finish(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t,
+                                           const Gemm &g) const
+    {
+        constexpr uint32_t B = 64 * N, Q = B / 4, C = Q / 4;   // columns of a tile, of a quarter; chunks of 4 in it
+        const uint32_t t = threadIdx.x, y = t / 4, q = t % 4, turn = (y & 4) << 3;
+        const float *line = lds + y * B;
+        uint32_t x[C];
+#pragma unroll
+        for (uint32_t k = 0; k < C; ++k)
+            x[k] = (k + t) % C * 4;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t row = m0 + (y >> 5) * 32 * N + i * 32 + (y & 31);
+            const int64_t at = row < g.m ? id_of(a.ids, row) - (int64_t)(a.v0 + n0) : -1;
+            if (i)
+                __syncthreads();
+            spread<N>(acc, i, lds);
+            __syncthreads();
+            f32x4 v[C];
+#pragma unroll
+            for (uint32_t k = 0; k < C; ++k)
+                v[k] = *reinterpret_cast<const f32x4 *>(line + ((q * Q + x[k]) ^ turn));
+            const uint32_t classes = min(B, g.n - n0);
+            const Stat s = classes == B ? stat<false, C>(v, x, 0) : stat<true, C>(v, x, classes > q * Q ? classes - q * Q : 0);
+            if (q == 0 && row < g.m) {
+                a.stats[(uint64_t)(a.part0 + n0 / B) * g.m + row] = s;
+                if (at >= 0 && at < (int64_t)classes)
+                    a.label[row] = line[(uint32_t)at ^ turn] * a.scale;
+            }
+        }
+    }
+};
+
+// The end of a tile of logits that becomes their gradient, in bf16 terms, each the nearest to what
+// those before leave: dloss (e^(z - lse) - [class = target]) times the scale.
+struct SlopeEnd {
+    LossTile a;
+
+    template <int N>
+    __device__ __forceinline__ void finish(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t,
+                                           const Gemm &g) const
+    {
+        constexpr uint32_t B = 64 * N, U = B / 8, R = 64 * U / kThreads;   // units of a row; rows of a thread
+        const uint32_t t = threadIdx.x, x = t % U * 8, classes = min(B, g.n - n0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float lse[R], factor[R];
+            int32_t at[R];   // the target in this thread's columns, -1 elsewhere, -2 for none
+#pragma unroll
+            for (uint32_t k = 0; k < R; ++k) {
+                const uint32_t y = t / U + k * (kThreads / U), row = min(m0 + (y >> 5) * 32 * N + i * 32 + (y & 31), g.m - 1);
+                const int64_t id = id_of(a.ids, row), d = id - (int64_t)(a.v0 + n0 + x);
+                lse[k] = a.lse[row];
+                factor[k] = a.dloss[row * a.dloss_step] * a.scale;
+                at[k] = id < 0 ? -2 : d >= 0 && d < 8 ? (int32_t)d : -1;
+            }
+            if (i)
+                __syncthreads();
+            spread<N>(acc, i, lds);
+            __syncthreads();
+#pragma unroll
+            for (uint32_t k = 0; k < R; ++k) {
+                const uint32_t y = t / U + k * (kThreads / U), row = m0 + (y >> 5) * 32 * N + i * 32 + (y & 31);
+                const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
+                const f32x4 lo = p[0], hi = p[1];
+                float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] = factor[k] * exp_of(__builtin_fmaf(v[e], a.scale, -lse[k]));
+                if (at[k] >= 0)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)   // (in one product: what e^0 - 1 leaves is not rounded away)
+                        v[e] = at[k] == e ? slope(__builtin_fmaf(reinterpret_cast<const float *>(p)[e], a.scale, -lse[k]), factor[k]) : v[e];
+                if (at[k] == -2 || classes < B)
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e)   // no gradient, whatever the logits are; no class
+                        v[e] = at[k] == -2 || x + e >= classes ? 0.0f : v[e];
+                if (row < g.m && n0 + x < a.ld)
+                    put_terms(a.dz + row * a.ld + n0 + x, a.plane, a.terms, v);
+            }
+        }
+    }
+};
+
 // One tile of c, or of one part of it, by 2 x 2 waves of 32 N x 32 N outputs each. TA: a is
 // summed over its rows (a[k][m]) instead of along them (a[m][k]); TB: the same of the MX
 // matrix. While a stage of 64 summed values is multiplied out of one half of the LDS, the next
@@ -115,8 +271,8 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
 // A whole stage is read without a check: rows and columns past the matrices' ends read the
 // last ones again, for results that are not stored. (Rows so long that a tile spans 2^32
 // bytes have no such stages; all of theirs are checked.)
-template <uint32_t FMT, bool TA, bool TB, int N>
-__global__ __launch_bounds__(kThreads, N > 2 ? 1 : 2) void gemm_kernel(Gemm g)
+template <uint32_t FMT, bool TA, bool TB, int N, class End>
+__global__ __launch_bounds__(kThreads, N > 2 ? 1 : 2) void gemm_kernel(Gemm g, End end)
 {
     constexpr int B = 64 * N, U = B * 8 / kThreads;   // outputs a side; units of 8 values that a thread copies of each operand
     constexpr uint32_t CB = FMT == kMx4 ? 4 : FMT == kMx8 ? 8 : 16;   // bytes of 8 codes, or bf16 values
@@ -381,10 +537,7 @@ __global__ __launch_bounds__(kThreads, N > 2 ? 1 : 2) void gemm_kernel(Gemm g)
         lds_barrier();
     }
 
-    Out o = {g.c, g.ldc, g.ctype, g.accumulate};
-    if (g.splits > 1)
-        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
-    put_tile<N>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
+    end.template finish<N>(acc, reinterpret_cast<float *>(lds), m0, n0, part, g);
 }
 
 // c = the sum of the parts, always in their order; four values of a row to a thread, or fewer at
@@ -490,7 +643,7 @@ Plan plan_as(const MxProduct &p, Path path, uint32_t tile, bool laid_out, uint64
     r.tm = (uint32_t)((r.m + tile - 1) / tile);
     r.tn = (uint32_t)((r.n + tile - 1) / tile);
     r.laid_out = laid_out && r.k;
-    r.planes = r.laid_out ? planes_of(p.type) : 1;
+    r.planes = p.terms ? p.terms : r.laid_out ? planes_of(p.type) : 1;
     r.a_ld = round_up(r.a_cols, 8);
     r.a_bytes = r.laid_out ? round_up(r.planes * r.a_rows * r.a_ld * 2, 256) : 0;
     r.stages = (uint32_t)((r.k + kBK - 1) / kBK) * r.planes;
@@ -535,9 +688,9 @@ Plan plan_of(const MxProduct &p, int num_cu)
         return plan_as(p, kDot, 1, false, 1);
     // gemm_kernel reads whole stages 16 bytes at a time at multiples of 4. Along its rows a may end
     // anywhere (the short stage looks at each value); across them, whole chunks.
-    const bool in_place = p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
-                          (!ta || a_cols % 8 == 0);
-    const uint64_t stages = (k + kBK - 1) / kBK, terms = planes_of(p.type);
+    const bool in_place = p.terms || (p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
+                          (!ta || a_cols % 8 == 0));
+    const uint64_t stages = (k + kBK - 1) / kBK, terms = p.terms ? p.terms : planes_of(p.type);
 
     // gemm_kernel: tiles of 256 where they give more than half the CUs work and the sum is long
     // enough to pay for a tile's ends (64 tokens' gradient of 8192 x 8192 weights: 67 us with tiles
@@ -550,7 +703,7 @@ Plan plan_of(const MxProduct &p, int num_cu)
     // (And where more tiles of 128 would be 2^32 threads, which no launch has.)
     const uint64_t tiles128 = (m + 127) / 128 * ((n + 127) / 128);
     const uint32_t tile = (large > cu / 2 && stages >= 4) || tiles128 * kThreads >= 1ull << 32 ? 256 : 128;
-    const uint64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), sum = stages * (in_place ? 1 : terms);
+    const uint64_t tiles = (m + tile - 1) / tile * ((n + tile - 1) / tile), sum = stages * (in_place && !p.terms ? 1 : terms);
     const double whole_us = (ta ? 0.65 : 0.4) * (double)sum;
     const uint64_t splits = tile == 256 ? 1 : cuts_of(whole_us, tiles, sum, m * n, cu);
     Plan as_tiles = plan_as(p, kTiles, tile, !in_place, splits);
@@ -564,7 +717,7 @@ Plan plan_of(const MxProduct &p, int num_cu)
         as_tiles.q_bytes = p.m * mx_blocks(p.k) * 64;
     }
     const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
-    if (tile == 256 || span >= 1ull << 31 || a_cols < 8 || k == 0)
+    if (tile == 256 || span >= 1ull << 31 || a_cols < 8 || k == 0 || p.terms > 1)
         return as_tiles;
 
     // Small tiles or gemm_kernel's of 128, by estimates of their times in us. A workgroup of small
@@ -922,14 +1075,13 @@ static hipError_t lay_out(const MxProduct &p, const Plan &r, hipStream_t s)
     return hipSuccess;
 }
 
-static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &a, const MxMatrix &q, float *parts,
-                               hipStream_t s)
+static Gemm gemm_of(const MxProduct &p, const Plan &r, const MxRows &a, const MxMatrix &q, float *parts)
 {
     Gemm g = {};
     g.a = reinterpret_cast<const uint16_t *>(a.p);
     g.lda = a.ld;
-    g.a_cols = (uint32_t)(r.laid_out ? r.a_ld : r.a_cols);
-    g.a_plane = r.a_rows * r.a_ld;
+    g.a_cols = (uint32_t)(r.laid_out ? r.a_ld : p.terms ? round_up(r.a_cols, 8) : r.a_cols);
+    g.a_plane = p.terms ? p.plane : r.a_rows * r.a_ld;
     g.q = q;
     g.nb = (uint32_t)mx_blocks(p.k);
     g.m = (uint32_t)r.m;
@@ -949,13 +1101,22 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
     g.ctype = p.ctype;
     g.accumulate = p.accumulate;
     g.parts = parts;
+    return g;
+}
+
+static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &a, const MxMatrix &q, float *parts,
+                               hipStream_t s)
+{
+    typedef Store End;
+    const End end;
+    const Gemm g = gemm_of(p, r, a, q, parts);
     const dim3 grid(r.tm * r.tn * r.splits);
 #define MX_GEMM(...)                                                                              \
     do {                                                                                          \
         if (r.tile == 256)                                                                        \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 4>), grid, dim3(kThreads), 0, s, g);     \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 4, End>), grid, dim3(kThreads), 0, s, g, end);     \
         else                                                                                      \
-            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2>), grid, dim3(kThreads), 0, s, g);     \
+            hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, End>), grid, dim3(kThreads), 0, s, g, end);     \
     } while (0)
     if (p.op == kLinear)
         MX_GEMM(kMx4, false, false);
@@ -964,9 +1125,47 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
     else if (!r.decoded)
         MX_GEMM(kMx8, true, true);
     else
-        hipLaunchKernelGGL((gemm_kernel<kDecoded, true, true, 4>), grid, dim3(kThreads), 0, s, g);
+        hipLaunchKernelGGL((gemm_kernel<kDecoded, true, true, 4, End>), grid, dim3(kThreads), 0, s, g, end);
 #undef MX_GEMM
     return hipGetLastError();
+}
+
+// A head's logits, one tile after the other, to an end of their own.
+template <class End>
+static hipError_t launch_logits(const MxProduct &p, const LossTile &t, bool laid_out, int num_cu, hipStream_t s)
+{
+    const Plan r = plan_of(p, num_cu);
+    MxRows a = p.a;
+    if (r.laid_out) {
+        const hipError_t e = laid_out ? hipSuccess : lay_out(p, r, s);
+        if (e != hipSuccess)
+            return e;
+        a = {p.work, r.a_ld};
+    }
+    const End end = {t};
+    const Gemm g = gemm_of(p, r, a, p.q, nullptr);
+    const dim3 grid(r.tm * r.tn);
+    if (r.tile == 256)
+        hipLaunchKernelGGL((gemm_kernel<kMx4, false, false, 4, End>), grid, dim3(kThreads), 0, s, g, end);
+    else
+        hipLaunchKernelGGL((gemm_kernel<kMx4, false, false, 2, End>), grid, dim3(kThreads), 0, s, g, end);
+    return hipGetLastError();
+}
+
+uint32_t mx_logits_tile(const MxProduct &p, int num_cu)
+{
+    const Plan r = plan_of(p, num_cu);
+    return r.path == kTiles && r.splits == 1 ? r.tile : 0;
+}
+
+hipError_t launch_mx_logits_stats(const MxProduct &p, const LossTile &t, bool laid_out, int num_cu, hipStream_t s)
+{
+    return launch_logits<StatEnd>(p, t, laid_out, num_cu, s);
+}
+
+hipError_t launch_mx_logits_slopes(const MxProduct &p, const LossTile &t, bool laid_out, int num_cu, hipStream_t s)
+{
+    return launch_logits<SlopeEnd>(p, t, laid_out, num_cu, s);
 }
 
 uint64_t mx_product_work(const MxProduct &p, int num_cu) { return plan_of(p, num_cu).bytes(); }

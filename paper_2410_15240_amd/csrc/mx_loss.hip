@@ -8,6 +8,7 @@
 #include "launch.h"
 #include "mx_dev.h"
 #include "mx_gemm_dev.h"
+#include "mx_loss_dev.h"
 #include "mx_model.h"
 
 namespace fastrack {
@@ -15,62 +16,29 @@ namespace mx {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ int64_t id_of(const MxIds &ids, uint64_t i)
-{
-    return ids.wide ? reinterpret_cast<const int64_t *>(ids.p)[i] : reinterpret_cast<const int32_t *>(ids.p)[i];
-}
-
-// A largest value and the sum of exponentials over it. An infinite largest value stands for none: e^z
-// itself is summed then, which is 0 for -inf and inf for inf.
-struct Stat {
-    float top, sum;
-};
-
-__device__ __forceinline__ float base_of(float top) { return __builtin_fabsf(top) == __builtin_inff() ? 0.0f : top; }
-
-// The larger one; NaN where either is (fmaxf would drop it).
-__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
-
-__device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
-{
-    const float top = larger(a.top, b.top), base = base_of(top);
-    return {top, a.sum * expf(base_of(a.top) - base) + b.sum * expf(base_of(b.top) - base)};
-}
-
-struct Piece {
-    const float *z;        // [m][n], unscaled
-    uint32_t m, n;         // of this piece
-    uint64_t v0;           // its first class
-    float scale;
-    MxIds ids;
-    Stat *stats;           // [parts][m]
-    float *label;          // [m]: the logit of the target
-    uint32_t part0, parts; // of this piece
-};
-
 // One workgroup: kThreads * 8 classes of a row.
 constexpr uint32_t kStatCols = kThreads * 8;
 
-__global__ __launch_bounds__(kThreads) void stat_kernel(Piece g)
+__global__ __launch_bounds__(kThreads) void stat_kernel(const float *z, uint32_t m, uint32_t n, uint32_t parts, LossTile a)
 {
     __shared__ Stat lds[kThreads / 64];
-    const uint32_t row = blockIdx.x / g.parts, part = blockIdx.x - row * g.parts, c = part * kStatCols + threadIdx.x * 8;
+    const uint32_t row = blockIdx.x / parts, part = blockIdx.x - row * parts, c = part * kStatCols + threadIdx.x * 8;
     Stat s = {-__builtin_inff(), 0.0f};
-    if (c < g.n) {
+    if (c < n) {
         float v[8];
-        load8<kFp32>(g.z, (uint64_t)row * g.n, c, g.n, v);
-        const int64_t at = id_of(g.ids, row) - (int64_t)g.v0 - c;
+        load8<kFp32>(z, (uint64_t)row * n, c, n, v);
+        const int64_t at = id_of(a.ids, row) - (int64_t)a.v0 - c;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            v[i] = c + i < g.n ? v[i] * g.scale : -__builtin_inff();
+            v[i] = c + i < n ? v[i] * a.scale : -__builtin_inff();
             s.top = larger(v[i], s.top);
-            if (at == i && c + i < g.n)
-                g.label[row] = v[i];
+            if (at == i && c + i < n)
+                a.label[row] = v[i];
         }
         const float base = base_of(s.top);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            s.sum += expf(v[i] - base);
+            s.sum += exp_of(v[i] - base);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2)
@@ -81,7 +49,7 @@ __global__ __launch_bounds__(kThreads) void stat_kernel(Piece g)
     if (threadIdx.x == 0) {
         for (int w = 1; w < kThreads / 64; ++w)
             s = join(s, lds[w]);
-        g.stats[(uint64_t)(g.part0 + part) * g.m + row] = s;
+        a.stats[(uint64_t)(a.part0 + part) * m + row] = s;
     }
 }
 
@@ -110,39 +78,26 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Stat *stats, uint3
     }
 }
 
-// The logits' gradient, dloss (e^(z - lse) - [class = target]) times the scale, in rows of ld values
+// The logits' gradient, dloss (e^(z - lse) - [class = target]) times the scale, in rows of a.ld values
 // that end in zeros.
-struct Slope {
-    const float *z;
-    uint32_t m, n, per_row, recip;
-    uint64_t row0, v0, ld;
-    float scale;
-    MxIds ids;
-    const float *lse, *dloss;
-    uint64_t dloss_step;
-    void *dz;
-};
-
-__device__ __forceinline__ float slope(float z, float lse, float factor, bool target)
-{
-    return factor * (expf(z - lse) - (target ? 1.0f : 0.0f));
-}
-
 template <uint32_t T>
-__global__ __launch_bounds__(kThreads) void slope_kernel(Slope g)
+__global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_t m, uint32_t n, uint32_t per_row, uint32_t recip, uint64_t row0,
+                                                         LossTile a)
 {
-    const uint32_t i = blockIdx.x * kThreads + threadIdx.x, r = div_recip(i, g.per_row, g.recip), c = (i - r * g.per_row) * 8;
-    const uint64_t row = g.row0 + r;
-    if (row >= g.m)
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x, r = div_recip(i, per_row, recip), c = (i - r * per_row) * 8;
+    const uint64_t row = row0 + r;
+    if (row >= m)
         return;
     float v[8];
-    load8<kFp32>(g.z, row * g.n, c, g.n, v);
-    const int64_t id = id_of(g.ids, row), at = id - (int64_t)g.v0 - c;
-    const float lse = g.lse[row], factor = g.dloss[row * g.dloss_step] * g.scale;
+    load8<kFp32>(z, row * n, c, n, v);
+    const int64_t id = id_of(a.ids, row), at = id - (int64_t)a.v0 - c;
+    const float lse = a.lse[row], factor = a.dloss[row * a.dloss_step] * a.scale;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        v[j] = id < 0 || c + j >= g.n ? 0.0f : slope(v[j] * g.scale, lse, factor, at == j);
-    store8<T>(g.dz, row * g.ld, c, (uint32_t)g.ld, v);
+    for (int j = 0; j < 8; ++j)   // (a token that is left out: no gradient, whatever its logits are)
+        v[j] = id < 0 || c + j >= n ? 0.0f
+               : at == j           ? slope(__builtin_fmaf(v[j], a.scale, -lse), factor)
+                                   : factor * exp_of(__builtin_fmaf(v[j], a.scale, -lse));
+    store8<T>(a.dz, row * a.ld, c, (uint32_t)a.ld, v);
 }
 
 // The result in its own type.
@@ -174,19 +129,11 @@ hipError_t over(uint64_t rows, uint32_t per_row, F launch)
 
 uint64_t round_to(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
-// Classes of a piece, whole tiles of 256: 2^26 logits, which lie in the workspace.
-constexpr uint64_t kPieceValues = 1ull << 26;
-uint64_t piece_of(const Loss &l)
+// Classes of a piece of `values` logits, whole tiles of 256.
+uint64_t piece_of(const Loss &l, uint64_t values)
 {
-    const uint64_t most = round_to(l.n, 256), v = kPieceValues / (l.m ? l.m : 1) / 256 * 256;
+    const uint64_t most = round_to(l.n, 256), v = values / (l.m ? l.m : 1) / 256 * 256;
     return v < 256 ? 256 : v < most ? v : most;
-}
-
-// Type of the logits' gradient: in 16 bits where that is what both results are rounded to.
-uint32_t slope_type(const Loss &l)
-{
-    const bool x = !l.dx.p || l.dx_type == kBf16, w = !l.x8.codes || l.dw_type == kBf16;
-    return x && w ? kBf16 : kFp32;
 }
 
 MxProduct logits(const Loss &l, uint64_t v0, uint64_t n, float *z)
@@ -203,12 +150,26 @@ MxProduct logits(const Loss &l, uint64_t v0, uint64_t n, float *z)
     return p;
 }
 
-struct LossPlan {
-    uint64_t piece, parts;
-    uint64_t z, stats, label, product;   // bytes
-    uint64_t dz, dx;
-    uint64_t bytes() const { return z + stats + label + product + dz + dx; }
+// How the logits of a piece's width run: in whole tiles, whose ends do the rest, or (0: few
+// outputs) into the workspace and through a kernel of their own.
+struct Width {
+    uint64_t n;
+    uint32_t tile;
 };
+
+struct LossPlan {
+    uint64_t piece;
+    Width whole, rest;                   // of a piece; of the last one, n = 0 if there is none of its own
+    uint64_t product, z, stats, label, dz, dx;   // bytes
+    uint32_t type;                       // of the logits' gradient where it is no bf16 terms
+    uint32_t terms_x, terms_w;           // of the logits' gradient that the products take, where it is
+    const Width &width(uint64_t left) const { return left >= whole.n ? whole : rest; }
+    uint64_t bytes() const { return product + z + stats + label + dz + dx; }
+};
+
+uint64_t parts_of(const Width &w) { return w.tile ? (w.n + w.tile - 1) / w.tile : (w.n + kStatCols - 1) / kStatCols; }
+
+uint32_t terms_of(uint32_t type) { return type == kBf16 ? 1 : type == kFp16 ? 2 : 3; }
 
 }  // namespace mx
 
@@ -216,113 +177,144 @@ using namespace mx;
 
 namespace {
 
-// What products of whole pieces and of the last one need.
-template <class F>
-uint64_t most_of(const Loss &l, uint64_t piece, F product, int num_cu)
-{
-    uint64_t most = 0;
-    for (uint64_t n : {piece < l.n ? piece : l.n, l.n % piece ? l.n % piece : piece}) {
-        const uint64_t need = mx_product_work(product(n), num_cu);
-        most = need > most ? need : most;
-    }
-    return round_to(most, 256);
-}
+// Values of a piece: forwards no more than a launch has tiles for; backwards so many that the products of
+// a piece fill the GPU and their sums over it are long (4096 tokens, 4096 x 65536: PIECES). Logits that
+// go through the workspace, half as many.
+constexpr uint64_t kForwardValues = 1ull << 34, kBackwardValues = 1ull << 27, kWorkspaceValues = 1ull << 26;
 
-LossPlan plan_of(const Loss &l, int num_cu)
+LossPlan plan_of(const Loss &l, int num_cu, uint64_t values)
 {
     LossPlan p = {};
-    p.piece = piece_of(l);
-    const uint64_t n = p.piece < l.n ? p.piece : l.n;
-    p.parts = l.n / p.piece * ((p.piece + kStatCols - 1) / kStatCols) + (l.n % p.piece + kStatCols - 1) / kStatCols;
-    p.z = round_to(l.m * n * 4, 256);
-    p.stats = round_to(p.parts * l.m * sizeof(Stat), 256);
+    const bool tiles = mx_logits_tile(logits(l, 0, l.n, nullptr), num_cu) != 0;
+    p.piece = piece_of(l, tiles ? values : kWorkspaceValues);
+    p.whole.n = p.piece < l.n ? p.piece : l.n;
+    p.rest.n = l.n % p.whole.n;
+    for (Width *w : {&p.whole, &p.rest}) {
+        if (w->n == 0)
+            continue;
+        const MxProduct z = logits(l, 0, w->n, nullptr);
+        w->tile = mx_logits_tile(z, num_cu);
+        const uint64_t need = round_to(mx_product_work(z, num_cu), 256), own = w->tile ? 0 : round_to(l.m * w->n * 4, 256);
+        p.product = need > p.product ? need : p.product;
+        p.z = own > p.z ? own : p.z;
+    }
+    return p;
+}
+
+LossPlan forward_plan(const Loss &l, int num_cu)
+{
+    LossPlan p = plan_of(l, num_cu, kForwardValues);
+    const uint64_t parts = l.n / p.whole.n * parts_of(p.whole) + (p.rest.n ? parts_of(p.rest) : 0);
+    p.stats = round_to(parts * l.m * sizeof(Stat), 256);
     p.label = round_to(l.m * 4, 256);
-    p.product = most_of(l, p.piece, [&](uint64_t w) { return logits(l, 0, w, nullptr); }, num_cu);
     return p;
 }
 
-MxProduct back_x(const Loss &l, uint64_t v0, uint64_t n, void *dz, uint32_t type, uint64_t ld, const Out &o)
+// The logits' gradient: one type of float for both products where it goes through a kernel of its own;
+// bf16 terms, as many as each product's result needs, where the tiles' ends write it.
+MxProduct slopes(const Loss &l, const LossPlan &p, const Width &w, void *dz, uint32_t terms)
 {
-    MxProduct p = logits(l, v0, n, nullptr);
-    p.op = kGradInput;
-    p.type = type;
-    p.a = {dz, ld};
-    p.c = {o.p, o.ld};
-    p.ctype = o.type;
-    p.accumulate = o.accumulate;
-    return p;
+    MxProduct r = {};
+    r.type = w.tile ? (uint32_t)kBf16 : p.type;
+    r.terms = w.tile ? terms : 0;
+    r.a = {dz, round_to(w.n, 8)};
+    r.plane = l.m * r.a.ld;
+    r.m = l.m, r.n = w.n, r.k = l.k;
+    return r;
 }
 
-MxProduct back_w(const Loss &l, uint64_t v0, uint64_t n, void *dz, uint32_t type, uint64_t ld)
+MxProduct back_x(const Loss &l, const LossPlan &p, const Width &w, uint64_t v0, void *dz, const Out &o)
 {
-    MxProduct p = {};
-    p.op = kWeightGrad;
-    p.type = type;
-    p.a = {dz, ld};
-    p.q = l.x8;
-    p.m = l.m, p.n = n, p.k = l.k;
-    p.ctype = l.dw_type;
-    p.c = {reinterpret_cast<uint8_t *>(l.dw.p) + v0 * l.dw.ld * mx_type_size(l.dw_type), l.dw.ld};
-    p.accumulate = l.accumulate;
-    return p;
+    MxProduct r = slopes(l, p, w, dz, p.terms_x);
+    r.op = kGradInput;
+    r.q = logits(l, v0, w.n, nullptr).q;
+    r.c = {o.p, o.ld};
+    r.ctype = o.type;
+    r.accumulate = o.accumulate;
+    return r;
 }
 
-// An address for a plan that asks where its float operand lies.
-void *some_place() { return reinterpret_cast<void *>(256); }
-
-LossPlan grad_plan_of(const Loss &l, int num_cu)
+MxProduct back_w(const Loss &l, const LossPlan &p, const Width &w, uint64_t v0, void *dz)
 {
-    LossPlan p = plan_of(l, num_cu);
-    p.stats = p.label = 0;
-    const uint32_t type = slope_type(l);
-    const uint64_t n = p.piece < l.n ? p.piece : l.n;
-    p.dz = round_to(l.m * round_to(n, 8) * mx_type_size(type), 256);
-    p.dx = l.dx.p && l.dx_type != kFp32 && p.piece < l.n ? round_to(l.m * l.k * 4, 256) : 0;
-    const uint64_t x = most_of(l, p.piece, [&](uint64_t w) { return back_x(l, 0, w, some_place(), type, round_to(w, 8), {}); }, num_cu);
-    const uint64_t w = most_of(l, p.piece, [&](uint64_t w) { return back_w(l, 0, w, some_place(), type, round_to(w, 8)); }, num_cu);
-    p.product = p.product > x ? p.product : x;
-    p.product = p.product > w ? p.product : w;
+    MxProduct r = slopes(l, p, w, dz, p.terms_w);
+    r.op = kWeightGrad;
+    r.q = l.x8;
+    r.ctype = l.dw_type;
+    r.c = {reinterpret_cast<uint8_t *>(l.dw.p) + v0 * l.dw.ld * mx_type_size(l.dw_type), l.dw.ld};
+    r.accumulate = l.accumulate;
+    return r;
+}
+
+LossPlan backward_plan(const Loss &l, int num_cu)
+{
+    LossPlan p = plan_of(l, num_cu, kBackwardValues);
+    p.terms_x = l.dx.p ? terms_of(l.dx_type) : 0;
+    p.terms_w = l.x8.codes ? terms_of(l.dw_type) : 0;
+    const uint32_t terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
+    p.type = terms <= 1 ? kBf16 : kFp32;
+    p.dx = l.dx.p && l.dx_type != kFp32 && p.whole.n < l.n ? round_to(l.m * l.k * 4, 256) : 0;
+    void *const some_place = reinterpret_cast<void *>(256);   // (a plan asks where its float operand lies)
+    for (const Width *w : {&p.whole, &p.rest}) {
+        if (w->n == 0)
+            continue;
+        const uint64_t dz = round_to(l.m * round_to(w->n, 8) * (w->tile ? 2 * terms : mx_type_size(p.type)), 256);
+        p.dz = dz > p.dz ? dz : p.dz;
+        const uint64_t x = l.dx.p ? round_to(mx_product_work(back_x(l, p, *w, 0, some_place, {}), num_cu), 256) : 0;
+        const uint64_t g = l.x8.codes ? round_to(mx_product_work(back_w(l, p, *w, 0, some_place), num_cu), 256) : 0;
+        p.product = x > p.product ? x : p.product;
+        p.product = g > p.product ? g : p.product;
+    }
     return p;
 }
 
-}  // namespace
-
-uint64_t mx_loss_work(const Loss &l, int num_cu) { return l.m && l.n ? plan_of(l, num_cu).bytes() : 0; }
-
-uint64_t mx_loss_grad_work(const Loss &l, int num_cu) { return l.m && l.n ? grad_plan_of(l, num_cu).bytes() : 0; }
-
-static hipError_t multiply(MxProduct p, uint8_t *work, uint64_t bytes, int num_cu, hipStream_t s)
+hipError_t multiply(MxProduct p, uint8_t *work, uint64_t bytes, int num_cu, hipStream_t s)
 {
     p.work = work;
     p.work_bytes = bytes;
     return launch_mx_product(p, num_cu, s);
 }
 
+}  // namespace
+
+uint64_t mx_loss_work(const Loss &l, int num_cu) { return l.m && l.n ? forward_plan(l, num_cu).bytes() : 0; }
+
+uint64_t mx_loss_grad_work(const Loss &l, int num_cu) { return l.m && l.n ? backward_plan(l, num_cu).bytes() : 0; }
+
 hipError_t launch_mx_loss(const Loss &l, int num_cu, hipStream_t s)
 {
     if (l.m == 0)
         return hipSuccess;
-    const LossPlan p = plan_of(l, num_cu);
+    const LossPlan p = forward_plan(l, num_cu);
     uint8_t *const work = reinterpret_cast<uint8_t *>(l.work);
-    Piece g = {};
-    g.z = reinterpret_cast<float *>(work + p.product);
-    g.stats = reinterpret_cast<Stat *>(work + p.product + p.z);
-    g.label = reinterpret_cast<float *>(work + p.product + p.z + p.stats);
-    g.m = (uint32_t)l.m;
-    g.scale = l.scale;
-    g.ids = l.ids;
-    for (g.v0 = 0; g.v0 < l.n; g.v0 += p.piece, g.part0 += g.parts) {
-        g.n = (uint32_t)(l.n - g.v0 < p.piece ? l.n - g.v0 : p.piece);
-        g.parts = (g.n + kStatCols - 1) / kStatCols;
-        hipError_t e = multiply(logits(l, g.v0, g.n, const_cast<float *>(g.z)), work, p.product, num_cu, s);
-        if (e != hipSuccess)
-            return e;
-        hipLaunchKernelGGL(stat_kernel, dim3(g.m * g.parts), dim3(kThreads), 0, s, g);
-        if ((e = hipGetLastError()) != hipSuccess)
-            return e;
+    float *const z = reinterpret_cast<float *>(work + p.product);
+    LossTile t = {};
+    t.ids = l.ids;
+    t.scale = l.scale;
+    t.stats = reinterpret_cast<Stat *>(work + p.product + p.z);
+    t.label = reinterpret_cast<float *>(work + p.product + p.z + p.stats);
+    bool laid_out = false;
+    hipError_t e;
+    while (t.v0 < l.n) {
+        const Width &w = p.width(l.n - t.v0);
+        MxProduct g = logits(l, t.v0, w.n, z);
+        if (w.tile) {
+            g.work = work;
+            if ((e = launch_mx_logits_stats(g, t, laid_out, num_cu, s)) != hipSuccess)
+                return e;
+            laid_out = true;
+        } else {
+            if ((e = multiply(g, work, p.product, num_cu, s)) != hipSuccess)
+                return e;
+            const uint32_t parts = (uint32_t)parts_of(w);
+            hipLaunchKernelGGL(stat_kernel, dim3((uint32_t)l.m * parts), dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, parts, t);
+            if ((e = hipGetLastError()) != hipSuccess)
+                return e;
+        }
+        t.part0 += (uint32_t)parts_of(w);
+        t.v0 += w.n;
     }
-    hipLaunchKernelGGL(loss_kernel, dim3((g.m + kJoinRows - 1) / kJoinRows), dim3(kThreads), 0, s, g.stats, g.part0, g.m, (uint32_t)l.n, l.ids,
-                       g.label, l.loss, l.lse);
+    hipLaunchKernelGGL(loss_kernel, dim3((uint32_t)((l.m + kJoinRows - 1) / kJoinRows)), dim3(kThreads), 0, s, t.stats, t.part0, (uint32_t)l.m,
+                       (uint32_t)l.n, l.ids, t.label, l.loss, l.lse);
     return hipGetLastError();
 }
 
@@ -330,52 +322,63 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
 {
     if (l.n == 0)
         return hipSuccess;
-    hipError_t e;
-    if (l.m == 0)   // no tokens: a head's gradient of zeros, or the one that is there
-        return l.x8.codes ? multiply(back_w(l, 0, l.n, nullptr, kBf16, l.n), nullptr, 0, num_cu, s) : hipSuccess;
-    const LossPlan p = grad_plan_of(l, num_cu);
-    const uint32_t type = slope_type(l);
+    if (l.m == 0) {   // no tokens: a head's gradient of zeros, or the one that is there
+        LossPlan p = {};
+        p.type = kBf16;
+        return l.x8.codes ? multiply(back_w(l, p, {l.n, 0}, 0, nullptr), nullptr, 0, num_cu, s) : hipSuccess;
+    }
+    const LossPlan p = backward_plan(l, num_cu);
     uint8_t *const work = reinterpret_cast<uint8_t *>(l.work);
-    Slope g = {};
-    g.z = reinterpret_cast<float *>(work + p.product);
-    g.dz = work + p.product + p.z;
-    float *const dx = reinterpret_cast<float *>(work + p.product + p.z + p.dz);
-    g.m = (uint32_t)l.m;
-    g.scale = l.scale;
-    g.ids = l.ids;
-    g.lse = l.lse;
-    g.dloss = l.dloss;
-    g.dloss_step = l.dloss_step;
-    for (g.v0 = 0; g.v0 < l.n; g.v0 += p.piece) {
-        g.n = (uint32_t)(l.n - g.v0 < p.piece ? l.n - g.v0 : p.piece);
-        g.ld = round_to(g.n, 8);
-        if ((e = multiply(logits(l, g.v0, g.n, const_cast<float *>(g.z)), work, p.product, num_cu, s)) != hipSuccess)
-            return e;
-        g.per_row = (uint32_t)(g.ld / 8);
-        g.recip = div_recip_of(g.per_row);
-        e = over(l.m, g.per_row, [&](uint64_t row0, dim3 grid) {
-            g.row0 = row0;
-            if (type == kBf16)
-                hipLaunchKernelGGL((slope_kernel<kBf16>), grid, dim3(kThreads), 0, s, g);
-            else
-                hipLaunchKernelGGL((slope_kernel<kFp32>), grid, dim3(kThreads), 0, s, g);
-        });
-        if (e != hipSuccess)
-            return e;
+    float *const z = reinterpret_cast<float *>(work + p.product);
+    uint8_t *const dz = work + p.product + p.z;
+    float *const dx = reinterpret_cast<float *>(dz + p.dz);
+    LossTile t = {};
+    t.ids = l.ids;
+    t.scale = l.scale;
+    t.lse = l.lse;
+    t.dloss = l.dloss;
+    t.dloss_step = l.dloss_step;
+    t.dz = reinterpret_cast<uint16_t *>(dz);
+    t.terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
+    hipError_t e;
+    for (; t.v0 < l.n; t.v0 += p.width(l.n - t.v0).n) {
+        const Width &w = p.width(l.n - t.v0);
+        MxProduct g = logits(l, t.v0, w.n, z);
+        t.ld = round_to(w.n, 8);
+        t.plane = l.m * t.ld;
+        if (w.tile) {
+            g.work = work;
+            if ((e = launch_mx_logits_slopes(g, t, false, num_cu, s)) != hipSuccess)
+                return e;
+        } else {
+            if ((e = multiply(g, work, p.product, num_cu, s)) != hipSuccess)
+                return e;
+            const uint32_t per_row = (uint32_t)(t.ld / 8);
+            e = over(l.m, per_row, [&](uint64_t row0, dim3 grid) {
+                if (p.type == kBf16)
+                    hipLaunchKernelGGL((slope_kernel<kBf16>), grid, dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, per_row,
+                                       div_recip_of(per_row), row0, t);
+                else
+                    hipLaunchKernelGGL((slope_kernel<kFp32>), grid, dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, per_row,
+                                       div_recip_of(per_row), row0, t);
+            });
+            if (e != hipSuccess)
+                return e;
+        }
         if (l.dx.p) {
-            const Out o = p.dx ? Out{dx, l.k, kFp32, g.v0 != 0} : Out{l.dx.p, l.dx.ld, l.dx_type, g.v0 != 0};
-            if ((e = multiply(back_x(l, g.v0, g.n, g.dz, type, g.ld, o), work, p.product, num_cu, s)) != hipSuccess)
+            const Out o = p.dx ? Out{dx, l.k, kFp32, t.v0 != 0} : Out{l.dx.p, l.dx.ld, l.dx_type, t.v0 != 0};
+            if ((e = multiply(back_x(l, p, w, t.v0, dz, o), work, p.product, num_cu, s)) != hipSuccess)
                 return e;
         }
         if (l.x8.codes)
-            if ((e = multiply(back_w(l, g.v0, g.n, g.dz, type, g.ld), work, p.product, num_cu, s)) != hipSuccess)
+            if ((e = multiply(back_w(l, p, w, t.v0, dz), work, p.product, num_cu, s)) != hipSuccess)
                 return e;
     }
     if (!p.dx)
         return hipSuccess;
     const uint32_t per_row = (uint32_t)((l.k + 7) / 8);
     return over(l.m, per_row, [&](uint64_t row0, dim3 grid) {
-        hipLaunchKernelGGL(round_kernel, grid, dim3(kThreads), 0, s, dx, g.m, (uint32_t)l.k, per_row, div_recip_of(per_row), row0,
+        hipLaunchKernelGGL(round_kernel, grid, dim3(kThreads), 0, s, dx, (uint32_t)l.m, (uint32_t)l.k, per_row, div_recip_of(per_row), row0,
                            Out{l.dx.p, l.dx.ld, l.dx_type, 0});
     });
 }

@@ -1,0 +1,82 @@
+// What the loss's own kernels (mx_loss.hip) and the ends of its products' tiles (mx_gemm.hip) share.
+#pragma once
+#include "mx_dev.h"
+#include "mx_model.h"
+
+namespace fastrack {
+
+// A largest value and the sum of exponentials over it. An infinite largest value stands for none: e^z
+// itself is summed then, which is 0 for -inf and inf for inf.
+struct Stat {
+    float top, sum;
+};
+
+// What a tile of logits needs to know of the loss.
+struct LossTile {
+    MxIds ids;
+    uint64_t v0;             // the piece's first class
+    float scale;
+    // Forwards:
+    Stat *stats;             // [parts][m]
+    float *label;            // [m]: the logit of the target
+    uint32_t part0;          // of this piece
+    // Backwards:
+    const float *lse, *dloss;
+    uint64_t dloss_step;
+    uint16_t *dz;            // bf16 terms, rows of ld values
+    uint64_t ld, plane;
+    uint32_t terms;
+};
+
+// The side of the tiles in which `p` (kLinear) comes out whole, 0 where it does not.
+uint32_t mx_logits_tile(const MxProduct &p, int num_cu);
+// Its tiles to their end; `laid_out`: x's terms lie in the workspace already.
+hipError_t launch_mx_logits_stats(const MxProduct &p, const LossTile &t, bool laid_out, int num_cu, hipStream_t s);
+hipError_t launch_mx_logits_slopes(const MxProduct &p, const LossTile &t, bool laid_out, int num_cu, hipStream_t s);
+
+namespace mx {
+
+__device__ __forceinline__ float base_of(float top) { return __builtin_fabsf(top) == __builtin_inff() ? 0.0f : top; }
+
+// The larger one; NaN where either is (fmaxf would drop it).
+__device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
+
+// e^v by the hardware's 2^v: off by 2^-23 of the result, and by |v| 2^-24 through the argument's rounding.
+constexpr float kLog2e = 1.44269504f;
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+
+__device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
+{
+    const float top = larger(a.top, b.top), base = base_of(top);
+    return {top, a.sum * exp_of(base_of(a.top) - base) + b.sum * exp_of(base_of(b.top) - base)};
+}
+
+// The gradient of a target's logit, for v = z - lse.
+__device__ __forceinline__ float slope(float v, float factor) { return factor * (exp_of(v) - 1.0f); }
+
+// The value of the lane next to this one, and of the one two further, within four.
+__device__ __forceinline__ float quad_xor1(float v)
+{
+    return bits_f32((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f32_bits(v), 0xB1, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float quad_xor2(float v)
+{
+    return bits_f32((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f32_bits(v), 0x4E, 0xF, 0xF, true));
+}
+
+// Eight values as bf16 terms, each the nearest to what those before leave.
+__device__ __forceinline__ void put_terms(uint16_t *p, uint64_t plane, uint32_t terms, float (&v)[8])
+{
+    for (uint32_t k = 0; k < terms; ++k) {
+        bf16x8 h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            h[e] = (__bf16)v[e];
+            v[e] = __builtin_fabsf((float)h[e]) == __builtin_inff() ? 0.0f : v[e] - (float)h[e];
+        }
+        *reinterpret_cast<bf16x8 *>(p + k * plane) = h;
+    }
+}
+
+}  // namespace mx
+}  // namespace fastrack

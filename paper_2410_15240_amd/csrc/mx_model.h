@@ -33,12 +33,6 @@ struct NormGrad {
 uint64_t mx_norm_grad_work(uint64_t rows, uint64_t cols, bool w1, int num_cu);
 hipError_t launch_mx_norm_grad(const NormGrad &n, int num_cu, hipStream_t s);
 
-// Ids of rows, 4 or 8 bytes each.
-struct MxIds {
-    const void *p;
-    uint32_t wide;
-};
-
 // y[t] = scale * table[id_t].
 struct Embedding {
     MxIds ids;
