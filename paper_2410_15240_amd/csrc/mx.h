@@ -69,6 +69,7 @@ struct MxProduct {
     // and the elements between them. type is kBf16.
     uint32_t terms;
     uint64_t plane;
+    const float *scale;     // of c, on the device; null: 1
 };
 
 // Workspace that a product needs: the parts of a long sum, and a's bf16 terms where a is not

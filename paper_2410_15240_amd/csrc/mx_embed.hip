@@ -701,7 +701,7 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
         g.tiles = (uint32_t)((e.cols + 511) / 512);
         g.dy = e.dy;
         g.scale = e.scale;
-        g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate};
+        g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate, nullptr};
         const dim3 grid((uint32_t)((e.rows + kOwnWaves - 1) / kOwnWaves) * g.tiles);
         MX_TYPE(e.type, {
             constexpr uint32_t D = T;
@@ -781,7 +781,7 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
     g.tiles = (uint32_t)((e.cols + kTileCols - 1) / kTileCols);
     g.dy = e.dy;
     g.scale = e.scale;
-    g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate};
+    g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate, nullptr};
     g.parts = reinterpret_cast<float *>(at);
     const dim3 grid(g.chunks * g.tiles);
     MX_TYPE(e.type, {

@@ -44,6 +44,7 @@ struct Gemm {
     uint32_t ctype;
     uint32_t accumulate;
     float *parts;            // [splits][m][n] where splits > 1
+    const float *scale;      // of c (null: 1)
 };
 
 // Tile of workgroup `id`. Workgroups go to the 8 XCDs in turn, each with its own L2: an XCD
@@ -69,6 +70,9 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
 {
     constexpr uint32_t B = 64 * N;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    float scale = 1.0f;
+    if (o.scale)
+        scale = *o.scale;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         if (i)
@@ -89,6 +93,10 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
             const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
             const f32x4 lo = p[0], hi = p[1];
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (o.scale)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] *= scale;
             if (row < m && col < n)
                 put8(o, row, col, n, v);
         }
@@ -101,9 +109,9 @@ struct Store {
     __device__ __forceinline__ void finish(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t part,
                                            const Gemm &g) const
     {
-        Out o = {g.c, g.ldc, g.ctype, g.accumulate};
+        Out o = {g.c, g.ldc, g.ctype, g.accumulate, g.scale};
         if (g.splits > 1)
-            o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
+            o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, nullptr};
         put_tile<N>(acc, lds, m0, n0, g.m, g.n, o);
     }
 };
@@ -219,7 +227,7 @@ struct SlopeEnd {
                 const uint32_t y = t / U + k * (kThreads / U), row = min(m0 + (y >> 5) * 32 * N + i * 32 + (y & 31), g.m - 1);
                 const int64_t id = id_of(a.ids, row), d = id - (int64_t)(a.v0 + n0 + x);
                 lse[k] = a.lse[row];
-                factor[k] = a.dloss[row * a.dloss_step] * a.scale;
+                factor[k] = factor_of(a, row);
                 at[k] = id < 0 ? -2 : d >= 0 && d < 8 ? (int32_t)d : -1;
             }
             if (i)
@@ -549,7 +557,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float *parts, uint
     if (row >= m)
         return;
     const uint64_t total = (uint64_t)m * n;
-    const float *p = parts + (uint64_t)row * n + c;
+    const float *p = parts + (uint64_t)row * n + c, scale = o.scale ? *o.scale : 1.0f;
     if (c + 4 <= n) {
         f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
@@ -560,13 +568,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float *parts, uint
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            put1(o, row, c + j, v[j]);
+            put1(o, row, c + j, v[j] * scale);
     } else {
         for (uint32_t j = c; j < n; ++j) {
             float v = 0.0f;
             for (uint32_t s = 0; s < splits; ++s)
                 v += p[s * total + j - c];
-            put1(o, row, j, v);
+            put1(o, row, j, v * scale);
         }
     }
 }
@@ -1002,9 +1010,9 @@ __global__ __launch_bounds__(kThreads, N > 2 ? 1 : 2) void gemm4_kernel(Gemm4 g)
         lds_barrier();
     }
 
-    Out o = {g.c, g.ldc, g.ctype, 0};
+    Out o = {g.c, g.ldc, g.ctype, 0, nullptr};
     if (g.splits > 1)
-        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0};
+        o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, nullptr};
     put_tile<N>(acc, reinterpret_cast<float *>(lds), m0, n0, g.m, g.n, o);
 }
 
@@ -1100,6 +1108,7 @@ static Gemm gemm_of(const MxProduct &p, const Plan &r, const MxRows &a, const Mx
     g.ldc = p.c.ld;
     g.ctype = p.ctype;
     g.accumulate = p.accumulate;
+    g.scale = p.scale;
     g.parts = parts;
     return g;
 }
@@ -1208,12 +1217,12 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
         g.slices = r.stages;
         g.cuts = r.splits;
         g.per = r.per;
-        g.out = {p.c.p, p.c.ld, p.ctype, p.accumulate};
+        g.out = {p.c.p, p.c.ld, p.ctype, p.accumulate, p.scale};
         g.parts = parts;
         e = r.path == kDot ? launch_mx_dot(g, type, s) : launch_mx_small(g, p.op, type, r.tile, s);
     }
     return e == hipSuccess && r.splits > 1
-               ? join(parts, r.splits, r.m, r.n, {p.c.p, p.c.ld, p.ctype, p.accumulate}, s)
+               ? join(parts, r.splits, r.m, r.n, {p.c.p, p.c.ld, p.ctype, p.accumulate, p.scale}, s)
                : e;
 }
 
@@ -1238,7 +1247,7 @@ hipError_t launch_mx4_product(const Mx4Product &p, int num_cu, hipStream_t s)
     else
         hipLaunchKernelGGL((gemm4_kernel<2>), grid, dim3(kThreads), 0, s, g);
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess && g.splits > 1 ? join(g.parts, g.splits, p.m, p.n, {p.c.p, p.c.ld, p.ctype, 0}, s) : e;
+    return e == hipSuccess && g.splits > 1 ? join(g.parts, g.splits, p.m, p.n, {p.c.p, p.c.ld, p.ctype, 0, nullptr}, s) : e;
 }
 
 }  // namespace fastrack

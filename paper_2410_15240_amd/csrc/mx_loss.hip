@@ -91,13 +91,64 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_
     float v[8];
     load8<kFp32>(z, row * n, c, n, v);
     const int64_t id = id_of(a.ids, row), at = id - (int64_t)a.v0 - c;
-    const float lse = a.lse[row], factor = a.dloss[row * a.dloss_step] * a.scale;
+    const float lse = a.lse[row], factor = factor_of(a, row);
 #pragma unroll
     for (int j = 0; j < 8; ++j)   // (a token that is left out: no gradient, whatever its logits are)
         v[j] = id < 0 || c + j >= n ? 0.0f
                : at == j           ? slope(__builtin_fmaf(v[j], a.scale, -lse), factor)
                                    : factor * exp_of(__builtin_fmaf(v[j], a.scale, -lse));
     store8<T>(a.dz, row * a.ld, c, (uint32_t)a.ld, v);
+}
+
+// The factor dloss * scale that all tokens have in common (a mean's or a sum's loss): out[1] is what
+// bf16 makes of it, out[0] what the results are multiplied by to make up for that. A token's largest
+// gradient is that of its target, near the factor itself while the model is unsure: rounded with
+// the factor, all of them would be off by the same part, up to 2^-8. Where the tokens have several
+// factors (or one far from 1, or none) out is 1 and 0, and each is rounded with its own.
+__global__ __launch_bounds__(1024) void common_kernel(LossTile a, uint32_t m, float *out)
+{
+    constexpr uint32_t K = 8;   // tokens of a thread at a time
+    const uint32_t t = threadIdx.x;
+    __shared__ uint32_t first;
+    if (t == 0)
+        first = m;
+    __syncthreads();
+    // The first token that counts, by the way whether those beside it have its dloss. (A NaN differs from all.)
+    uint32_t f = m;
+    float want = 0.0f;
+    int differ = 0;
+    for (uint32_t i0 = 0; i0 < m && !differ; i0 += 1024 * K) {
+        float v[K];
+        bool counts[K];
+#pragma unroll
+        for (uint32_t k = 0; k < K; ++k) {
+            const uint32_t i = i0 + k * 1024 + t;
+            counts[k] = i < m && id_of(a.ids, i) >= 0;
+            v[k] = i < m ? a.dloss[i * a.dloss_step] : 0.0f;
+        }
+        if (f == m) {   // (the same in all threads)
+#pragma unroll
+            for (int k = (int)K - 1; k >= 0; --k)
+                if (counts[k])
+                    f = i0 + k * 1024 + t;
+            if (f < m)
+                atomicMin(&first, f);
+            __syncthreads();
+            f = first;
+            want = f < m ? a.dloss[f * a.dloss_step] : 0.0f;
+        }
+        int other = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < K; ++k)
+            other |= counts[k] && v[k] != want;
+        differ = __syncthreads_or(other);
+    }
+    if (t == 0) {
+        const float factor = want * a.scale, size = __builtin_fabsf(factor), rounded = (float)(__bf16)factor;
+        const bool one = !differ && size >= 0x1p-100f && size <= 0x1p100f;
+        out[0] = one ? factor / rounded : 1.0f;
+        out[1] = one ? rounded : 0.0f;
+    }
 }
 
 // The result in its own type.
@@ -160,11 +211,12 @@ struct Width {
 struct LossPlan {
     uint64_t piece;
     Width whole, rest;                   // of a piece; of the last one, n = 0 if there is none of its own
-    uint64_t product, z, stats, label, dz, dx;   // bytes
+    uint64_t product, z, stats, label, dz, dx, common;   // bytes
     uint32_t type;                       // of the logits' gradient where it is no bf16 terms
     uint32_t terms_x, terms_w;           // of the logits' gradient that the products take, where it is
+    const float *common_at;              // the results' factor (null: 1)
     const Width &width(uint64_t left) const { return left >= whole.n ? whole : rest; }
-    uint64_t bytes() const { return product + z + stats + label + dz + dx; }
+    uint64_t bytes() const { return product + z + stats + label + dz + dx + common; }
 };
 
 uint64_t parts_of(const Width &w) { return w.tile ? (w.n + w.tile - 1) / w.tile : (w.n + kStatCols - 1) / kStatCols; }
@@ -220,6 +272,7 @@ MxProduct slopes(const Loss &l, const LossPlan &p, const Width &w, void *dz, uin
     r.a = {dz, round_to(w.n, 8)};
     r.plane = l.m * r.a.ld;
     r.m = l.m, r.n = w.n, r.k = l.k;
+    r.scale = p.common_at;
     return r;
 }
 
@@ -252,6 +305,7 @@ LossPlan backward_plan(const Loss &l, int num_cu)
     p.terms_w = l.x8.codes ? terms_of(l.dw_type) : 0;
     const uint32_t terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
     p.type = terms <= 1 ? kBf16 : kFp32;
+    p.common = p.terms_x == 1 || p.terms_w == 1 ? 256 : 0;   // (more terms round nothing that counts)
     p.dx = l.dx.p && l.dx_type != kFp32 && p.whole.n < l.n ? round_to(l.m * l.k * 4, 256) : 0;
     void *const some_place = reinterpret_cast<void *>(256);   // (a plan asks where its float operand lies)
     for (const Width *w : {&p.whole, &p.rest}) {
@@ -327,11 +381,12 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
         p.type = kBf16;
         return l.x8.codes ? multiply(back_w(l, p, {l.n, 0}, 0, nullptr), nullptr, 0, num_cu, s) : hipSuccess;
     }
-    const LossPlan p = backward_plan(l, num_cu);
+    LossPlan p = backward_plan(l, num_cu);
     uint8_t *const work = reinterpret_cast<uint8_t *>(l.work);
     float *const z = reinterpret_cast<float *>(work + p.product);
     uint8_t *const dz = work + p.product + p.z;
-    float *const dx = reinterpret_cast<float *>(dz + p.dz);
+    float *const dx = reinterpret_cast<float *>(dz + p.dz), *const common = reinterpret_cast<float *>(dz + p.dz + p.dx);
+    p.common_at = p.common ? common : nullptr;
     LossTile t = {};
     t.ids = l.ids;
     t.scale = l.scale;
@@ -340,7 +395,13 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
     t.dloss_step = l.dloss_step;
     t.dz = reinterpret_cast<uint16_t *>(dz);
     t.terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
+    t.common = p.common_at;
     hipError_t e;
+    if (p.common) {
+        hipLaunchKernelGGL(common_kernel, dim3(1), dim3(1024), 0, s, t, (uint32_t)l.m, common);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+    }
     for (; t.v0 < l.n; t.v0 += p.width(l.n - t.v0).n) {
         const Width &w = p.width(l.n - t.v0);
         MxProduct g = logits(l, t.v0, w.n, z);
@@ -366,7 +427,7 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
                 return e;
         }
         if (l.dx.p) {
-            const Out o = p.dx ? Out{dx, l.k, kFp32, t.v0 != 0} : Out{l.dx.p, l.dx.ld, l.dx_type, t.v0 != 0};
+            const Out o = p.dx ? Out{dx, l.k, kFp32, t.v0 != 0, nullptr} : Out{l.dx.p, l.dx.ld, l.dx_type, t.v0 != 0, nullptr};
             if ((e = multiply(back_x(l, p, w, t.v0, dz, o), work, p.product, num_cu, s)) != hipSuccess)
                 return e;
         }
@@ -379,7 +440,7 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
     const uint32_t per_row = (uint32_t)((l.k + 7) / 8);
     return over(l.m, per_row, [&](uint64_t row0, dim3 grid) {
         hipLaunchKernelGGL(round_kernel, grid, dim3(kThreads), 0, s, dx, (uint32_t)l.m, (uint32_t)l.k, per_row, div_recip_of(per_row), row0,
-                           Out{l.dx.p, l.dx.ld, l.dx_type, 0});
+                           Out{l.dx.p, l.dx.ld, l.dx_type, 0, nullptr});
     });
 }
 

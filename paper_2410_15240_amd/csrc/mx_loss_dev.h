@@ -26,6 +26,7 @@ struct LossTile {
     uint16_t *dz;            // bf16 terms, rows of ld values
     uint64_t ld, plane;
     uint32_t terms;
+    const float *common;     // [2], see common_kernel (null: no common factor)
 };
 
 // The side of the tiles in which `p` (kLinear) comes out whole, 0 where it does not.
@@ -49,6 +50,13 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
 {
     const float top = larger(a.top, b.top), base = base_of(top);
     return {top, a.sum * exp_of(base_of(a.top) - base) + b.sum * exp_of(base_of(b.top) - base)};
+}
+
+// What a token's gradient is multiplied by: the tokens' common factor as it is in bf16, or its own.
+__device__ __forceinline__ float factor_of(const LossTile &a, uint64_t row)
+{
+    const float common = a.common ? a.common[1] : 0.0f;
+    return common != 0.0f ? common : a.dloss[row * a.dloss_step] * a.scale;
 }
 
 // The gradient of a target's logit, for v = z - lse.

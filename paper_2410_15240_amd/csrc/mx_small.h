@@ -9,6 +9,7 @@ struct Out {
     void *p;
     uint64_t ld;
     uint32_t type, accumulate;
+    const float *scale;      // of the results before put1 or put8 adds or rounds them (launch_mx_dot: none); null: 1
 };
 
 struct SmallProduct {

@@ -402,7 +402,13 @@ __global__ __launch_bounds__(kThreads, S == 2 ? 2 : 4) void small_kernel(SmallPr
     }
     Out o = g.out;
     if (g.cuts > 1)
-        o = {g.parts + (uint64_t)cut * g.m * g.n, g.n, kFp32, 0};
+        o = {g.parts + (uint64_t)cut * g.m * g.n, g.n, kFp32, 0, nullptr};
+    if (o.scale) {
+        const float scale = *o.scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            sum[i] *= scale;
+    }
     put8(o, m0 + y, n0 + x, g.n, sum);
 }
 

@@ -124,7 +124,8 @@ def loss_grad(x, w, ids, dloss, scale, terms, x8, dx_type, dw_type):
     rows = torch.arange(m, device=x.device)[ids >= 0]
     one[rows, ids[ids >= 0]] = 1.0
     dz = factor * (p - one)
-    off_dz = factor.abs() * off_p + 4 * U32 * dz.abs()
+    # (The factor's product, its common part divided out and multiplied in again, the difference's product.)
+    off_dz = factor.abs() * off_p + 8 * U32 * dz.abs()
     res = {}
     for name, a, b, t, sums in (("dx", dz, w, dx_type, n), ("dw", dz.t().contiguous(), x8, dw_type, m)):
         off = off_dz if name == "dx" else off_dz.t().contiguous()

@@ -305,6 +305,33 @@ def test_cross_entropy_over_several_pieces():
         close(dw, o["dw"], o["off_dw"], wt)
 
 
+@pytest.mark.parametrize("m", [40, 700])
+def test_a_common_dloss_does_not_round_every_target_the_same_way(m):
+    """With one factor for all tokens (a mean's loss) bf16 gradients are about as near as their own rounding lets them be;
+    factors of their own, ignored tokens with another one, zeros and infinities go their own way."""
+    gen, x, w, wv, ids = head(m, 4000, 256, "bf16", 31, ignored=0.3)
+    ids[0] = -1
+    x8 = F.mx8_quantize(x)
+    _, lse = F.mx4_cross_entropy(x, w, ids)
+    for factor in (1.0 / 3677, 0.7 * 1.0039, 0.0):   # (1.0039 is near the middle of two bf16 values)
+        dloss = torch.where(ids < 0, 5.0, factor)
+        o = O.loss_grad(x.double(), wv, ids, dloss.double(), 1.0, 1, values(x8), torch.bfloat16, torch.bfloat16)
+        dx, dw = F.mx4_cross_entropy_grad(dloss, x, w, ids, lse, saved=x8, weight_dtype=torch.bfloat16)
+        for got, name in ((dx, "dx"), (dw, "dw")):
+            close(got, o[name], o["off_" + name])
+            if factor:   # the rounding of the results alone is 2^-8 / sqrt(12) of a value's power of two on average
+                assert ((got.double() - o[name]).norm() / o[name].norm()).item() < 1.25 * 2.0 ** -8 / 12 ** 0.5 * 2 / 1.5
+    dloss = torch.rand(m, device="cuda", generator=gen)
+    o = O.loss_grad(x.double(), wv, ids, dloss.double(), 1.0, 1, values(x8), torch.bfloat16, torch.bfloat16)
+    dx, dw = F.mx4_cross_entropy_grad(dloss, x, w, ids, lse, saved=x8, weight_dtype=torch.bfloat16)
+    close(dx, o["dx"], o["off_dx"])
+    close(dw, o["dw"], o["off_dw"])
+    dx = F.mx4_cross_entropy_grad(torch.full((m,), math.inf, device="cuda"), x, w, ids, lse)[0]
+    assert not bool(dx[ids >= 0].isfinite().any()) and bool((dx[ids < 0] == 0).all())
+    dx = F.mx4_cross_entropy_grad(torch.ones(m, device="cuda"), x, w, torch.full_like(ids, -1), lse, saved=x8)
+    assert bool((dx[0] == 0).all()) and bool((dx[1] == 0).all())
+
+
 def test_cross_entropy_grad_against_differences():
     gen, x, w, wv, ids = head(4, 50, 7, "fp32", 12, ignored=0.0)
     ids[2] = -1
