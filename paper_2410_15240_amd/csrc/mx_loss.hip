@@ -78,9 +78,8 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Stat *stats, uint3
     }
 }
 
-// The logits' gradient, dloss (e^(z - lse) - [class = target]) times the scale, in rows of a.ld values
-// that end in zeros.
-template <uint32_t T>
+// The logits' gradient, dloss (e^(z - lse) - [class = target]) times the scale, as bf16 terms in rows of
+// a.ld values that end in zeros.
 __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_t m, uint32_t n, uint32_t per_row, uint32_t recip, uint64_t row0,
                                                          LossTile a)
 {
@@ -97,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_
         v[j] = id < 0 || c + j >= n ? 0.0f
                : at == j           ? slope(__builtin_fmaf(v[j], a.scale, -lse), factor)
                                    : factor * exp_of(__builtin_fmaf(v[j], a.scale, -lse));
-    store8<T>(a.dz, row * a.ld, c, (uint32_t)a.ld, v);
+    put_terms(a.dz + row * a.ld + c, a.plane, a.terms, v);
 }
 
 // The factor dloss * scale that all tokens have in common (a mean's or a sum's loss): out[1] is what
@@ -212,8 +211,7 @@ struct LossPlan {
     uint64_t piece;
     Width whole, rest;                   // of a piece; of the last one, n = 0 if there is none of its own
     uint64_t product, z, stats, label, dz, dx, common;   // bytes
-    uint32_t type;                       // of the logits' gradient where it is no bf16 terms
-    uint32_t terms_x, terms_w;           // of the logits' gradient that the products take, where it is
+    uint32_t terms_x, terms_w;           // bf16 terms of the logits' gradient that the products take
     const float *common_at;              // the results' factor (null: 1)
     const Width &width(uint64_t left) const { return left >= whole.n ? whole : rest; }
     uint64_t bytes() const { return product + z + stats + label + dz + dx + common; }
@@ -262,13 +260,12 @@ LossPlan forward_plan(const Loss &l, int num_cu)
     return p;
 }
 
-// The logits' gradient: one type of float for both products where it goes through a kernel of its own;
-// bf16 terms, as many as each product's result needs, where the tiles' ends write it.
+// A product with the logits' gradient, of which it takes as many terms as its result needs.
 MxProduct slopes(const Loss &l, const LossPlan &p, const Width &w, void *dz, uint32_t terms)
 {
     MxProduct r = {};
-    r.type = w.tile ? (uint32_t)kBf16 : p.type;
-    r.terms = w.tile ? terms : 0;
+    r.type = kBf16;
+    r.terms = terms;
     r.a = {dz, round_to(w.n, 8)};
     r.plane = l.m * r.a.ld;
     r.m = l.m, r.n = w.n, r.k = l.k;
@@ -304,14 +301,13 @@ LossPlan backward_plan(const Loss &l, int num_cu)
     p.terms_x = l.dx.p ? terms_of(l.dx_type) : 0;
     p.terms_w = l.x8.codes ? terms_of(l.dw_type) : 0;
     const uint32_t terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
-    p.type = terms <= 1 ? kBf16 : kFp32;
     p.common = p.terms_x == 1 || p.terms_w == 1 ? 256 : 0;   // (more terms round nothing that counts)
     p.dx = l.dx.p && l.dx_type != kFp32 && p.whole.n < l.n ? round_to(l.m * l.k * 4, 256) : 0;
     void *const some_place = reinterpret_cast<void *>(256);   // (a plan asks where its float operand lies)
     for (const Width *w : {&p.whole, &p.rest}) {
         if (w->n == 0)
             continue;
-        const uint64_t dz = round_to(l.m * round_to(w->n, 8) * (w->tile ? 2 * terms : mx_type_size(p.type)), 256);
+        const uint64_t dz = round_to(l.m * round_to(w->n, 8) * 2 * terms, 256);
         p.dz = dz > p.dz ? dz : p.dz;
         const uint64_t x = l.dx.p ? round_to(mx_product_work(back_x(l, p, *w, 0, some_place, {}), num_cu), 256) : 0;
         const uint64_t g = l.x8.codes ? round_to(mx_product_work(back_w(l, p, *w, 0, some_place), num_cu), 256) : 0;
@@ -378,7 +374,7 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
         return hipSuccess;
     if (l.m == 0) {   // no tokens: a head's gradient of zeros, or the one that is there
         LossPlan p = {};
-        p.type = kBf16;
+        p.terms_w = 1;
         return l.x8.codes ? multiply(back_w(l, p, {l.n, 0}, 0, nullptr), nullptr, 0, num_cu, s) : hipSuccess;
     }
     LossPlan p = backward_plan(l, num_cu);
@@ -416,12 +412,8 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
                 return e;
             const uint32_t per_row = (uint32_t)(t.ld / 8);
             e = over(l.m, per_row, [&](uint64_t row0, dim3 grid) {
-                if (p.type == kBf16)
-                    hipLaunchKernelGGL((slope_kernel<kBf16>), grid, dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, per_row,
-                                       div_recip_of(per_row), row0, t);
-                else
-                    hipLaunchKernelGGL((slope_kernel<kFp32>), grid, dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, per_row,
-                                       div_recip_of(per_row), row0, t);
+                hipLaunchKernelGGL(slope_kernel, grid, dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, per_row,
+                                   div_recip_of(per_row), row0, t);
             });
             if (e != hipSuccess)
                 return e;
