@@ -70,6 +70,7 @@ struct MxProduct {
     uint32_t terms;
     uint64_t plane;
     const float *scale;     // of c, on the device; null: 1
+    bool few;               // kLinear: few tokens always in small tiles
 };
 
 // Workspace that a product needs: the parts of a long sum, and a's bf16 terms where a is not

@@ -694,6 +694,16 @@ Plan plan_of(const MxProduct &p, int num_cu)
         return plan_as(p, kTiles, 128, false, 1);   // no outputs: nothing is launched
     if (p.op == kLinear && p.m <= 2 && p.k >= 512)
         return plan_as(p, kDot, 1, false, 1);
+    const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
+    // A loss's logits of up to 32 tokens, 64 of 16 bits: tiles of 128 and 256 are mostly empty, and
+    // however many of them there are, small ones take less (us with the loss's kernels, as below and
+    // small: 8 tokens of bf16, 4096 x 65536: 113, 57; fp32: 301, 134; 1024 x 32768: 22, 20; 64 of bf16, 4096 x
+    // 65536: 114, 88; fp32: 305, 256, but 1024 x 32768: 40, 46).
+    const uint64_t side = p.m <= 32 ? 32 : 64, few = (p.n + side - 1) / side;
+    if (p.few && p.m <= (p.type == kFp32 ? 32 : 64) && p.k >= 8 && span < 1ull << 31 && few * kSmallThreads < 1ull << 32) {
+        const uint64_t slices = (k + kBK - 1) / kBK, most = slices / 16 < cu / few ? slices / 16 : cu / few;
+        return plan_as(p, kSmall, (uint32_t)side, false, few <= cu / 2 && most > 1 ? most : 1);
+    }
     // gemm_kernel reads whole stages 16 bytes at a time at multiples of 4. Along its rows a may end
     // anywhere (the short stage looks at each value); across them, whole chunks.
     const bool in_place = p.terms || (p.type == kBf16 && reinterpret_cast<uintptr_t>(p.a.p) % 4 == 0 && (p.a.ld % 2 == 0 || p.m == 1) &&
@@ -724,7 +734,6 @@ Plan plan_of(const MxProduct &p, int num_cu)
         as_tiles.decoded = true;
         as_tiles.q_bytes = p.m * mx_blocks(p.k) * 64;
     }
-    const uint64_t span = 64 * (p.a.ld * 4 + mx_blocks(p.k) * 32) + 4096;   // a small tile's offsets in 31 bits
     if (tile == 256 || span >= 1ull << 31 || a_cols < 8 || k == 0 || p.terms > 1)
         return as_tiles;
 

@@ -197,6 +197,7 @@ MxProduct logits(const Loss &l, uint64_t v0, uint64_t n, float *z)
     p.m = l.m, p.n = n, p.k = l.k;
     p.ctype = kFp32;
     p.c = {z, n};
+    p.few = true;
     return p;
 }
 
