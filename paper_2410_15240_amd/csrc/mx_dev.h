@@ -73,17 +73,22 @@ __device__ __forceinline__ void load8(const void *base, uint64_t row_off, uint32
     }
 }
 
-// Eight elements of a row as they lie in memory.
+// Eight elements of a row as they lie in memory. `once`: they are not read again, and the caches need
+// not keep them.
 template <uint32_t T>
 struct Raw8 {
     typedef typename Elem<T>::type E;
     typedef E Ex8 __attribute__((ext_vector_type(8)));
+    typedef E Any8 __attribute__((ext_vector_type(8), aligned(sizeof(E))));
     Ex8 v;
-    __device__ __forceinline__ void load(const void *base, uint64_t row_off, uint32_t c, uint32_t cols)
+    __device__ __forceinline__ void load(const void *base, uint64_t row_off, uint32_t c, uint32_t cols, bool once = false)
     {
         const E *p = reinterpret_cast<const E *>(base) + row_off + c;
         if (c + 8 <= cols) {
-            __builtin_memcpy(&v, p, sizeof v);
+            if (once)
+                v = __builtin_nontemporal_load(reinterpret_cast<const Any8 *>(p));
+            else
+                __builtin_memcpy(&v, p, sizeof v);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)

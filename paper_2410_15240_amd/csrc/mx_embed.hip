@@ -514,7 +514,9 @@ __global__ __launch_bounds__(64 * kOwnWaves, 8) void owned_kernel(Owned g)
 }
 
 // The sums of kChunk sorted tokens, 8 columns to a lane, a wave to a workgroup. All of the tokens' rows
-// are on their way before the first is added. A sum that lies in the chunk whole is put out; one
+// are on their way before the first is added, past the caches, which hold zeros that are still to be
+// written (16384 tokens of 4096 after 1 GiB of zeros: 53 us, kept in them 80, of which the zeros then
+// take 17 less). A sum that lies in the chunk whole is put out; one
 // that goes on from the chunk before is left in part 0, one that begins here and goes on in part 1.
 template <uint32_t T, uint32_t OT>
 __global__ __launch_bounds__(64) void sums_kernel(Sums g)
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(64) void sums_kernel(Sums g)
 #pragma unroll
         for (int i = 0; i < (int)kChunk; ++i)
             if (i < (int)count && key_at(i) < g.rows)
-                raw[i].load(g.dy.p, places[i] * g.dy.ld, c, g.cols);
+                raw[i].load(g.dy.p, places[i] * g.dy.ld, c, g.cols, true);
     if (c >= g.cols)
         return;
     float sum[8] = {};
