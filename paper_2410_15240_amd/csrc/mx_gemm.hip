@@ -10,6 +10,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "launch.h"
 #include "mx.h"
 #include "mx_dev.h"
@@ -64,14 +66,14 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
 // l % 32 of rows 8 (r / 4) + 4 (l / 32) + r % 4 of each. They pass through LDS, 64 rows at a
 // time, so that c is written in whole rows of the tile. Rows whose bit 2 is set are turned by
 // 32 columns: the two halves of a wave then write to different banks.
-template <int N>
+template <int N, bool SCALED = false>
 __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t m,
                                          uint32_t n, const Out &o)
 {
     constexpr uint32_t B = 64 * N;
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
     float scale = 1.0f;
-    if (o.scale)
+    if (SCALED && o.scale)   // (a part of a sum has none)
         scale = *o.scale;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -93,7 +95,7 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
             const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
             const f32x4 lo = p[0], hi = p[1];
             float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (o.scale)
+            if (SCALED)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     v[e] *= scale;
@@ -103,7 +105,9 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[N][N], float *lds, 
     }
 }
 
-// The end of a tile: its results to c, or to their part of a sum.
+// The end of a tile: its results to c, or to their part of a sum; SCALED: by g.scale. (Looking for a
+// scale in every product costs a large one 1% of its time.)
+template <bool SCALED>
 struct Store {
     template <int N>
     __device__ __forceinline__ void finish(const f32x16 (&acc)[N][N], float *lds, uint32_t m0, uint32_t n0, uint32_t part,
@@ -112,7 +116,7 @@ struct Store {
         Out o = {g.c, g.ldc, g.ctype, g.accumulate, g.scale};
         if (g.splits > 1)
             o = {g.parts + (uint64_t)part * g.m * g.n, g.n, kFp32, 0, nullptr};
-        put_tile<N>(acc, lds, m0, n0, g.m, g.n, o);
+        put_tile<N, SCALED>(acc, lds, m0, n0, g.m, g.n, o);
     }
 };
 
@@ -1122,10 +1126,10 @@ static Gemm gemm_of(const MxProduct &p, const Plan &r, const MxRows &a, const Mx
     return g;
 }
 
+template <class End>
 static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &a, const MxMatrix &q, float *parts,
                                hipStream_t s)
 {
-    typedef Store End;
     const End end;
     const Gemm g = gemm_of(p, r, a, q, parts);
     const dim3 grid(r.tm * r.tn * r.splits);
@@ -1136,9 +1140,10 @@ static hipError_t launch_tiles(const MxProduct &p, const Plan &r, const MxRows &
         else                                                                                      \
             hipLaunchKernelGGL((gemm_kernel<__VA_ARGS__, 2, End>), grid, dim3(kThreads), 0, s, g, end);     \
     } while (0)
-    if (p.op == kLinear)
-        MX_GEMM(kMx4, false, false);
-    else if (p.op == kGradInput)
+    if (p.op == kLinear) {
+        if constexpr (std::is_same<End, Store<false>>::value)   // (none is scaled)
+            MX_GEMM(kMx4, false, false);
+    } else if (p.op == kGradInput)
         MX_GEMM(kMx4, false, true);
     else if (!r.decoded)
         MX_GEMM(kMx8, true, true);
@@ -1212,7 +1217,8 @@ hipError_t launch_mx_product(const MxProduct &p, int num_cu, hipStream_t s)
     }
     hipError_t e;
     if (r.path == kTiles) {
-        e = launch_tiles(p, r, a, q, parts, s);
+        e = p.scale && r.splits == 1 ? launch_tiles<Store<true>>(p, r, a, q, parts, s)
+                                     : launch_tiles<Store<false>>(p, r, a, q, parts, s);
     } else {
         SmallProduct g = {};
         g.a = a;
