@@ -549,8 +549,10 @@ int fastrack_mx_norm_grad(uint32_t type, const void *d_dy, uint64_t ld_dy, const
  *              dw[v][k] = sum over t of dz[t][v] x^[t][k], x kept in MX8 (d_dw NULL: not
  *              computed); added to what d_dw holds where accumulate is 1 (32-bit only)
  * from the same x, w, ids and scale and the lse that they gave. The logits are computed
- * again, a piece of the vocabulary at a time. dz is rounded once to bf16 for a gradient in
- * bf16 and taken as two or three bf16 terms for one in fp16 or fp32; sums are in 32 bits.
+ * again, a piece of the vocabulary at a time. For a gradient in bf16 dz is rounded once to
+ * bf16, for one in fp16, or of up to 32 tokens, taken as two bf16 terms, for one in fp32 as
+ * three (each the nearest to what is left); sums are in 32 bits. A dloss that all tokens
+ * that count have in common is multiplied in after the sums.
  * d_loss, d_lse, d_dloss: 32-bit floats [m], d_dloss `dloss_step` elements apart (0: one for
  * all). d_work: fastrack_mx_loss_work_bytes(...) or fastrack_mx_loss_grad_work_bytes(...)
  * bytes, 16-byte aligned; they depend on x's address and stride and on the device; dx and

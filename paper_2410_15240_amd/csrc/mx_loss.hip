@@ -99,11 +99,12 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_
     put_terms(a.dz + row * a.ld + c, a.plane, a.terms, v);
 }
 
-// The factor dloss * scale that all tokens have in common (a mean's or a sum's loss): out[1] is what
-// bf16 makes of it, out[0] what the results are multiplied by to make up for that. A token's largest
-// gradient is that of its target, near the factor itself while the model is unsure: rounded with
-// the factor, all of them would be off by the same part, up to 2^-8. Where the tokens have several
-// factors (or one far from 1, or none) out is 1 and 0, and each is rounded with its own.
+// The factor dloss * scale that all tokens have in common (a mean's or a sum's loss) does not have to be
+// in the logits' gradient: out[1], 255 / 128, stands there for it, and out[0] makes up for that in the
+// results. A token's largest gradient is that of its target, p - 1 of the factor. Rounded to bf16 with
+// whatever factor, all of them would be off by the same part, up to 2^-8, while the model is unsure
+// (p near 0); of 255 / 128 itself nothing is lost, and of what lies below it least. Where the tokens have
+// several factors (or one far from 1, or none) out is 1 and 0, and each is rounded with its own.
 __global__ __launch_bounds__(1024) void common_kernel(LossTile a, uint32_t m, float *out)
 {
     constexpr uint32_t K = 8;   // tokens of a thread at a time
@@ -143,10 +144,10 @@ __global__ __launch_bounds__(1024) void common_kernel(LossTile a, uint32_t m, fl
         differ = __syncthreads_or(other);
     }
     if (t == 0) {
-        const float factor = want * a.scale, size = __builtin_fabsf(factor), rounded = (float)(__bf16)factor;
+        const float factor = want * a.scale, size = __builtin_fabsf(factor), common = 255.0f / 128.0f;
         const bool one = !differ && size >= 0x1p-100f && size <= 0x1p100f;
-        out[0] = one ? factor / rounded : 1.0f;
-        out[1] = one ? rounded : 0.0f;
+        out[0] = one ? factor / common : 1.0f;
+        out[1] = one ? common : 0.0f;
     }
 }
 
@@ -220,7 +221,9 @@ struct LossPlan {
 
 uint64_t parts_of(const Width &w) { return w.tile ? (w.n + w.tile - 1) / w.tile : (w.n + kStatCols - 1) / kStatCols; }
 
-uint32_t terms_of(uint32_t type) { return type == kBf16 ? 1 : type == kFp16 ? 2 : 3; }
+// bf16 terms of the logits' gradient for a result of this type. One for bf16, whose own rounding is as
+// large; but of few tokens, whose errors do not even out, two.
+uint32_t terms_of(uint32_t type, uint64_t m) { return type == kBf16 ? (m <= 32 ? 2 : 1) : type == kFp16 ? 2 : 3; }
 
 }  // namespace mx
 
@@ -299,8 +302,8 @@ MxProduct back_w(const Loss &l, const LossPlan &p, const Width &w, uint64_t v0, 
 LossPlan backward_plan(const Loss &l, int num_cu)
 {
     LossPlan p = plan_of(l, num_cu, kBackwardValues);
-    p.terms_x = l.dx.p ? terms_of(l.dx_type) : 0;
-    p.terms_w = l.x8.codes ? terms_of(l.dw_type) : 0;
+    p.terms_x = l.dx.p ? terms_of(l.dx_type, l.m) : 0;
+    p.terms_w = l.x8.codes ? terms_of(l.dw_type, l.m) : 0;
     const uint32_t terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
     p.common = p.terms_x == 1 || p.terms_w == 1 ? 256 : 0;   // (more terms round nothing that counts)
     p.dx = l.dx.p && l.dx_type != kFp32 && p.whole.n < l.n ? round_to(l.m * l.k * 4, 256) : 0;

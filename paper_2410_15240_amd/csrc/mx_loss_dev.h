@@ -52,7 +52,7 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
     return {top, a.sum * exp_of(base_of(a.top) - base) + b.sum * exp_of(base_of(b.top) - base)};
 }
 
-// What a token's gradient is multiplied by: the tokens' common factor as it is in bf16, or its own.
+// What a token's gradient is multiplied by: what stands for the tokens' common factor, or its own.
 __device__ __forceinline__ float factor_of(const LossTile &a, uint64_t row)
 {
     const float common = a.common ? a.common[1] : 0.0f;
