@@ -60,16 +60,43 @@ __device__ __forceinline__ float square_sum(const float (&v)[8])
     return s;
 }
 
-__device__ __forceinline__ float inverse_rms(float squares, uint32_t cols, float eps)
+// 1 / rms as the float next to it and what that leaves, from a row's threads' sums of squares. Those are
+// in 32 bits, what is made of them in 64: a row's error would be in all of its values alike, and a
+// value next to the border of two of its 8 bits' codes would go to the other one.
+struct Inverse {
+    float hi, lo;
+    __device__ __forceinline__ float times(float v) const { return __builtin_fmaf(v, hi, v * lo); }
+};
+
+template <int G>
+__device__ __forceinline__ Inverse inverse_rms(float squares, uint32_t cols, float eps, double (*lds)[16], int slot)
 {
-    return 1.0f / sqrtf(squares / (float)cols + eps);
+    double s = (double)squares;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+        s += __shfl_xor(s, d, 64);
+    if (G > 64) {
+        if (threadIdx.x % 64 == 0)
+            lds[slot][threadIdx.x / 64] = s;
+        __syncthreads();
+        s = 0.0;
+#pragma unroll
+        for (int w = 0; w < G / 64; ++w)
+            s += lds[slot][w];
+    }
+    const double mean = s / (double)cols + (double)eps;
+    // A Newton step of 1 / sqrt takes 32 bits' error to its square.
+    const double near = (double)(1.0f / sqrtf((float)mean)), inv = near * (1.5 - 0.5 * mean * near * near);
+    // (0, infinity and NaN as the first value has them)
+    const float hi = near > 0.0 && near < (double)__builtin_inff() ? (float)inv : (float)near, lo = (float)(inv - (double)hi);
+    return {hi, __builtin_fabsf(lo) < __builtin_fabsf(hi) ? lo : 0.0f};
 }
 
 template <uint32_t T, int G, int U>
 __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t row0)
 {
     constexpr int N = U ? U : 1, R = threads_of<G>() / G;
-    __shared__ float lds[2][16];
+    __shared__ double lds[2][16];
     const uint32_t t = threadIdx.x % G, cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols));
     const uint64_t row = row0 + (uint64_t)blockIdx.x * R + threadIdx.x / G;
     if (row >= n.rows)   // (a whole wave, or a whole workgroup)
@@ -86,16 +113,16 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
         }
     };
     float h[N][8];
-    float inv1 = 1.0f;
+    Inverse inv1 = {1.0f, 0.0f};
     if (n.w1) {
         float s = 0.0f;
         each([&](int i, uint32_t j) {
             load8<T>(n.x.p, row * n.x.ld, j * 8, cols, h[i]);
             s += square_sum(h[i]);
         });
-        inv1 = inverse_rms(row_sum<G>(s, lds, 0), cols, n.eps);
+        inv1 = inverse_rms<G>(s, cols, n.eps, lds, 0);
         if (t == 0)
-            n.inv1[row] = inv1;
+            n.inv1[row] = inv1.hi;
     }
     // h of a unit, and on the way (`keep`) what is kept of x and g.
     auto hidden = [&](int i, uint32_t j, bool keep) {
@@ -106,7 +133,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
         if (n.w1)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                h[i][e] *= inv1;
+                h[i][e] = inv1.times(h[i][e]);
         if (keep && n.v.codes)
             put<kMx8>(n.v, u, h[i]);
         if (n.w1) {
@@ -141,16 +168,16 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
         if (n.h.p)
             store8<T>(n.h.p, row * n.h.ld, j * 8, cols, h[i]);
     });
-    const float inv2 = inverse_rms(row_sum<G>(s, lds, 1), cols, n.eps);
+    const Inverse inv2 = inverse_rms<G>(s, cols, n.eps, lds, 1);
     if (t == 0)
-        n.inv2[row] = inv2;
+        n.inv2[row] = inv2.hi;
     each([&](int i, uint32_t j) {
         if (!U)
             hidden(i, j, false);
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            h[i][e] *= inv2;
+            h[i][e] = inv2.times(h[i][e]);
         put<kMx8>(n.u, unit_at(row, j, units), h[i]);
         weights8<T>(n.w2, n.wtype, j * 8, cols, w);
 #pragma unroll
