@@ -1,6 +1,9 @@
 // The norm between two blocks of a model, with what stands around it: the block's own norm, its
 // gate, the residual and its scale. Forwards in one pass, with what the gradient needs kept in 8
-// bits; backwards in one pass over that.
+// bits; backwards in one pass over that. Every value is read once and written once: what bounds it
+// is HBM. 4096 rows of 8192 of bf16 with a norm, a gate and a residual: forwards 438 MB in 97-99 us,
+// 4.4-4.5 TB/s (the VALU busy half of it), backwards 439 MB in 96-99 and 5 for the weights' sums; a
+// device copy runs at 5.2.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -15,6 +18,14 @@ namespace mx {
 // which stay in its registers from the row's sum to its end. U = 0: rows of any length, read again
 // after each sum.
 template <int G> constexpr int threads_of() { return G < 128 ? 256 : G; }
+
+// Which of a workgroup's rows is this thread's: the same for a whole wave, so that addresses are
+// computed once for it.
+template <int G>
+__device__ __forceinline__ uint32_t part_of()
+{
+    return threads_of<G>() == G ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / G);
+}
 
 // The sum over the G threads of a row, to all of them. `slot` takes turns between 0 and 1: what one
 // sum leaves in LDS is read until the next one's barrier.
@@ -98,7 +109,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
     constexpr int N = U ? U : 1, R = threads_of<G>() / G;
     __shared__ double lds[2][16];
     const uint32_t t = threadIdx.x % G, cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols));
-    const uint64_t row = row0 + (uint64_t)blockIdx.x * R + threadIdx.x / G;
+    const uint64_t row = row0 + (uint64_t)blockIdx.x * R + part_of<G>();
     if (row >= n.rows)   // (a whole wave, or a whole workgroup)
         return;
     auto each = [&](auto f) {
@@ -187,7 +198,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
     });
 }
 
-// How rows of a length are shared out. (Measured choices stand at the launches.)
+// How rows of a length are shared out: threads of a row and units of a thread.
 enum Way : int { kWave1, kWave, k128x1, k256x1, k256x2, k256x4, k512x1, k1024x1, k1024x2, k1024x4, kLoop };
 
 // ---- backwards -----------------------------------------------------------------------------------
@@ -211,10 +222,12 @@ template <uint32_t T, int G, int U>
 __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad n, uint32_t groups)
 {
     constexpr int R = threads_of<G>() / G;
-    constexpr bool AHEAD = U == 1;   // (two units leave no registers for a second row, nor for the weights)
+    // Two units leave no registers for a second row, for the weights, nor for the sums: these are in LDS.
+    constexpr bool AHEAD = U == 1;
     __shared__ float lds[2][16];
+    __shared__ f32x4 sums[AHEAD ? 1 : 2][AHEAD ? 1 : 2][AHEAD ? 1 : U * G];   // of dw2, dw1; halves of a unit
     const uint32_t t = threadIdx.x % G, cols = (uint32_t)n.cols, units = (uint32_t)(4 * mx_blocks(cols));
-    const uint32_t group = blockIdx.x * R + threadIdx.x / G;
+    const uint32_t group = blockIdx.x * R + part_of<G>();
     if (group >= groups)
         return;
     auto each = [&](auto f) {
@@ -224,6 +237,30 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
                 f(i, t + i * G);
     };
     float sum2[U][8] = {}, sum1[U][8] = {}, w2[U][8], w1[U][8];
+    if (!AHEAD)
+        each([&](int, uint32_t j) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                sums[AHEAD ? 0 : k / 2][AHEAD ? 0 : k % 2][AHEAD ? 0 : j] = f32x4{0, 0, 0, 0};
+        });
+    // sum += x y, of the registers or of the LDS (each unit there is one thread's).
+    auto add = [&](float (&sum)[8], int which, uint32_t j, const float (&x)[8], const float (&y)[8]) {
+        if (AHEAD) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                sum[e] = __builtin_fmaf(x[e], y[e], sum[e]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4 &at = sums[AHEAD ? 0 : which][AHEAD ? 0 : h][AHEAD ? 0 : j];
+                f32x4 v = at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = __builtin_fmaf(x[4 * h + e], y[4 * h + e], v[e]);
+                at = v;
+            }
+        }
+    };
     auto weights = [&](int i, uint32_t j) {
         weights8<T>(n.w2, n.wtype, j * 8, cols, w2[i]);
         if (n.w1)
@@ -239,25 +276,23 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
             r[i].eu = n.u.scales[u.block];
         });
     };
-    auto fetch_others = [&](uint64_t row, GradRow<T> (&r)[U]) {
-        each([&](int i, uint32_t j) {
-            const Unit u = unit_at(row, j, units);
-            if (n.dh.p)
-                r[i].dh.load(n.dh.p, row * n.dh.ld, u.c, cols);
-            if (n.v.codes) {
-                r[i].v = reinterpret_cast<const u32x2 *>(n.v.codes)[u.block * 4 + u.lane];
-                r[i].ev = n.v.scales[u.block];
-            }
-            if (n.gq.codes) {
-                r[i].g = reinterpret_cast<const u32x2 *>(n.gq.codes)[u.block * 4 + u.lane];
-                r[i].eg = n.gq.scales[u.block];
-            }
-        });
+    auto fetch_rest = [&](uint64_t row, GradRow<T> &r, uint32_t j) {
+        const Unit u = unit_at(row, j, units);
+        if (n.dh.p)
+            r.dh.load(n.dh.p, row * n.dh.ld, u.c, cols);
+        if (n.v.codes) {
+            r.v = reinterpret_cast<const u32x2 *>(n.v.codes)[u.block * 4 + u.lane];
+            r.ev = n.v.scales[u.block];
+        }
+        if (n.gq.codes) {
+            r.g = reinterpret_cast<const u32x2 *>(n.gq.codes)[u.block * 4 + u.lane];
+            r.eg = n.gq.scales[u.block];
+        }
     };
     GradRow<T> now[U], next[U];
     if (AHEAD && group < n.rows) {
         fetch_first(group, now);
-        fetch_others(group, now);
+        each([&](int i, uint32_t j) { fetch_rest(group, now[i], j); });
     }
     for (uint64_t row = group; row < n.rows; row += groups) {
         const float inv2 = n.inv2[row], inv1 = n.w1 ? n.inv1[row] : 0.0f;
@@ -265,7 +300,7 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
             fetch_first(row, now);
         } else if (row + groups < n.rows) {
             fetch_first(row + groups, next);
-            fetch_others(row + groups, next);
+            each([&](int i, uint32_t j) { fetch_rest(row + groups, next[i], j); });
         }
         float d[U][8], a[U][8];   // dy w2 and then what goes on; u and then v
         float s = 0.0f;
@@ -274,18 +309,20 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
                 weights8<T>(n.w2, n.wtype, j * 8, cols, w2[i]);
             decode8_f32(now[i].u, scale8_f32(now[i].eu), a[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8; ++e)
                 d[i][e] = (float)now[i].dy.v[e];
-                sum2[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum2[i][e]);
+            add(sum2[i], 0, j, d[i], a[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
                 d[i][e] *= w2[i][e];
                 s = __builtin_fmaf(d[i][e], a[i][e], s);
             }
         });
         const float along2 = row_sum<G>(s, lds, 0) / (float)cols;
-        if (!AHEAD)
-            fetch_others(row, now);
         s = 0.0f;
         each([&](int i, uint32_t j) {
+            if (!AHEAD)
+                fetch_rest(row, now[i], j);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 d[i][e] = inv2 * __builtin_fmaf(-along2, a[i][e], d[i][e]);
@@ -316,9 +353,9 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
                 store8<T>(n.dx.p, row * n.dx.ld, j * 8, cols, d[i]);
                 return;
             }
+            add(sum1[i], 1, j, d[i], a[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                sum1[i][e] = __builtin_fmaf(d[i][e], a[i][e], sum1[i][e]);
                 d[i][e] *= w1[i][e];
                 s = __builtin_fmaf(d[i][e], a[i][e], s);
             }
@@ -339,6 +376,12 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
     }
     float *const part2 = n.work + (uint64_t)group * cols, *const part1 = part2 + (uint64_t)groups * cols;
     each([&](int i, uint32_t j) {
+        if (!AHEAD)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum2[i][e] = sums[0][AHEAD ? 0 : e / 4][AHEAD ? 0 : j][e % 4];
+                sum1[i][e] = sums[AHEAD ? 0 : 1][AHEAD ? 0 : e / 4][AHEAD ? 0 : j][e % 4];
+            }
         store8<kFp32>(part2, 0, j * 8, cols, sum2[i]);
         if (n.w1)
             store8<kFp32>(part1, 0, j * 8, cols, sum1[i]);
@@ -464,6 +507,11 @@ __global__ __launch_bounds__(1024) void columns_kernel(const float *work, uint32
 
 using namespace mx;
 
+// Rows that fill the GPU: as few threads of a row as hold it (us, 4096 rows of bf16 with all operands: 1024
+// columns a wave 13.7, 256 threads 17.3, 1024 42.8; 4096 columns 256 threads 43.6, 1024 66.4; 8192
+// columns 96.7, 98.6). Few rows: more of them (1 row: 1024 columns a wave 6.5, 256 threads 5.1; 4096
+// columns 256 threads 7.3, 1024 5.9; 8192 columns 11.5, 7.3; 100 rows of 2048 5.6, 6.0; 300 rows of 8192 16.1,
+// 13.4).
 static Way forward_way(uint64_t rows, uint64_t cols, int num_cu)
 {
     const uint64_t units = 4 * mx_blocks(cols);
@@ -471,9 +519,10 @@ static Way forward_way(uint64_t rows, uint64_t cols, int num_cu)
         return kLoop;
     if (units > 1024)
         return k1024x4;
-    if (units <= 128)
-        return kWave;
-    if (rows < (uint64_t)num_cu)
+    const bool few = rows < (uint64_t)num_cu;
+    if (few ? units <= 256 : units <= 128)
+        return few ? k256x1 : kWave;
+    if (few || (units > 512 && rows <= 2 * (uint64_t)num_cu))
         return k1024x1;
     return units <= 256 ? k256x1 : units <= 512 ? k256x2 : k256x4;
 }
@@ -508,17 +557,20 @@ hipError_t launch_mx_norm(const Norm &n, int num_cu, hipStream_t s)
     return hipSuccess;
 }
 
+// A unit to a thread, which leaves registers for the next row (4096 rows of 4096: 512 threads 50.8 us, 1024
+// 60.9); two up to 16384 columns (2048 such rows: 166 us, read again after each sum 240).
 static Way backward_way(uint64_t cols)
 {
     const uint64_t units = 4 * mx_blocks(cols);
     return units <= 64 ? kWave1 : units <= 128 ? k128x1 : units <= 256 ? k256x1 : units <= 512 ? k512x1 : units <= 1024 ? k1024x1 : units <= 2048 ? k1024x2 : kLoop;
 }
 
-// Groups that take the rows in turn: as many as run at once, 16 waves to a CU.
+// Groups that take the rows in turn: as many as run at once, 16 waves to a CU; of short rows fewer, since
+// each leaves sums behind (4096 rows of 512: 1024 groups 19.1 us, 2048 21.5, 4096 29.1).
 static uint32_t groups_of(uint64_t rows, uint64_t cols, int num_cu)
 {
     const Way way = backward_way(cols);
-    const uint64_t most = (uint64_t)num_cu * (way == kWave1 ? 16 : way == k128x1 ? 8 : way == k256x1 ? 4 : way == k512x1 ? 2 : 1);
+    const uint64_t most = (uint64_t)num_cu * (way == k512x1 ? 2 : way == k1024x1 || way == k1024x2 || way == kLoop ? 1 : 4);
     return (uint32_t)(rows < most ? rows : most);
 }
 
