@@ -557,7 +557,7 @@ int fastrack_mx_norm_grad(uint32_t type, const void *d_dy, uint64_t ld_dy, const
  * all). d_work: fastrack_mx_loss_work_bytes(...) or fastrack_mx_loss_grad_work_bytes(...)
  * bytes, 16-byte aligned; they depend on x's address and stride and on the device; dx and
  * dw say which gradients are wanted.
- * EINVAL too: n = 0 with m > 0; more than 2^24 - 1 tokens; more than 2^24 output tiles of
+ * EINVAL too: n = 0 with m > 0; more than 2^22 - 1 tokens; more than 2^24 output tiles of
  * 128 x 128 in a gradient.
  */
 uint64_t fastrack_mx_loss_work_bytes(uint32_t type, const void *d_x, uint64_t ldx, uint64_t m, uint64_t n, uint64_t k);

@@ -46,10 +46,13 @@ __device__ __forceinline__ float larger(float a, float b) { return a > b || a !=
 constexpr float kLog2e = 1.44269504f;
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 
+// (Of no logits, or none but -inf, the sum is 0, whatever the other one's largest value makes of it.)
+__device__ __forceinline__ float over(const Stat &s, float base) { return s.sum == 0.0f ? 0.0f : s.sum * exp_of(base_of(s.top) - base); }
+
 __device__ __forceinline__ Stat join(const Stat &a, const Stat &b)
 {
     const float top = larger(a.top, b.top), base = base_of(top);
-    return {top, a.sum * exp_of(base_of(a.top) - base) + b.sum * exp_of(base_of(b.top) - base)};
+    return {top, over(a, base) + over(b, base)};
 }
 
 // What a token's gradient is multiplied by: what stands for the tokens' common factor, or its own.

@@ -71,7 +71,7 @@ int check_norm_types(uint32_t type, uint32_t wtype)
     return FASTRACK_OK;
 }
 
-constexpr uint64_t kMostPieces = (1ull << 24) - 1;   // workgroups of 256 threads: fewer than 2^32 of these
+constexpr uint64_t kMostTokens = (1ull << 22) - 1;   // workgroups of 1024 threads: fewer than 2^32 of these
 
 }  // namespace
 
@@ -268,8 +268,8 @@ int check_loss(const Loss &l)
     FT_TRY(check_index(l.ids.wide));
     FT_TRY(check_type(l.type));
     FT_TRY(check_dims(l.m, l.n, l.k));
-    if (l.m > kMostPieces)
-        return fail(FASTRACK_EINVAL, "more than 2^24 - 1 tokens");
+    if (l.m > kMostTokens)
+        return fail(FASTRACK_EINVAL, "more than 2^22 - 1 tokens");
     if (l.m && l.n == 0)
         return fail(FASTRACK_EINVAL, "a vocabulary of no classes");
     if ((l.n + 127) / 128 * ((l.k + 127) / 128) > 1ull << 24 || (l.m + 127) / 128 * ((l.k + 127) / 128) > 1ull << 24)
@@ -283,7 +283,7 @@ int check_loss(const Loss &l)
 
 FT_EXPORT uint64_t fastrack_mx_loss_work_bytes(uint32_t type, const void *d_x, uint64_t ldx, uint64_t m, uint64_t n, uint64_t k)
 {
-    if (type > kFp32 || m > kMostPieces || n > kMaxDim || k > kMaxDim)
+    if (type > kFp32 || m > kMostTokens || n > kMaxDim || k > kMaxDim)
         return 0;
     return mx_loss_work(loss_of(type, d_x, ldx, nullptr, nullptr, 0, nullptr, m, n, k, 1.0f), num_cu());
 }
@@ -313,7 +313,7 @@ FT_EXPORT int fastrack_mx_loss(uint32_t type, const void *d_x, uint64_t ldx, con
 FT_EXPORT uint64_t fastrack_mx_loss_grad_work_bytes(uint32_t type, const void *d_x, uint64_t ldx, uint64_t m, uint64_t n, uint64_t k,
                                                     uint32_t dx, uint32_t dx_type, uint32_t dw, uint32_t dw_type)
 {
-    if (type > kFp32 || dx_type > kFp32 || dw_type > kFp32 || m > kMostPieces || n > kMaxDim || k > kMaxDim)
+    if (type > kFp32 || dx_type > kFp32 || dw_type > kFp32 || m > kMostTokens || n > kMaxDim || k > kMaxDim)
         return 0;
     Loss l = loss_of(type, d_x, ldx, nullptr, nullptr, 0, nullptr, m, n, k, 1.0f);
     uint8_t some;   // (the plan asks which gradients there are, not where)

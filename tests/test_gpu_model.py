@@ -377,6 +377,30 @@ def test_logits_far_apart_infinite_and_nan(m, v, k):
     assert bool(loss[1:].isfinite().all()) and not bool(lse[0].isfinite())
 
 
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+@pytest.mark.parametrize("m,v,k", [(1, 5000, 1024), (3, 700, 64), (40, 300000, 64), (700, 9000, 64)])
+def test_logits_that_are_all_far_from_zero(m, v, k, scale):
+    """All far below it, all far above it, and some of each row -inf: what holds no class, or none but -inf, adds nothing."""
+    gen = generator(m + v)
+    w = F.mx4_quantize(torch.rand(v, k, device="cuda", generator=gen) + 0.5)
+    x = -(torch.rand(m, k, device="cuda", generator=gen) * 20 + 20).bfloat16()
+    ids = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    loss, lse = F.mx4_cross_entropy(x, w, ids, scale=scale)
+    o = O.loss(x.double(), F.mx4_dequantize(w, dtype=torch.float32).double(), ids, scale, 1)
+    assert bool((o["z"] * scale < -500).all())
+    close(lse, o["lse"], o["off_lse"])
+    close(loss, o["loss"], o["off_loss"])
+    w.codes[: v // 2] |= 0x88    # half of the classes the other way round
+    w.scales[: v // 2] = 254     # and out of range: +-inf
+    lse = F.mx4_cross_entropy(-x * scale, w, ids)[1]
+    half = F.MX4(w.codes[v // 2:].contiguous(), w.scales[v // 2:].contiguous(), k)
+    want = F.mx4_cross_entropy(-x * scale, half, ids.clamp(max=v - v // 2 - 1))[1]
+    if scale > 0:
+        assert bool(lse.isfinite().all()) and torch.allclose(lse, want, rtol=1e-6)
+    else:
+        assert bool((lse == math.inf).all())
+
+
 def test_no_tokens():
     _, x, w, _, ids = head(4, 60, 40, "bf16", 2)
     x8 = F.mx8_quantize(x[:0])

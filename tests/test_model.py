@@ -150,7 +150,7 @@ def loss(L, type=BF16, x=AT[0], ldx=64, codes=AT[1], scales=AT[2], itype=1, ids=
 
 
 @pytest.mark.parametrize("kw", [dict(type=3), dict(x=None), dict(x=AT[0] + 1), dict(codes=None), dict(codes=AT[1] + 8), dict(scales=None),
-                                dict(itype=2), dict(ids=None), dict(ids=AT[3] + 4), dict(m=1 << 24), dict(n=1 << 31), dict(n=0),
+                                dict(itype=2), dict(ids=None), dict(ids=AT[3] + 4), dict(m=1 << 22), dict(n=1 << 31), dict(n=0),
                                 dict(out=None), dict(lse=None), dict(lse=AT[5] + 2), dict(work=None), dict(size=100), dict(work=AT[6] + 8),
                                 dict(out=AT[5] + 8), dict(out=AT[0]), dict(lse=AT[3]), dict(work=AT[1]), dict(n=1 << 30, k=1 << 10)])
 def test_loss_refuses(L, kw):
@@ -164,7 +164,7 @@ def loss_grad(L, type=BF16, x=AT[0], ldx=64, codes=AT[1], scales=AT[2], xc=AT[3]
 
 
 @pytest.mark.parametrize("kw", [dict(type=3), dict(x=None), dict(codes=None), dict(xc=None), dict(xs=None), dict(xc=AT[3] + 8), dict(itype=2),
-                                dict(ids=None), dict(dloss=None), dict(dloss=AT[6] + 2), dict(step=1 << 41), dict(lse=None), dict(m=1 << 24),
+                                dict(ids=None), dict(dloss=None), dict(dloss=AT[6] + 2), dict(step=1 << 41), dict(lse=None), dict(m=1 << 22),
                                 dict(n=0), dict(xt=3), dict(wt=3), dict(ldd=63), dict(ldw=63), dict(acc=2), dict(acc=1, wt=BF16),
                                 dict(work=None), dict(size=100), dict(dx=AT[0]), dict(dw=AT[8]), dict(dw=AT[1]), dict(dx=AT[7]),
                                 dict(work=AT[6]), dict(dw=AT[3]), dict(dx=AT[6] + 12 * 8, step=8), dict(n=1 << 30, k=1 << 10)])
