@@ -485,11 +485,11 @@ enum fastrack_index { FASTRACK_I32 = 0, FASTRACK_I64 = 1 };
  * id is padding: its row is 0, and it counts for nothing in the gradient. An id of `rows`
  * or more is a mistake that the device alone can see: its row is NaN.
  *   embedding_grad  dw[i][k] = scale * sum of dy[t][k] over the t with id_t = i, added in
- *                   the order of t (so that it is the same every time) within runs of 16
- *                   sorted tokens, and these in their order; added to what d_dw holds
- *                   where accumulate is 1 (32-bit d_dw only). Ids of `rows` or more
- *                   count for nothing.
- * d_work: fastrack_mx_embedding_grad_work_bytes(...) bytes, 16-byte aligned.
+ *                   an order that the ids and the sizes alone decide (so it is the same
+ *                   every time); rows that no id names become 0. Added to what d_dw
+ *                   holds where accumulate is 1 (32-bit d_dw only): those rows are then
+ *                   left as they are. Ids of `rows` or more count for nothing.
+ * d_work: fastrack_mx_embedding_grad_work_bytes(...) bytes, 16-byte aligned (NULL if 0).
  * EINVAL too: 2^26 pieces of 16 tokens and 512 columns, or more (of the gradient).
  */
 int fastrack_mx_embedding(uint32_t index_type, const void *d_ids, uint64_t m, const uint8_t *d_codes, const uint8_t *d_scales,
@@ -518,8 +518,9 @@ int fastrack_mx_embedding_grad(uint32_t index_type, const void *d_ids, uint32_t 
  *   db = scale * gate^ * dh,  dgate = scale * dh * (v * post_weight, or x^)
  *   dpost_weight = sum over rows of db v
  *   dx = post_inverse * (t1 - v * mean(t1 v)), t1 = db * post_weight; without one dx = db
- * dweight and dpost_weight are 32-bit floats [cols], added in an order that is the same
- * every time. d_work: fastrack_mx_norm_grad_work_bytes(rows, cols, has post_weight) bytes,
+ * Each is the gradient of every row: that of a residual or a gate whose one row stands for
+ * all is the sum of theirs. dweight and dpost_weight are 32-bit floats [cols], added in an
+ * order that is the same every time. d_work: fastrack_mx_norm_grad_work_bytes(rows, cols, has post_weight) bytes,
  * 16-byte aligned. EINVAL too: eps negative or not finite, a scale that is no number.
  */
 int fastrack_mx_norm(uint32_t type, const void *d_x, uint64_t ldx, const void *d_residual, uint64_t ld_residual,
