@@ -162,7 +162,6 @@ struct Zero {
     uint64_t stride, width, rows;
     uint32_t parts;
 };
-constexpr uint64_t kZeroPart = kSortThreads * 16;
 
 // The 16-byte pieces first, first + step, ... of p[0, n), and the 16-bit values before and behind the
 // aligned ones.
@@ -177,15 +176,18 @@ __device__ __forceinline__ void zero_bytes(uint8_t *p, uint64_t n, uint64_t firs
         *reinterpret_cast<uint16_t *>(p + (b < head ? b : tail + (b - head))) = 0;
 }
 
+template <uint32_t THREADS>
 __device__ __forceinline__ void zero_part(const Zero &z, uint32_t part)
 {
     if (z.rows == 1) {
-        zero_bytes(z.p, z.width, (uint64_t)part * kSortThreads + threadIdx.x, (uint64_t)z.parts * kSortThreads);
+        zero_bytes(z.p, z.width, (uint64_t)part * THREADS + threadIdx.x, (uint64_t)z.parts * THREADS);
         return;
     }
-    for (uint64_t r = part * kSortWaves + threadIdx.x / 64; r < z.rows; r += (uint64_t)z.parts * kSortWaves)
+    for (uint64_t r = (uint64_t)part * (THREADS / 64) + threadIdx.x / 64; r < z.rows; r += (uint64_t)z.parts * (THREADS / 64))
         zero_bytes(z.p + r * z.stride, z.width, threadIdx.x % 64, 64);
 }
+
+__global__ __launch_bounds__(256) void zero_kernel(Zero z) { zero_part<256>(z, blockIdx.x); }
 
 // All passes by one workgroup, up to kSortBlock ids. Keys and places go from pass to pass through
 // LDS.
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_small_kernel(SortSmall g, Z
 {
     __shared__ SortLds<K> l;
     if (blockIdx.x)
-        zero_part(z, blockIdx.x - 1);
+        zero_part<kSortThreads>(z, blockIdx.x - 1);
     else
         sort_small(g, l);
 }
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(1024) void sums_before_kernel(uint32_t *counts, uin
 {
     __shared__ uint32_t sums[16];
     if (blockIdx.x) {
-        zero_part(z, blockIdx.x - 1);
+        zero_part<kSortThreads>(z, blockIdx.x - 1);
         return;
     }
     const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -397,6 +399,7 @@ __device__ __forceinline__ void put_row(const Out &o, uint64_t row, uint32_t c, 
 // through all ids for them, and writes its rows once, sums and zeros. Its waves look through a part
 // of the ids each; what they find, one list after the other, is in the order of the tokens.
 constexpr uint32_t kOwnWaves = 16, kOwnMost = 2048;
+constexpr uint32_t kTokensMost = 1024;
 constexpr uint32_t kOwnAlone = 8;   // tokens of a row that its wave adds up alone
 
 struct Owned {
@@ -511,6 +514,79 @@ __global__ __launch_bounds__(64 * kOwnWaves, 8) void owned_kernel(Owned g)
         }
         __syncthreads();
     }
+}
+
+// Few tokens of a large table: no sorting either. A workgroup has one token and 512 columns, and looks for
+// the token's id in all of them, a quarter to each wave. The first token of an id adds up all of
+// them, each wave those that it found, and their sums are added in the order of the waves: in that
+// of the tokens.
+template <uint32_t T, uint32_t OT>
+__global__ __launch_bounds__(256) void tokens_kernel(Owned g)
+{
+    constexpr int B = T == kFp32 ? 8 : 16;   // rows on their way at once
+    constexpr uint32_t K = kTokensMost / 256;
+    __shared__ uint16_t list[4][64 * K];
+    __shared__ uint32_t count[4], before[4];
+    __shared__ float part[3][512];
+    const uint32_t t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t token = blockIdx.x / g.tiles, c = (blockIdx.x - token * g.tiles) * 512 + lane * 8;
+    const int64_t id = id_of(g.ids, token);
+    if (id < 0 || id >= (int64_t)g.rows)   // the whole workgroup
+        return;
+    const uint32_t per = (g.n + 255) / 256 * 64;
+    int64_t ids[K];
+#pragma unroll
+    for (uint32_t k = 0; k < K; ++k) {
+        const uint32_t at = wave * per + k * 64 + lane;
+        ids[k] = k * 64 < per && at < g.n ? id_of(g.ids, at) : -1;
+    }
+    uint32_t m = 0;
+    bool early = false;
+#pragma unroll
+    for (uint32_t k = 0; k < K; ++k) {
+        const uint32_t at = wave * per + k * 64 + lane;
+        const bool same = ids[k] == id;
+        const uint64_t lanes = __ballot(same);
+        if (same)
+            list[wave][m + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0))] = (uint16_t)at;
+        early |= same && at < token;
+        m += (uint32_t)__popcll(lanes);
+    }
+    if (lane == 0)
+        count[wave] = m;
+    early = __ballot(early) != 0;
+    if (lane == 0)
+        before[wave] = early;
+    __syncthreads();
+    if (before[0] | before[1] | before[2] | before[3])   // another one's
+        return;
+    float sum[8] = {};
+    if (c < g.cols)
+        for (uint32_t i = 0; i < m; i += B) {
+            Raw8<T> raw[B];
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                if (i + j < m)
+                    raw[j].load(g.dy.p, list[wave][i + j] * g.dy.ld, c, g.cols, true);
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                if (i + j < m)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sum[e] += (float)raw[j].v[e];
+        }
+    if (wave && m)
+        store8<kFp32>(part[wave - 1], 0, lane * 8, 512, sum);
+    __syncthreads();
+    if (wave || c >= g.cols)
+        return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+        if (count[w + 1])
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                sum[e] += part[w][lane * 8 + e];
+    put_row<OT>(g.out, (uint64_t)id, c, g.cols, sum, g.scale);
 }
 
 // The sums of kChunk sorted tokens, 8 columns to a lane, a wave to a workgroup. All of the tokens' rows
@@ -645,8 +721,6 @@ hipError_t launch_mx_embedding(const Embedding &e, hipStream_t s)
 
 namespace {
 
-constexpr uint64_t kMostParts = (1u << 22) - 2;   // workgroups of 1024 threads: fewer than 2^32 of these
-
 uint64_t round16(uint64_t v) { return (v + 15) / 16 * 16; }
 
 struct GradPlan {
@@ -673,20 +747,30 @@ GradPlan plan_of(uint64_t m, uint64_t rows, uint64_t cols)
     return p;
 }
 
-// Whether few tokens' gradient goes without sorting: where no row has many of them on average, and few
-// workgroups have to look through the ids. (us sorted, owned, bf16: 1001 tokens, 5003 x 1111: 22.6, 13.7; 2048
+enum Unsorted : int { kSorted, kOwned, kTokens };
+
+// How few tokens' gradient goes without sorting. By the table's rows, where no row has many tokens on average
+// and few workgroups have to look through the ids. (us sorted, owned, bf16: 1001 tokens, 5003 x 1111: 22.6, 13.7; 2048
 // tokens, 5003 x 1111: 28.9, 18.4; 1 token, 32768 x 512, 2048 workgroups: 13.6, 17.4; 1001 tokens, 20000 x 1024, 2500
-// workgroups: 23.0, 23.6; 500 and 2048 tokens, 100 x 4096: 14.1, 11.2 and 17.4, 31.7.)
-bool owned(uint64_t m, uint64_t rows, uint64_t cols)
+// workgroups: 23.0, 23.6; 500 and 2048 tokens, 100 x 4096: 14.1, 11.2 and 17.4, 31.7.) By the tokens, where the table is
+// large and no launch of theirs is. (us sorted, by tokens: 87 tokens, 25917 x 615: 27.4, 16.9; 204 tokens, 11520 x 8192:
+// 75.9, 64.6; 1001 tokens, 20000 x 1024 23.7, 19.4, 32768 x 4096, 8008 workgroups, 102.3, 102.2; 2048 tokens, 32768 x 1024:
+// 30.6, 33.9.)
+Unsorted unsorted(uint64_t m, uint64_t rows, uint64_t cols)
 {
-    return m && m <= kOwnMost && m <= 8 * rows && (rows + kOwnWaves - 1) / kOwnWaves * ((cols + 511) / 512) <= 1536;
+    const uint64_t tiles = (cols + 511) / 512;
+    if (m == 0 || m > kOwnMost || m > 8 * rows)
+        return kSorted;
+    if ((rows + kOwnWaves - 1) / kOwnWaves * tiles <= 1536)
+        return kOwned;
+    return m <= kTokensMost && m * tiles <= 8192 ? kTokens : kSorted;
 }
 
 }  // namespace
 
 uint64_t mx_embedding_grad_work(uint64_t m, uint64_t rows, uint64_t cols)
 {
-    return m && rows && cols && !owned(m, rows, cols) ? plan_of(m, rows, cols).bytes() : 0;
+    return m && rows && cols && unsorted(m, rows, cols) == kSorted ? plan_of(m, rows, cols).bytes() : 0;
 }
 
 hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
@@ -694,7 +778,24 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
     if (e.rows == 0 || e.cols == 0)
         return hipSuccess;
     hipError_t err;
-    if (owned(e.m, e.rows, e.cols)) {
+    const uint64_t size = mx_type_size(e.otype);
+    const bool whole = e.dw.ld == e.cols || e.rows == 1;
+    const Unsorted way = unsorted(e.m, e.rows, e.cols);
+    // Zeros by workgroups of so many threads, 16 bytes to each.
+    auto zeros = [&](uint32_t threads) {
+        Zero z = {reinterpret_cast<uint8_t *>(e.dw.p), e.dw.ld * size, (whole ? e.rows : 1) * e.cols * size, whole ? 1 : e.rows, 0};
+        const uint64_t parts = whole ? (z.width + threads * 16 - 1) / (threads * 16) : (z.rows + threads / 64 - 1) / (threads / 64);
+        const uint64_t most = 0xFFFFFF00u / threads - 1;   // (a launch has fewer than 2^32 threads)
+        z.parts = (uint32_t)(parts < most ? parts : most);
+        return z;
+    };
+    if (way != kSorted) {
+        if (way == kTokens && !e.accumulate) {
+            const Zero z = zeros(256);
+            hipLaunchKernelGGL(zero_kernel, dim3(z.parts), dim3(256), 0, s, z);
+            if ((err = hipGetLastError()) != hipSuccess)
+                return err;
+        }
         Owned g = {};
         g.ids = e.ids;
         g.n = (uint32_t)e.m;
@@ -704,21 +805,21 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
         g.dy = e.dy;
         g.scale = e.scale;
         g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate, nullptr};
-        const dim3 grid((uint32_t)((e.rows + kOwnWaves - 1) / kOwnWaves) * g.tiles);
+        const dim3 grid((way == kOwned ? (uint32_t)((e.rows + kOwnWaves - 1) / kOwnWaves) : g.n) * g.tiles);
         MX_TYPE(e.type, {
             constexpr uint32_t D = T;
-            MX_TYPE(e.otype, hipLaunchKernelGGL((owned_kernel<D, T>), grid, dim3(64 * kOwnWaves), 0, s, g));
+            MX_TYPE(e.otype, {
+                if (way == kOwned)
+                    hipLaunchKernelGGL((owned_kernel<D, T>), grid, dim3(64 * kOwnWaves), 0, s, g);
+                else
+                    hipLaunchKernelGGL((tokens_kernel<D, T>), grid, dim3(256), 0, s, g);
+            });
         });
         return hipGetLastError();
     }
     Zero z = {};
-    if (!e.accumulate) {
-        const uint64_t size = mx_type_size(e.otype);
-        const bool whole = e.dw.ld == e.cols || e.rows == 1;
-        z = {reinterpret_cast<uint8_t *>(e.dw.p), e.dw.ld * size, (whole ? e.rows : 1) * e.cols * size, whole ? 1 : e.rows, 0};
-        const uint64_t parts = whole ? (z.width + kZeroPart - 1) / kZeroPart : (z.rows + kSortWaves - 1) / kSortWaves;
-        z.parts = (uint32_t)(parts < kMostParts ? parts : kMostParts);
-    }
+    if (!e.accumulate)
+        z = zeros(kSortThreads);
     if (e.m == 0) {
         if (!z.parts)
             return hipSuccess;

@@ -74,7 +74,9 @@ SPREADS = {"any": lambda m, v, gen: torch.randint(0, v, (m,), device="cuda", gen
 @pytest.mark.parametrize("spread", list(SPREADS))
 @pytest.mark.parametrize("m,v,k,t,pad", [(1, 1, 1, "fp32", 0), (31, 7, 40, "bf16", 0), (32, 300, 33, "fp16", 5),
                                          (33, 255, 64, "fp32", 0), (1001, 5003, 111, "bf16", 3), (16384, 70000, 8, "fp32", 0),
-                                         (16385, 256, 16, "bf16", 0), (40000, 3000, 24, "fp16", 0), (100, 65536, 2100, "bf16", 0)])
+                                         (16385, 256, 16, "bf16", 0), (40000, 3000, 24, "fp16", 0), (100, 65536, 2100, "bf16", 0),
+                                         (1, 25000, 600, "fp32", 0), (777, 26000, 515, "fp16", 3), (1024, 24700, 516, "bf16", 0),
+                                         (1025, 24700, 520, "fp32", 0), (2048, 3000, 70, "bf16", 0)])
 def test_embedding_grad(spread, m, v, k, t, pad):
     gen = generator(m + v)
     ids, dy = SPREADS[spread](m, v, gen), rows(m, k, TYPES[t], gen, pad)
@@ -85,7 +87,7 @@ def test_embedding_grad(spread, m, v, k, t, pad):
     close(got, want, off)
     for _ in range(2):   # the same every time
         assert torch.equal(F.mx4_embedding_grad(dy, ids, v, scale=scale), got)
-    if v * k < 1 << 22:
+    if v * k < 1 << 24:
         for dtype in (torch.bfloat16, torch.float16):
             close(F.mx4_embedding_grad(dy, ids, v, scale=scale, dtype=dtype), want, off, dtype)
         base = torch.randn(v, k + 3, device="cuda", generator=gen)
