@@ -74,7 +74,8 @@ __device__ __forceinline__ void load8(const void *base, uint64_t row_off, uint32
 }
 
 // Eight elements of a row as they lie in memory. `once`: they are not read again, and the caches need
-// not keep them.
+// not keep them. Where the row ends inside them its last eight are read, and settle() moves them to
+// their place, zeros behind: not until they are used, so that no load waits for another.
 template <uint32_t T>
 struct Raw8 {
     typedef typename Elem<T>::type E;
@@ -83,17 +84,41 @@ struct Raw8 {
     Ex8 v;
     __device__ __forceinline__ void load(const void *base, uint64_t row_off, uint32_t c, uint32_t cols, bool once = false)
     {
-        const E *p = reinterpret_cast<const E *>(base) + row_off + c;
-        if (c + 8 <= cols) {
-            if (once)
-                v = __builtin_nontemporal_load(reinterpret_cast<const Any8 *>(p));
-            else
-                __builtin_memcpy(&v, p, sizeof v);
-        } else {
+        const E *row = reinterpret_cast<const E *>(base) + row_off;
+        if (cols < 8) {   // (the same for all)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                v[i] = c + i < cols ? p[i] : (E)0.0f;
+                v[i] = c + i < cols ? row[c + i] : (E)0.0f;
+            return;
         }
+        const uint32_t from = min(c, cols - 8);
+        if (once)
+            v = __builtin_nontemporal_load(reinterpret_cast<const Any8 *>(row + from));
+        else
+            __builtin_memcpy(&v, row + from, sizeof v);
+    }
+    __device__ __forceinline__ void settle(uint32_t c, uint32_t cols)
+    {
+        if (cols % 8 == 0 && c < cols)   // (the first is the same for all)
+            return;
+        const uint32_t late = cols < 8 || c + 8 <= cols ? 0 : c + 8 - cols;
+        if (late) {
+#pragma unroll
+            for (uint32_t step = 4; step; step /= 2)
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) {
+                    const E next = i + step < 8 ? v[(i + step) % 8] : (E)0.0f;
+                    v[i] = late & step ? next : v[i];
+                }
+            if (late >= 8)
+                v = Ex8((E)0.0f);
+        }
+    }
+    __device__ __forceinline__ void floats(float (&f)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = (float)v[i];
     }
 };
 

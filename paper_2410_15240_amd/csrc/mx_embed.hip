@@ -373,7 +373,8 @@ struct Sums {
     MxRows dy;
     float scale;
     Out out;
-    float *parts;                    // [chunks][2][cols]
+    float *parts;                    // [chunks][2][part_ld], whole units
+    uint32_t part_ld;
 };
 
 constexpr uint32_t kChunk = 16, kTileCols = 64 * 8;
@@ -471,10 +472,12 @@ __global__ __launch_bounds__(64 * kOwnWaves, 8) void owned_kernel(Owned g)
                     raw[j].load(g.dy.p, list[i + j] * g.dy.ld, c, g.cols);
 #pragma unroll
             for (int j = 0; j < B; ++j)
-                if (i + j < to)
+                if (i + j < to) {
+                    raw[j].settle(c, g.cols);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         sum[e] += (float)raw[j].v[e];
+                }
         }
     };
     uint32_t m = 0;
@@ -570,10 +573,12 @@ __global__ __launch_bounds__(256) void tokens_kernel(Owned g)
                     raw[j].load(g.dy.p, list[wave][i + j] * g.dy.ld, c, g.cols, true);
 #pragma unroll
             for (int j = 0; j < B; ++j)
-                if (i + j < m)
+                if (i + j < m) {
+                    raw[j].settle(c, g.cols);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         sum[e] += (float)raw[j].v[e];
+                }
         }
     if (wave && m)
         store8<kFp32>(part[wave - 1], 0, lane * 8, 512, sum);
@@ -624,6 +629,7 @@ __global__ __launch_bounds__(64) void sums_kernel(Sums g)
 #pragma unroll
     for (int i = 0; i < (int)kChunk; ++i) {
         if (i < (int)count && key_at(i) < g.rows) {   // (ids that name no row are sorted last)
+            raw[i].settle(c, g.cols);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 sum[e] += (float)raw[i].v[e];
@@ -631,7 +637,7 @@ __global__ __launch_bounds__(64) void sums_kernel(Sums g)
             if (last && here)
                 put_row<OT>(g.out, key_at(i), c, g.cols, sum, g.scale);
             else if (last || i + 1 == (int)kChunk)
-                store8<kFp32>(g.parts, ((uint64_t)chunk * 2 + here) * g.cols, c, g.cols, sum);
+                store8<kFp32>(g.parts, ((uint64_t)chunk * 2 + here) * g.part_ld, c, g.part_ld, sum);
             if (last) {
                 here = true;
 #pragma unroll
@@ -668,13 +674,13 @@ __global__ __launch_bounds__(64) void join_sums_kernel(Sums g)
     if (c >= g.cols)
         return;
     float sum[8];
-    load8<kFp32>(g.parts, ((uint64_t)chunk * 2 + 1) * g.cols, c, g.cols, sum);
+    load8<kFp32>(g.parts, ((uint64_t)chunk * 2 + 1) * g.part_ld, c, g.part_ld, sum);
     uint32_t k = chunk + 1;
     for (; k + 8 <= last + 1; k += 8) {   // 8 on their way at once, added in their order
         float v[8][8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            load8<kFp32>(g.parts, (uint64_t)(k + i) * 2 * g.cols, c, g.cols, v[i]);
+            load8<kFp32>(g.parts, (uint64_t)(k + i) * 2 * g.part_ld, c, g.part_ld, v[i]);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -683,7 +689,7 @@ __global__ __launch_bounds__(64) void join_sums_kernel(Sums g)
     }
     for (; k <= last; ++k) {
         float v[8];
-        load8<kFp32>(g.parts, (uint64_t)k * 2 * g.cols, c, g.cols, v);
+        load8<kFp32>(g.parts, (uint64_t)k * 2 * g.part_ld, c, g.part_ld, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             sum[e] += v[e];
@@ -743,7 +749,7 @@ GradPlan plan_of(uint64_t m, uint64_t rows, uint64_t cols)
     p.chunks = (uint32_t)((m + kChunk - 1) / kChunk);
     p.keys = round16(m * 4);
     p.counts = p.small ? 0 : round16(((uint64_t)p.blocks << p.bits) * 4);
-    p.parts = p.chunks > 1 ? (uint64_t)p.chunks * 2 * cols * 4 : 0;
+    p.parts = p.chunks > 1 ? (uint64_t)p.chunks * 2 * ((cols + 7) / 8 * 8) * 4 : 0;
     return p;
 }
 
@@ -886,6 +892,7 @@ hipError_t launch_mx_embedding_grad(const EmbeddingGrad &e, hipStream_t s)
     g.scale = e.scale;
     g.out = {e.dw.p, e.dw.ld, e.otype, e.accumulate, nullptr};
     g.parts = reinterpret_cast<float *>(at);
+    g.part_ld = (uint32_t)((e.cols + 7) / 8 * 8);
     const dim3 grid(g.chunks * g.tiles);
     MX_TYPE(e.type, {
         constexpr uint32_t D = T;

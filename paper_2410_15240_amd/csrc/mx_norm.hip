@@ -47,14 +47,23 @@ __device__ __forceinline__ float row_sum(float v, float (*lds)[16], int slot)
     return v;
 }
 
+template <uint32_t T>
+__device__ __forceinline__ void row8(const void *p, uint64_t row_off, uint32_t c, uint32_t cols, float (&v)[8])
+{
+    Raw8<T> r;
+    r.load(p, row_off, c, cols);
+    r.settle(c, cols);
+    r.floats(v);
+}
+
 // Eight of a weight vector, in the rows' type or in 32 bits.
 template <uint32_t T>
 __device__ __forceinline__ void weights8(const void *w, uint32_t wtype, uint32_t c, uint32_t cols, float (&v)[8])
 {
     if (T != kFp32 && wtype == kFp32)
-        load8<kFp32>(w, 0, c, cols, v);
+        row8<kFp32>(w, 0, c, cols, v);
     else
-        load8<T>(w, 0, c, cols, v);
+        row8<T>(w, 0, c, cols, v);
 }
 
 __device__ __forceinline__ Unit unit_at(uint64_t row, uint32_t j, uint32_t units)
@@ -128,7 +137,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
     if (n.w1) {
         float s = 0.0f;
         each([&](int i, uint32_t j) {
-            load8<T>(n.x.p, row * n.x.ld, j * 8, cols, h[i]);
+            row8<T>(n.x.p, row * n.x.ld, j * 8, cols, h[i]);
             s += square_sum(h[i]);
         });
         inv1 = inverse_rms<G>(s, cols, n.eps, lds, 0);
@@ -140,7 +149,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
         const Unit u = unit_at(row, j, units);
         float f[8];
         if (!U || !n.w1)
-            load8<T>(n.x.p, row * n.x.ld, u.c, cols, h[i]);
+            row8<T>(n.x.p, row * n.x.ld, u.c, cols, h[i]);
         if (n.w1)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -154,7 +163,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
                 h[i][e] *= f[e];
         }
         if (n.g.p) {
-            load8<T>(n.g.p, row * n.g.ld, u.c, cols, f);
+            row8<T>(n.g.p, row * n.g.ld, u.c, cols, f);
             if (keep)
                 put<kMx8>(n.gq, u, f);
 #pragma unroll
@@ -162,7 +171,7 @@ __global__ __launch_bounds__(threads_of<G>()) void norm_kernel(Norm n, uint64_t 
                 h[i][e] *= f[e];
         }
         if (n.r.p) {
-            load8<T>(n.r.p, row * n.r.ld, u.c, cols, f);
+            row8<T>(n.r.p, row * n.r.ld, u.c, cols, f);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 h[i][e] = __builtin_fmaf(h[i][e], n.scale, f[e]);
@@ -296,9 +305,7 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
     }
     for (uint64_t row = group; row < n.rows; row += groups) {
         const float inv2 = n.inv2[row], inv1 = n.w1 ? n.inv1[row] : 0.0f;
-        if (!AHEAD) {
-            fetch_first(row, now);
-        } else if (row + groups < n.rows) {
+        if (AHEAD && row + groups < n.rows) {
             fetch_first(row + groups, next);
             each([&](int i, uint32_t j) { fetch_rest(row + groups, next[i], j); });
         }
@@ -307,10 +314,14 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
         each([&](int i, uint32_t j) {
             if (!AHEAD)
                 weights8<T>(n.w2, n.wtype, j * 8, cols, w2[i]);
-            decode8_f32(now[i].u, scale8_f32(now[i].eu), a[i]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                d[i][e] = (float)now[i].dy.v[e];
+            if (AHEAD) {
+                decode8_f32(now[i].u, scale8_f32(now[i].eu), a[i]);
+                now[i].dy.settle(j * 8, cols);
+                now[i].dy.floats(d[i]);
+            } else {
+                get<kMx8>(n.u, unit_at(row, j, units), a[i]);
+                load8<T>(n.dy.p, row * n.dy.ld, j * 8, cols, d[i]);
+            }
             add(sum2[i], 0, j, d[i], a[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -321,21 +332,32 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
         const float along2 = row_sum<G>(s, lds, 0) / (float)cols;
         s = 0.0f;
         each([&](int i, uint32_t j) {
-            if (!AHEAD)
-                fetch_rest(row, now[i], j);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8; ++e)
                 d[i][e] = inv2 * __builtin_fmaf(-along2, a[i][e], d[i][e]);
-                if (n.dh.p)
-                    d[i][e] += (float)now[i].dh.v[e];
+            if (n.dh.p) {
+                float f[8];
+                if (AHEAD) {
+                    now[i].dh.settle(j * 8, cols);
+                    now[i].dh.floats(f);
+                } else {
+                    load8<T>(n.dh.p, row * n.dh.ld, j * 8, cols, f);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[i][e] += f[e];
             }
             if (n.dr.p)
                 store8<T>(n.dr.p, row * n.dr.ld, j * 8, cols, d[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 d[i][e] *= n.scale;
-            if (n.v.codes)
-                decode8_f32(now[i].v, scale8_f32(now[i].ev), a[i]);
+            if (n.v.codes) {
+                if (AHEAD)
+                    decode8_f32(now[i].v, scale8_f32(now[i].ev), a[i]);
+                else
+                    get<kMx8>(n.v, unit_at(row, j, units), a[i]);
+            }
             if (!AHEAD && n.w1)
                 weights8<T>(n.w1, n.wtype, j * 8, cols, w1[i]);
             if (n.gq.codes) {
@@ -344,7 +366,10 @@ __global__ __launch_bounds__(threads_of<G>(), 4) void norm_grad_kernel(NormGrad 
                 for (int e = 0; e < 8; ++e)
                     f[e] = d[i][e] * (n.w1 ? a[i][e] * w1[i][e] : a[i][e]);
                 store8<T>(n.dg.p, row * n.dg.ld, j * 8, cols, f);
-                decode8_f32(now[i].g, scale8_f32(now[i].eg), f);
+                if (AHEAD)
+                    decode8_f32(now[i].g, scale8_f32(now[i].eg), f);
+                else
+                    get<kMx8>(n.gq, unit_at(row, j, units), f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     d[i][e] *= f[e];
@@ -411,7 +436,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGrad n, uint32
         float along2 = 0.0f, d[8], a[8], w[8], s = 0.0f;
         auto begin = [&](uint32_t j, bool sums) {   // d = dy w2, a = u
             const Unit u = unit_at(row, j, units);
-            load8<T>(n.dy.p, row * n.dy.ld, u.c, cols, d);
+            row8<T>(n.dy.p, row * n.dy.ld, u.c, cols, d);
             get<kMx8>(n.u, u, a);
             weights8<T>(n.w2, n.wtype, u.c, cols, w);
             if (sums)
@@ -425,7 +450,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGrad n, uint32
             float f[8] = {};
             begin(j, false);
             if (n.dh.p)
-                load8<T>(n.dh.p, row * n.dh.ld, u.c, cols, f);
+                row8<T>(n.dh.p, row * n.dh.ld, u.c, cols, f);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 d[e] = inv2 * __builtin_fmaf(-along2, a[e], d[e]) + f[e];
@@ -558,7 +583,7 @@ hipError_t launch_mx_norm(const Norm &n, int num_cu, hipStream_t s)
 }
 
 // A unit to a thread, which leaves registers for the next row (4096 rows of 4096: 512 threads 50.8 us, 1024
-// 60.9); two up to 16384 columns (2048 such rows: 166 us, read again after each sum 240).
+// 60.9); two up to 16384 columns (2048 such rows: 142 us, read again after each sum 240).
 static Way backward_way(uint64_t cols)
 {
     const uint64_t units = 4 * mx_blocks(cols);

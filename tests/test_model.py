@@ -68,7 +68,7 @@ def test_workspaces(L):
     assert L.fastrack_mx_norm_grad_work_bytes(1 << 30, 8192, 1) <= 2 * 4 * 8192 * 8192
     assert L.fastrack_mx_embedding_grad_work_bytes(0, 10, 10) == 0
     assert L.fastrack_mx_embedding_grad_work_bytes(20, 10, 10) == 0
-    assert L.fastrack_mx_embedding_grad_work_bytes(3000, 10, 10) == 2 * 12000 + 188 * 2 * 40
+    assert L.fastrack_mx_embedding_grad_work_bytes(3000, 10, 10) == 2 * 12000 + 188 * 2 * 16 * 4
     assert L.fastrack_mx_embedding_grad_work_bytes(1 << 31, 10, 10) == 0
     assert L.fastrack_mx_loss_work_bytes(BF16, AT[0], 4096, 0, 1000, 4096) == 0
     # The logits of a large batch are never all there.
