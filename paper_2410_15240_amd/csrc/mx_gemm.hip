@@ -139,42 +139,37 @@ __device__ __forceinline__ void spread(const f32x16 (&acc)[N][N], int i, float *
 // The end of a tile of logits, of which their largest and the sum of their exponentials are left.
 // 64 rows at a time are in LDS, a quarter of a row to a thread, which holds it in registers between
 // the two; threads begin at different places of their quarters, for the banks. What bounds it is
-// v_exp_f32, 16 cycles of the 26 of a value: 6656 of a tile, whose products take 131072 with 4096
+// v_exp_f32, 16 cycles of the 30 of a value: 7680 of a tile, whose products take 131072 with 4096
 // inputs.
 struct StatEnd {
     LossTile a;
 
     template <bool EDGE, uint32_t C>   // EDGE: only the first `left` columns of the quarter are classes
-    __device__ __forceinline__ Stat stat(const f32x4 (&v)[C], const uint32_t (&x)[C], uint32_t left) const
+    __device__ __forceinline__ Stat stat(f32x4 (&v)[C], const uint32_t (&x)[C], uint32_t left) const
     {
         const float inf = __builtin_inff();
-        // The largest value (a NaN shows in the sum). A negative scale turns the order.
-        const bool turned = a.scale < 0.0f;
-        float top = turned ? inf : -inf;
+        float top = -inf;   // (a NaN shows in the sum)
 #pragma unroll
         for (uint32_t k = 0; k < C; ++k)
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
-                const float u = EDGE && x[k] + e >= left ? top : v[k][e];
-                top = turned ? fminf(top, u) : fmaxf(top, u);
+                v[k][e] *= a.scale;
+                top = fmaxf(top, EDGE && x[k] + e >= left ? -inf : v[k][e]);
             }
-        float other = quad_xor1(top);
-        top = turned ? fminf(top, other) : fmaxf(top, other);
-        other = quad_xor2(top);
-        top = turned ? fminf(top, other) : fmaxf(top, other);
-        const float scale2 = a.scale * kLog2e, base = __builtin_fabsf(top) == inf ? 0.0f : top * scale2;
+        top = fmaxf(top, quad_xor1(top));
+        top = fmaxf(top, quad_xor2(top));
+        const float base = base_of(top) * kLog2e;
         float sum = 0.0f;
 #pragma unroll
         for (uint32_t k = 0; k < C; ++k)
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k][e], scale2, -base));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(v[k][e], kLog2e, -base));
                 sum += EDGE && x[k] + e >= left ? 0.0f : p;
             }
         sum += quad_xor1(sum);
         sum += quad_xor2(sum);
-        // (Of infinite logits the scale's sign is kept; of none, or of NaN, any will do.)
-        return {__builtin_fabsf(top) == inf ? (turned ? -top : top) : top * a.scale, sum};
+        return {top, sum};
     }
 
     template <int N>
