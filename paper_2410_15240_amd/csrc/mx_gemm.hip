@@ -217,39 +217,48 @@ struct SlopeEnd {
     {
         constexpr uint32_t B = 64 * N, U = B / 8, R = 64 * U / kThreads;   // units of a row; rows of a thread
         const uint32_t t = threadIdx.x, x = t % U * 8, classes = min(B, g.n - n0);
+        const float scale2 = a.scale * kLog2e;
+        const bool fast = a.terms == 1 && __builtin_fabsf(scale2) < __builtin_inff();
+        // What a row needs, once for all, behind the 64 rows of logits: lse, factor, lse for 2^v, the
+        // target's column in the tile (-1: elsewhere, -2: no target).
+        f32x4 *const rows = reinterpret_cast<f32x4 *>(lds + 64 * B);
+        if (B >= kThreads || t < B) {
+            const uint32_t row = min(m0 + t, g.m - 1);
+            const int64_t id = id_of(a.ids, row), d = id - (int64_t)(a.v0 + n0);
+            const float lse = a.lse[row];
+            rows[t] = f32x4{lse, factor_of(a, row), lse * kLog2e, bits_f32(id < 0 ? -2u : d >= 0 && d < B ? (uint32_t)d : -1u)};
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float lse[R], factor[R];
-            int32_t at[R];   // the target in this thread's columns, -1 elsewhere, -2 for none
-#pragma unroll
-            for (uint32_t k = 0; k < R; ++k) {
-                const uint32_t y = t / U + k * (kThreads / U), row = min(m0 + (y >> 5) * 32 * N + i * 32 + (y & 31), g.m - 1);
-                const int64_t id = id_of(a.ids, row), d = id - (int64_t)(a.v0 + n0 + x);
-                lse[k] = a.lse[row];
-                factor[k] = factor_of(a, row);
-                at[k] = id < 0 ? -2 : d >= 0 && d < 8 ? (int32_t)d : -1;
-            }
             if (i)
                 __syncthreads();
             spread<N>(acc, i, lds);
             __syncthreads();
 #pragma unroll
             for (uint32_t k = 0; k < R; ++k) {
-                const uint32_t y = t / U + k * (kThreads / U), row = m0 + (y >> 5) * 32 * N + i * 32 + (y & 31);
+                const uint32_t y = t / U + k * (kThreads / U), in = (y >> 5) * 32 * N + i * 32 + (y & 31), row = m0 + in;
+                const f32x4 r = rows[in];
+                const float lse = r[0], factor = r[1];
+                const int32_t target = (int32_t)f32_bits(r[3]), at = target - (int32_t)x;
                 const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
                 const f32x4 lo = p[0], hi = p[1];
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                if (fast)   // (lse rounded once more, by 2^-24 of it: nothing beside the term's own rounding)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] = factor[k] * exp_of(__builtin_fmaf(v[e], a.scale, -lse[k]));
-                if (at[k] >= 0)
+                    for (int e = 0; e < 8; ++e)
+                        v[e] = factor * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], scale2, -r[2]));
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[e] = factor * exp_of(__builtin_fmaf(v[e], a.scale, -lse));
+                if (target >= 0 && at >= 0 && at < 8)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)   // (in one product: what e^0 - 1 leaves is not rounded away)
-                        v[e] = at[k] == e ? slope(__builtin_fmaf(reinterpret_cast<const float *>(p)[e], a.scale, -lse[k]), factor[k]) : v[e];
-                if (at[k] == -2 || classes < B)
+                        v[e] = at == e ? slope(__builtin_fmaf(reinterpret_cast<const float *>(p)[e], a.scale, -lse), factor) : v[e];
+                if (target == -2 || classes < B)
 #pragma unroll
                     for (uint32_t e = 0; e < 8; ++e)   // no gradient, whatever the logits are; no class
-                        v[e] = at[k] == -2 || x + e >= classes ? 0.0f : v[e];
+                        v[e] = target == -2 || x + e >= classes ? 0.0f : v[e];
                 if (row < g.m && n0 + x < a.ld)
                     put_terms(a.dz + row * a.ld + n0 + x, a.plane, a.terms, v);
             }

@@ -433,7 +433,7 @@ hipError_t launch_mx_loss(const Loss &l, int num_cu, hipStream_t s)
 
 hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
 {
-    if (l.n == 0)
+    if (l.n == 0 || (!l.dx.p && !l.x8.codes))
         return hipSuccess;
     if (l.m == 0) {   // no tokens: a head's gradient of zeros, or the one that is there
         LossPlan p = {};

@@ -78,14 +78,17 @@ __device__ __forceinline__ float quad_xor2(float v)
 // Eight values as bf16 terms, each the nearest to what those before leave.
 __device__ __forceinline__ void put_terms(uint16_t *p, uint64_t plane, uint32_t terms, float (&v)[8])
 {
-    for (uint32_t k = 0; k < terms; ++k) {
+    for (uint32_t k = 0;; ++k) {
         bf16x8 h;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 8; ++e)
             h[e] = (__bf16)v[e];
-            v[e] = __builtin_fabsf((float)h[e]) == __builtin_inff() ? 0.0f : v[e] - (float)h[e];
-        }
         *reinterpret_cast<bf16x8 *>(p + k * plane) = h;
+        if (k + 1 == terms)
+            return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = __builtin_fabsf((float)h[e]) == __builtin_inff() ? 0.0f : v[e] - (float)h[e];
     }
 }
 
