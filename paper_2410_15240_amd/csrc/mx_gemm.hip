@@ -243,7 +243,7 @@ struct SlopeEnd {
                 const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
                 const f32x4 lo = p[0], hi = p[1];
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                if (fast)   // (lse rounded once more, by 2^-24 of it: nothing beside the term's own rounding)
+                if (fast)   // (scale and lse rounded once more, by as much as lse is rounded itself)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         v[e] = factor * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], scale2, -r[2]));

@@ -403,6 +403,54 @@ def test_logits_that_are_all_far_from_zero(m, v, k, scale):
         assert bool((lse == math.inf).all())
 
 
+@pytest.mark.parametrize("m,v,k", [(40, 700, 64), (300, 9000, 64), (1200, 33000, 64)])
+def test_the_gradient_where_logits_are_all_far_from_zero(m, v, k):
+    """e^(z - lse) of large z and lse: each of the two, the scale and 1 / ln 2 in it are rounded (4 times 2^-24 of |z|, 2 more for
+    the sums of a logit), dz once in bf16 (2^-8), and dx."""
+    gen = generator(m * v)
+    w = F.mx4_quantize(torch.rand(v, k, device="cuda", generator=gen) + 0.5)
+    x = -(torch.rand(m, k, device="cuda", generator=gen) + 10).bfloat16()
+    ids = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    dloss = torch.rand(m, device="cuda", generator=gen) + 0.5
+    scale = 1.3
+    lse = F.mx4_cross_entropy(x, w, ids, scale=scale)[1]
+    dx, _ = F.mx4_cross_entropy_grad(dloss, x, w, ids, lse, scale=scale)
+    w64 = F.mx4_dequantize(w, dtype=torch.float32).double()
+    z = scale * x.double() @ w64.t()
+    assert bool((z < -400).all())
+    p = torch.exp(z - torch.logsumexp(z, 1, keepdim=True))
+    hot = torch.zeros_like(p).scatter_(1, ids[:, None], 1.0)
+    f = (dloss.double() * scale)[:, None]
+    off = f * ((p - hot).abs() * 2.0 ** -8 + p * z.abs() * 6 * 2.0 ** -24)
+    want, bound = f * (p - hot) @ w64, off @ w64.abs()
+    assert bool(((dx.double() - want).abs() <= bound * (1 + 2.0 ** -8) + want.abs() * 2.0 ** -8 + 1e-12).all())
+
+
+@pytest.mark.parametrize("m,v,k", [(5, 40, 64), (300, 9000, 64)])
+def test_a_gradient_with_the_largest_of_scales(m, v, k):
+    """Logits of zero stay zero at a scale of 3e38, though that over ln 2 is past the type: p is 1 / v."""
+    gen = generator(m + v + k)
+    w = F.mx4_quantize(torch.randn(v, k, device="cuda", generator=gen))
+    x = torch.zeros(m, k, device="cuda", dtype=torch.bfloat16)
+    ids = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    loss, lse = F.mx4_cross_entropy(x, w, ids, scale=3e38)
+    assert torch.allclose(loss, torch.full_like(loss, math.log(v)), rtol=1e-6)
+    dx, _ = F.mx4_cross_entropy_grad(torch.full_like(loss, 1e-38), x, w, ids, lse, scale=3e38)
+    w64 = F.mx4_dequantize(w, dtype=torch.float32).double()
+    hot = torch.zeros(m, v, device="cuda", dtype=torch.double).scatter_(1, ids[:, None], 1.0)
+    dz = 3.0 * (1.0 / v - hot)
+    want, bound = dz @ w64, dz.abs() @ w64.abs()
+    assert bool(((dx.double() - want).abs() <= bound * (2.0 ** -8 + 2.0 ** -20) + want.abs() * 2.0 ** -8).all())
+
+
+@pytest.mark.parametrize("m", [1, 300])
+def test_a_gradient_of_neither(m):
+    _, x, w, _, ids = head(m, 900, 64, "bf16", 3)
+    loss, lse = F.mx4_cross_entropy(x, w, ids)
+    assert F.mx4_cross_entropy_grad(torch.ones_like(loss), x, w, ids, lse, grad_input=False) == (None, None)
+    torch.cuda.synchronize()
+
+
 def test_no_tokens():
     _, x, w, _, ids = head(4, 60, 40, "bf16", 2)
     x8 = F.mx8_quantize(x[:0])
