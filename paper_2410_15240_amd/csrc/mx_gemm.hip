@@ -255,11 +255,11 @@ struct SlopeEnd {
                 else
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        v[e] = factor * exp_of(__builtin_fmaf(v[e], a.scale, -lse));
+                        v[e] = slope(__builtin_fmaf(v[e], a.scale, -lse), factor);
                 if (target >= 0 && at >= 0 && at < 8)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)   // (in one product: what e^0 - 1 leaves is not rounded away)
-                        v[e] = at == e ? slope(__builtin_fmaf(reinterpret_cast<const float *>(p)[e], a.scale, -lse), factor) : v[e];
+                        v[e] = at == e ? target_slope(__builtin_fmaf(reinterpret_cast<const float *>(p)[e], a.scale, -lse), factor) : v[e];
                 if (target == -2 || classes < B)
 #pragma unroll
                     for (uint32_t e = 0; e < 8; ++e)   // no gradient, whatever the logits are; no class

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void stat_kernel(const float *z, uint32_t
         const float base = base_of(s.top);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            s.sum += exp_of(v[i] - base);
+            s.sum += exp_of(minus(v[i], base));
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2)
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kRowThreads) void row_loss_kernel(const float *z, u
             const float base = base_of(u.top);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                u.sum += exp_of(v[k][i] - base);
+                u.sum += exp_of(minus(v[k][i], base));
             s = join(s, u);
         }
     }
@@ -149,8 +149,8 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_
 #pragma unroll
     for (int j = 0; j < 8; ++j)   // (a token that is left out: no gradient, whatever its logits are)
         v[j] = id < 0 || c + j >= n ? 0.0f
-               : at == j           ? slope(__builtin_fmaf(v[j], a.scale, -lse), factor)
-                                   : factor * exp_of(__builtin_fmaf(v[j], a.scale, -lse));
+               : at == j           ? target_slope(minus(v[j] * a.scale, lse), factor)
+                                   : slope(minus(v[j] * a.scale, lse), factor);
     put_terms(a.dz + row * a.ld + c, a.plane, a.terms, v);
 }
 

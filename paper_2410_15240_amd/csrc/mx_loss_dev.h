@@ -42,6 +42,14 @@ __device__ __forceinline__ float base_of(float top) { return __builtin_fabsf(top
 // The larger one; NaN where either is (fmaxf would drop it).
 __device__ __forceinline__ float larger(float a, float b) { return a > b || a != a ? a : b; }
 
+// a - b of a logit a as it is rounded to 32 bits. (Made one with the product that a comes from, as the compiler may,
+// the difference of a logit and itself would be what the product's rounding takes off: hundreds, of logits of 1e10.)
+__device__ __forceinline__ float minus(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a - b;
+}
+
 // e^v by the hardware's 2^v: off by 2^-23 of the result, and by |v| 2^-24 through the argument's rounding.
 constexpr float kLog2e = 1.44269504f;
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
@@ -62,8 +70,9 @@ __device__ __forceinline__ float factor_of(const LossTile &a, uint64_t row)
     return common != 0.0f ? common : a.dloss[row * a.dloss_step] * a.scale;
 }
 
-// The gradient of a target's logit, for v = z - lse.
-__device__ __forceinline__ float slope(float v, float factor) { return factor * (exp_of(v) - 1.0f); }
+// The gradient of a logit and of a target's, for v = z - lse.
+__device__ __forceinline__ float slope(float v, float factor) { return factor * exp_of(v); }
+__device__ __forceinline__ float target_slope(float v, float factor) { return factor * (exp_of(v) - 1.0f); }
 
 // The value of the lane next to this one, and of the one two further, within four.
 __device__ __forceinline__ float quad_xor1(float v)
