@@ -138,7 +138,9 @@ __device__ __forceinline__ void spread(const f32x16 (&acc)[N][N], int i, float *
 
 // The end of a tile of logits, of which their largest and the sum of their exponentials are left.
 // 64 rows at a time are in LDS, a quarter of a row to a thread, which holds it in registers between
-// the two; threads begin at different places of their quarters, for the banks. What bounds it is
+// the two; threads begin at different places of their quarters, for the banks. An exponential is one fma and
+// 2^v, with the largest value over ln 2 rounded; what that takes off it all have in common, and the sum is
+// multiplied by it. What bounds it is
 // v_exp_f32, 16 cycles of the 30 of a value: 7680 of a tile, whose products take 131072 with 4096
 // inputs.
 struct StatEnd {
@@ -158,7 +160,15 @@ struct StatEnd {
             }
         top = fmaxf(top, quad_xor1(top));
         top = fmaxf(top, quad_xor2(top));
-        const float base = base_of(top) * kLog2e;
+        float from = base_of(top), base = from * kLog2e;
+        if (!near(base)) {   // (logits of 1e7 and more)
+#pragma unroll
+            for (uint32_t k = 0; k < C; ++k)
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    v[k][e] = minus(v[k][e], from);
+            from = base = 0.0f;
+        }
         float sum = 0.0f;
 #pragma unroll
         for (uint32_t k = 0; k < C; ++k)
@@ -169,7 +179,7 @@ struct StatEnd {
             }
         sum += quad_xor1(sum);
         sum += quad_xor2(sum);
-        return {top, sum};
+        return {top, sum * rounding_of(base, from)};
     }
 
     template <int N>

@@ -54,6 +54,12 @@ __device__ __forceinline__ float minus(float a, float b)
 constexpr float kLog2e = 1.44269504f;
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 
+// e^(v - from) for many v and one `from` as 2^(v log2e - base), one fma, with base = from log2e as it is rounded: that is
+// off by the same factor for all v, 2 to what the rounding took off, and rounding_of() is the factor that makes up for it. As long
+// as that is no more than 2^0.5; else from is taken off v first, exactly where it matters.
+__device__ __forceinline__ bool near(float base) { return __builtin_fabsf(base) < 0x1p24f; }
+__device__ __forceinline__ float rounding_of(float base, float from) { return __builtin_amdgcn_exp2f(__builtin_fmaf(-from, kLog2e, base)); }
+
 // (Of no logits, or none but -inf, the sum is 0, whatever the other one's largest value makes of it.)
 __device__ __forceinline__ float over(const Stat &s, float base) { return s.sum == 0.0f ? 0.0f : s.sum * exp_of(base_of(s.top) - base); }
 

@@ -15,6 +15,8 @@ pytestmark = pytest.mark.gpu
 TYPES = O.TYPES
 # Logits through the workspace, their statistics in one launch and in parts.
 FEW = [(3, 700, 64), (40, 20000, 64), (300, 3000, 333)]
+# In whole tiles of 128 and of 256.
+TILES = [(600, 9000, 64), (2100, 9000, 300)]
 # A sum of exponentials: 66 additions in a thread, 20 joinings of five roundings each, the exponentials' own two units and what
 # their arguments' rounding makes of them (no more than the logarithm of the number of classes, 14, once and a quarter), the logarithm.
 SUM = 256 * O.U32
@@ -93,7 +95,7 @@ KINDS = [("bf16", 1.0), ("bf16", -1.3), ("fp16", 2.0 ** 8), ("fp16", 1.3 * 2.0 *
 
 
 @pytest.mark.parametrize("t,scale", KINDS)
-@pytest.mark.parametrize("m,v,k", FEW)
+@pytest.mark.parametrize("m,v,k", FEW + TILES)
 def test_the_loss_of_logits_of_any_size(t, scale, m, v, k):
     check_loss(*logits_of_any_size(t, scale, m, v, k))
 
