@@ -220,9 +220,10 @@ struct StatEnd {
 // those before leave: dloss (e^(z - lse) - [class = target]) times the scale.
 // What it adds to a tile's products is v_exp_f32 and the writing of 128 KB of terms, which most
 // workgroups do at once: 4096 tokens, 4096 x 32768, 880 us, the matrix unit busy 64% of the cycles
-// (71% with StatEnd). With a row's values loaded for every 32 rows, the logits' scaling and 2^v in two
-// products and the rounding's rest found after the last term too, 7092 instead of 6982 us for loss and
-// both gradients of 4096 tokens and 65536 classes.
+// (71% with StatEnd). With a row's values loaded for every 32 rows and the rounding's rest found after
+// the last term too, 100 us more of the 6980 for loss and both gradients of 4096 tokens and 65536 classes. The
+// scale and 1 / ln 2 in one factor would save 5, but logits have to be rounded as they were for lse: p of a class that
+// has all of a row is off by lse's last digits otherwise.
 struct SlopeEnd {
     LossTile a;
 
@@ -232,16 +233,15 @@ struct SlopeEnd {
     {
         constexpr uint32_t B = 64 * N, U = B / 8, R = 64 * U / kThreads;   // units of a row; rows of a thread
         const uint32_t t = threadIdx.x, x = t % U * 8, classes = min(B, g.n - n0);
-        const float scale2 = a.scale * kLog2e;
-        const bool fast = a.terms == 1 && __builtin_fabsf(scale2) < __builtin_inff();
-        // What a row needs, once for all, behind the 64 rows of logits: lse, factor, lse for 2^v, the
-        // target's column in the tile (-1: elsewhere, -2: no target).
+        // What a row needs, once for all, behind the 64 rows of logits: lse, its factor with what makes up
+        // for the rounding of the third, lse over ln 2, and the target's column in the tile (-1: elsewhere,
+        // -2: no target).
         f32x4 *const rows = reinterpret_cast<f32x4 *>(lds + 64 * B);
         if (B >= kThreads || t < B) {
             const uint32_t row = min(m0 + t, g.m - 1);
             const int64_t id = id_of(a.ids, row), d = id - (int64_t)(a.v0 + n0);
-            const float lse = a.lse[row];
-            rows[t] = f32x4{lse, factor_of(a, row), lse * kLog2e, bits_f32(id < 0 ? -2u : d >= 0 && d < B ? (uint32_t)d : -1u)};
+            const float lse = a.lse[row], base = lse * kLog2e, factor = factor_of(a, row);
+            rows[t] = f32x4{lse, near(base) ? factor * rounding_of(base, lse) : factor, base, bits_f32(id < 0 ? -2u : d >= 0 && d < B ? (uint32_t)d : -1u)};
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -254,22 +254,29 @@ struct SlopeEnd {
                 const uint32_t y = t / U + k * (kThreads / U), in = (y >> 5) * 32 * N + i * 32 + (y & 31), row = m0 + in;
                 const f32x4 r = rows[in];
                 const float lse = r[0], factor = r[1];
+                float base = r[2];
                 const int32_t target = (int32_t)f32_bits(r[3]), at = target - (int32_t)x;
                 const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + y * B + (x ^ ((y & 4) << 3)));
                 const f32x4 lo = p[0], hi = p[1];
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                if (fast)   // (scale and lse rounded once more, by as much as lse is rounded itself)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] *= a.scale;
+                if (!near(base)) {   // (logits of 1e7 and more)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        v[e] = factor * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], scale2, -r[2]));
-                else
+                        v[e] = minus(v[e], lse);
+                    base = 0.0f;
+                }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[e] = slope(__builtin_fmaf(v[e], a.scale, -lse), factor);
-                if (target >= 0 && at >= 0 && at < 8)
+                for (int e = 0; e < 8; ++e)
+                    v[e] = factor * __builtin_amdgcn_exp2f(__builtin_fmaf(v[e], kLog2e, -base));
+                if (target >= 0 && at >= 0 && at < 8) {
+                    const float own = factor_of(a, row < g.m ? row : g.m - 1);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)   // (in one product: what e^0 - 1 leaves is not rounded away)
-                        v[e] = at == e ? target_slope(__builtin_fmaf(reinterpret_cast<const float *>(p)[e], a.scale, -lse), factor) : v[e];
+                        v[e] = at == e ? target_slope(minus(reinterpret_cast<const float *>(p)[e] * a.scale, lse), own) : v[e];
+                }
                 if (target == -2 || classes < B)
 #pragma unroll
                     for (uint32_t e = 0; e < 8; ++e)   // no gradient, whatever the logits are; no class

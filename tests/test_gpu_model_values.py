@@ -101,6 +101,6 @@ def test_the_loss_of_logits_of_any_size(t, scale, m, v, k):
 
 
 @pytest.mark.parametrize("t,scale", KINDS)
-@pytest.mark.parametrize("m,v,k", FEW)
+@pytest.mark.parametrize("m,v,k", FEW + TILES)
 def test_the_gradient_of_logits_of_any_size(t, scale, m, v, k):
     check_grad(*logits_of_any_size(t, scale, m, v, k), t)
