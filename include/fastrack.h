@@ -542,6 +542,7 @@ int fastrack_mx_norm_grad(uint32_t type, const void *d_dy, uint64_t ld_dy, const
  * Softmax cross entropy over n classes whose head w [n][k] is in MX4, without keeping the
  * logits z[t][v] = scale * sum over k of x[t][k] w[v][k] (products as in mx_linear):
  *   lse[t] = log sum over v of e^z[t][v],  loss[t] = lse[t] - z[t][id_t]
+ * (the loss from the logits' differences, not from lse as it is rounded).
  * A negative id leaves its token out: loss 0, no gradient (its lse is written). An id of n
  * or more is a mistake that the device alone can see: its loss and lse are NaN, and all
  * gradients that it counts for.

@@ -16,12 +16,15 @@ namespace mx {
 
 constexpr int kThreads = 256;
 
-// A token's loss. A target that is no class makes what comes of it a NaN.
+// A token's loss, from the largest logit and not from lse, whose rounding would be all that is left of a small one.
+// (What the sum of an exponential of 1 and others is off may be on the other side of 1.) A target that is no class
+// makes what comes of it a NaN.
 __device__ __forceinline__ void put_loss(const Stat &s, int64_t id, uint32_t n, float label, uint32_t row, float *loss, float *lse)
 {
-    const float v = id >= (int64_t)n ? __builtin_nanf("") : base_of(s.top) + logf(s.sum);
-    lse[row] = v;
-    loss[row] = id < 0 ? 0.0f : v - label;
+    const bool wrong = id >= (int64_t)n;
+    const float base = base_of(s.top), above = logf(s.sum), v = minus(base, label) + above;
+    lse[row] = wrong ? __builtin_nanf("") : base + above;
+    loss[row] = id < 0 ? 0.0f : wrong ? __builtin_nanf("") : v < 0.0f ? 0.0f : v;
 }
 
 // One workgroup: kThreads * 8 classes of a row.

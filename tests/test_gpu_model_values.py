@@ -104,3 +104,30 @@ def test_the_loss_of_logits_of_any_size(t, scale, m, v, k):
 @pytest.mark.parametrize("m,v,k", FEW + TILES)
 def test_the_gradient_of_logits_of_any_size(t, scale, m, v, k):
     check_grad(*logits_of_any_size(t, scale, m, v, k), t)
+
+
+def logits_of_thousands(t, m, v, k):
+    """Hundreds and thousands that differ by some."""
+    gen = generator(m * 7 + v)
+    w = torch.randint(-4, 5, (v, k), device="cuda", generator=gen).float()
+    w[:, 0] = 6.0
+    w[v // 2, 1] = 6.0
+    w = F.mx4_quantize(w)
+    w64 = F.mx4_dequantize(w, dtype=torch.float32).double()
+    x = torch.zeros(m, k, device="cuda")
+    x[:, 0] = torch.randint(-2047, 2048, (m,), device="cuda", generator=gen).float().bfloat16().float()
+    x[:, 1] = torch.randint(1, 256, (m,), device="cuda", generator=gen).float() / 32     # 20 bits in all
+    x = x.to(TYPES[t])
+    z = x.double()[:, :2] @ w64[:, :2].t()
+    assert torch.equal(z, z.float().double())
+    return x, w, targets(m, v, gen, v // 2), 1.0, z
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("m,v,k", FEW + TILES)
+def test_a_loss_that_is_small_beside_its_logits_keeps_its_digits(t, m, v, k):
+    x, w, ids, scale, z = logits_of_thousands(t, m, v, k)
+    check_loss(x, w, ids, scale, z)
+    check_grad(x, w, ids, scale, z, t)
+    loss = F.mx4_cross_entropy(x, w, z.argmax(dim=1), scale=scale)[0]
+    assert bool((loss >= 0).all()) and bool((loss[x[:, 1] > 4] < math.log(v)).all())
