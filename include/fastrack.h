@@ -543,9 +543,10 @@ int fastrack_mx_norm_grad(uint32_t type, const void *d_dy, uint64_t ld_dy, const
  * logits z[t][v] = scale * sum over k of x[t][k] w[v][k] (products as in mx_linear):
  *   lse[t] = log sum over v of e^z[t][v],  loss[t] = lse[t] - z[t][id_t]
  * (the loss from the logits' differences, not from lse as it is rounded).
- * A negative id leaves its token out: loss 0, no gradient (its lse is written). An id of n
- * or more is a mistake that the device alone can see: its loss and lse are NaN, and all
- * gradients that it counts for.
+ * A negative id leaves its token out: loss 0, no gradient, whatever x and the kept x hold there
+ * (its lse is written). An id of n or more is a mistake that the device alone can see: its
+ * loss and lse are NaN, and all gradients that it counts for. (Where w holds a NaN or an
+ * infinity, every lse and all of dx have it.)
  *   loss_grad  dz[t][v] = scale * dloss[t] * (e^(z[t][v] - lse[t]) - [v = id_t])
  *              dx[t][k] = sum over v of dz[t][v] w[v][k]   (d_dx NULL: not computed)
  *              dw[v][k] = sum over t of dz[t][v] x^[t][k], x kept in MX8 (d_dw NULL: not

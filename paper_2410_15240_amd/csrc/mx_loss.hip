@@ -136,10 +136,24 @@ __global__ __launch_bounds__(kThreads) void loss_kernel(const Stat *stats, uint3
     }
 }
 
+// The scales of the kept x as the head's gradient takes them: the smallest one where a token is left out. Its dz is
+// 0, but 0 times the NaN that a block of its stands for (x of a padded or masked token is anything) would be in
+// the sum.
+struct Kept {
+    const uint8_t *scales;   // [m][blocks]
+    uint8_t *counted;        // null: they are there already, or no such gradient is wanted
+    uint32_t blocks;
+    __device__ __forceinline__ void count(uint64_t row, int64_t id, uint32_t b, uint32_t step) const
+    {
+        for (; b < blocks; b += step)
+            counted[row * blocks + b] = id < 0 ? 0 : scales[row * blocks + b];
+    }
+};
+
 // The logits' gradient, dloss (e^(z - lse) - [class = target]) times the scale, as bf16 terms in rows of
 // a.ld values that end in zeros.
 __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_t m, uint32_t n, uint32_t per_row, uint32_t recip, uint64_t row0,
-                                                         LossTile a)
+                                                         LossTile a, Kept kept)
 {
     const uint32_t i = blockIdx.x * kThreads + threadIdx.x, r = div_recip(i, per_row, recip), c = (i - r * per_row) * 8;
     const uint64_t row = row0 + r;
@@ -149,6 +163,8 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_
     load8<kFp32>(z, row * n, c, n, v);
     const int64_t id = id_of(a.ids, row), at = id - (int64_t)a.v0 - c;
     const float lse = a.lse[row], factor = factor_of(a, row);
+    if (kept.counted)
+        kept.count(row, id, c / 8, per_row);
 #pragma unroll
     for (int j = 0; j < 8; ++j)   // (a token that is left out: no gradient, whatever its logits are)
         v[j] = id < 0 || c + j >= n ? 0.0f
@@ -163,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(const float *z, uint32_
 // whatever factor, all of them would be off by the same part, up to 2^-8, while the model is unsure
 // (p near 0); of 255 / 128 itself nothing is lost, and of what lies below it least. Where the tokens have
 // several factors (or one far from 1, or none) out is 1 and 0, and each is rounded with its own.
-__global__ __launch_bounds__(1024) void common_kernel(LossTile a, uint32_t m, float *out)
+__device__ __forceinline__ void find_common(const LossTile &a, uint32_t m, float *out)
 {
     constexpr uint32_t K = 8;   // tokens of a thread at a time
     const uint32_t t = threadIdx.x;
@@ -207,6 +223,20 @@ __global__ __launch_bounds__(1024) void common_kernel(LossTile a, uint32_t m, fl
         out[0] = one ? factor / common : 1.0f;
         out[1] = one ? common : 0.0f;
     }
+}
+
+// What goes before whole tiles: the first workgroup finds the common factor (`out` null: none), the others
+// see to the tokens that are left out, one to a wave.
+__global__ __launch_bounds__(1024) void before_kernel(LossTile a, uint32_t m, float *out, Kept kept)
+{
+    const uint32_t finds = out ? 1 : 0;
+    if (blockIdx.x < finds) {
+        find_common(a, m, out);
+        return;
+    }
+    const uint32_t row = (blockIdx.x - finds) * 16 + threadIdx.x / 64;
+    if (row < m)
+        kept.count(row, id_of(a.ids, row), threadIdx.x % 64, 64);
 }
 
 // The result in its own type.
@@ -270,11 +300,12 @@ struct Width {
 struct LossPlan {
     uint64_t piece;
     Width whole, rest;                   // of a piece; of the last one, n = 0 if there is none of its own
-    uint64_t product, z, stats, label, dz, dx, common;   // bytes
+    uint64_t product, z, stats, label, dz, dx, common, counted;   // bytes
     uint32_t terms_x, terms_w;           // bf16 terms of the logits' gradient that the products take
     const float *common_at;              // the results' factor (null: 1)
+    uint8_t *counted_at;                 // the kept x's scales, of the tokens that count
     const Width &width(uint64_t left) const { return left >= whole.n ? whole : rest; }
-    uint64_t bytes() const { return product + z + stats + label + dz + dx + common; }
+    uint64_t bytes() const { return product + z + stats + label + dz + dx + common + counted; }
 };
 
 uint64_t parts_of(const Width &w) { return w.tile ? (w.n + w.tile - 1) / w.tile : (w.n + kStatCols - 1) / kStatCols; }
@@ -350,7 +381,7 @@ MxProduct back_w(const Loss &l, const LossPlan &p, const Width &w, uint64_t v0, 
 {
     MxProduct r = slopes(l, p, w, dz, p.terms_w);
     r.op = kWeightGrad;
-    r.q = l.x8;
+    r.q = {l.x8.codes, p.counted_at};
     r.ctype = l.dw_type;
     r.c = {reinterpret_cast<uint8_t *>(l.dw.p) + v0 * l.dw.ld * mx_type_size(l.dw_type), l.dw.ld};
     r.accumulate = l.accumulate;
@@ -364,6 +395,7 @@ LossPlan backward_plan(const Loss &l, int num_cu)
     p.terms_w = l.x8.codes ? terms_of(l.dw_type, l.m) : 0;
     const uint32_t terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
     p.common = p.terms_x == 1 || p.terms_w == 1 ? 256 : 0;   // (more terms round nothing that counts)
+    p.counted = l.x8.codes ? round_to(l.m * mx_blocks(l.k), 256) : 0;
     p.dx = l.dx.p && l.dx_type != kFp32 && p.whole.n < l.n ? round_to(l.m * l.k * 4, 256) : 0;
     void *const some_place = reinterpret_cast<void *>(256);   // (a plan asks where its float operand lies)
     for (const Width *w : {&p.whole, &p.rest}) {
@@ -447,8 +479,10 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
     uint8_t *const work = reinterpret_cast<uint8_t *>(l.work);
     float *const z = reinterpret_cast<float *>(work + p.product);
     uint8_t *const dz = work + p.product + p.z;
-    float *const dx = reinterpret_cast<float *>(dz + p.dz), *const common = reinterpret_cast<float *>(dz + p.dz + p.dx);
-    p.common_at = p.common ? common : nullptr;
+    float *const dx = reinterpret_cast<float *>(dz + p.dz);
+    uint8_t *const tail = dz + p.dz + p.dx;
+    p.common_at = p.common ? reinterpret_cast<float *>(tail) : nullptr;
+    p.counted_at = p.counted ? tail + p.common : nullptr;
     LossTile t = {};
     t.ids = l.ids;
     t.scale = l.scale;
@@ -457,13 +491,19 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
     t.dloss_step = l.dloss_step;
     t.dz = reinterpret_cast<uint16_t *>(dz);
     t.terms = p.terms_x > p.terms_w ? p.terms_x : p.terms_w;
-    t.common = p.common_at;
+    Kept kept = {l.x8.scales, p.counted_at, (uint32_t)mx_blocks(l.k)};
     hipError_t e;
-    if (p.common) {
-        hipLaunchKernelGGL(common_kernel, dim3(1), dim3(1024), 0, s, t, (uint32_t)l.m, common);
+    // (slope_kernel looks at the tokens itself.)
+    const uint32_t counts = p.counted && p.whole.tile ? (uint32_t)((l.m + 15) / 16) : 0;
+    if (p.common || counts) {
+        float *const common = p.common ? reinterpret_cast<float *>(tail) : nullptr;
+        hipLaunchKernelGGL(before_kernel, dim3((common ? 1 : 0) + counts), dim3(1024), 0, s, t, (uint32_t)l.m, common, kept);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
     }
+    if (counts)
+        kept.counted = nullptr;
+    t.common = p.common_at;
     for (; t.v0 < l.n; t.v0 += p.width(l.n - t.v0).n) {
         const Width &w = p.width(l.n - t.v0);
         MxProduct g = logits(l, t.v0, w.n, z);
@@ -479,10 +519,11 @@ hipError_t launch_mx_loss_grad(const Loss &l, int num_cu, hipStream_t s)
             const uint32_t per_row = (uint32_t)(t.ld / 8);
             e = over_rows(l.m, per_row, [&](uint64_t row0, dim3 grid) {
                 hipLaunchKernelGGL(slope_kernel, grid, dim3(kThreads), 0, s, z, (uint32_t)l.m, (uint32_t)w.n, per_row,
-                                   div_recip_of(per_row), row0, t);
+                                   div_recip_of(per_row), row0, t, kept);
             });
             if (e != hipSuccess)
                 return e;
+            kept.counted = nullptr;
         }
         if (l.dx.p) {
             const Out o = p.dx ? Out{dx, l.k, kFp32, t.v0 != 0, nullptr} : Out{l.dx.p, l.dx.ld, l.dx_type, t.v0 != 0, nullptr};

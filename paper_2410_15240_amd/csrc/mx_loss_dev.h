@@ -26,7 +26,7 @@ struct LossTile {
     uint16_t *dz;            // bf16 terms, rows of ld values
     uint64_t ld, plane;
     uint32_t terms;
-    const float *common;     // [2], see common_kernel (null: no common factor)
+    const float *common;     // [2], see find_common (null: no common factor)
 };
 
 // The side of the tiles in which `p` (kLinear) comes out whole, 0 where it does not.

@@ -131,3 +131,27 @@ def test_a_loss_that_is_small_beside_its_logits_keeps_its_digits(t, m, v, k):
     check_grad(x, w, ids, scale, z, t)
     loss = F.mx4_cross_entropy(x, w, z.argmax(dim=1), scale=scale)[0]
     assert bool((loss >= 0).all()) and bool((loss[x[:, 1] > 4] < math.log(v)).all())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("t,wt", [("bf16", "bf16"), ("bf16", "fp32"), ("fp16", "fp32"), ("fp32", "fp32")])
+@pytest.mark.parametrize("m,v,k", [(1, 50, 40), (29, 2777, 1003)] + FEW + TILES + [(600, 9000, 1024)])   # (the last: decoded once)
+def test_tokens_left_out_count_for_nothing_whatever_they_hold(t, wt, bad, m, v, k):
+    gen = generator(m + k)
+    w = F.mx4_quantize(torch.randn(v, k, device="cuda", generator=gen))
+    x = torch.randn(m, k, device="cuda", generator=gen).to(TYPES[t])
+    ids = torch.randint(0, v, (m,), device="cuda", generator=gen)
+    ids[torch.rand(m, device="cuda", generator=gen) < 0.3] = -100
+    ids[-1] = -1
+    out = ids < 0
+    results = []
+    for held in (0.0, bad):
+        x = torch.where(out[:, None], held, x).to(TYPES[t])
+        loss, lse = F.mx4_cross_entropy(x, w, ids)
+        for dloss in (torch.where(out, held, torch.rand(m, device="cuda", generator=generator(m))), torch.ones(m, device="cuda")):
+            dx, dw = F.mx4_cross_entropy_grad(dloss, x, w, ids, lse, saved=F.mx8_quantize(x), weight_dtype=TYPES[wt])
+            results.append((loss, torch.where(out, 0.0, lse), dx, dw))
+    for got in results[2:]:
+        for a, b in zip(got, results.pop(0)):
+            assert bool(a.isfinite().all()) and torch.equal(a, b)
+    assert bool((dx[out] == 0).all()) and bool((loss[out] == 0).all())
