@@ -507,11 +507,11 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGrad n, uint32
 }
 
 // Sums of 64 columns of `parts` rows, always in the same order: a wave takes every 16th row, the
-// waves' sums are added in theirs.
-__global__ __launch_bounds__(1024) void columns_kernel(const float *work, uint32_t parts, uint32_t cols, float *out0, float *out1)
+// waves' sums are added in theirs. c0: the launch's first column.
+__global__ __launch_bounds__(1024) void columns_kernel(const float *work, uint32_t parts, uint32_t cols, uint32_t c0, float *out0, float *out1)
 {
     __shared__ float lds[16][64];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = c0 + blockIdx.x * 64 + lane;
     const float *p = work + (uint64_t)blockIdx.y * parts * cols;
     float s = 0.0f;
     if (c < cols)
@@ -627,9 +627,16 @@ hipError_t launch_mx_norm_grad(const NormGrad &n, int num_cu, hipStream_t s)
         if (e != hipSuccess)
             return e;
     }
-    hipLaunchKernelGGL(columns_kernel, dim3((uint32_t)((n.cols + 63) / 64), n.w1 ? 2 : 1), dim3(1024), 0, s, n.work, groups,
-                       (uint32_t)n.cols, n.dw2, n.dw1);
-    return hipGetLastError();
+    const uint64_t most = 1ull << 26;   // columns of a launch: fewer than 2^32 threads for both weights
+    for (uint64_t c0 = 0; c0 < n.cols; c0 += most) {
+        const uint64_t c = n.cols - c0 < most ? n.cols - c0 : most;
+        hipLaunchKernelGGL(columns_kernel, dim3((uint32_t)((c + 63) / 64), n.w1 ? 2 : 1), dim3(1024), 0, s, n.work, groups,
+                           (uint32_t)n.cols, (uint32_t)c0, n.dw2, n.dw1);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace fastrack
