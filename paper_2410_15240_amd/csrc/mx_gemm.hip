@@ -219,7 +219,7 @@ struct StatEnd {
 // The end of a tile of logits that becomes their gradient, in bf16 terms, each the nearest to what
 // those before leave: dloss (e^(z - lse) - [class = target]) times the scale.
 // What it adds to a tile's products is v_exp_f32 and the writing of 128 KB of terms, which most
-// workgroups do at once: 4096 tokens, 4096 x 32768, 880 us, the matrix unit busy 64% of the cycles
+// workgroups do at once: 4096 tokens, 4096 x 32768, 883 us, the matrix unit busy 63% of the cycles
 // (71% with StatEnd). With a row's values loaded for every 32 rows and the rounding's rest found after
 // the last term too, 100 us more of the 6980 for loss and both gradients of 4096 tokens and 65536 classes. The
 // scale and 1 / ln 2 in one factor would save 5, but logits have to be rounded as they were for lse: p of a class that

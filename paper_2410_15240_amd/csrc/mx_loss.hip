@@ -321,8 +321,8 @@ using namespace mx;
 namespace {
 
 // Values of a piece: forwards no more than a launch has tiles for; backwards so many that the products
-// of a piece fill the GPU and their sums over it are long (4096 tokens, 4096 x 65536, us: 2^26 7190,
-// 2^27 6990, 2^28, which is all of them, 6880). Logits that go through the workspace, half as many.
+// of a piece fill the GPU and their sums over it are long (4096 tokens, 4096 x 65536, us: 2^26 6750,
+// 2^27 6580, 2^28, which is all of them, 6580). Logits that go through the workspace, half as many.
 constexpr uint64_t kForwardValues = 1ull << 34, kBackwardValues = 1ull << 27, kWorkspaceValues = 1ull << 26;
 
 LossPlan plan_of(const Loss &l, int num_cu, uint64_t values)
